@@ -54,7 +54,7 @@ typedef struct tb_cache_desc {
 } tb_cache_desc;
 
 /* Operation selector for tb_workspace_bytes. */
-enum { TB_OP_SELECT = 1, TB_OP_ATTN = 2, TB_OP_DECODE_STEP = 3 };
+enum { TB_OP_SELECT = 1, TB_OP_ATTN = 2, TB_OP_DECODE_STEP = 3, TB_OP_ATTN_MX = 4 };
 
 /* Key-cache projection (Sec. 3.1, "Key-cache projection": K_imp = K W_K, W_K in R^{D x Dimp}).
  * Fills K_imp[b,h,n,:] = round(K[b,h,n,:] . W[hw]) for n_begin <= n < n_end, fp32 accumulation,
@@ -236,6 +236,57 @@ typedef struct {
 tb_status tb_predict_queries(const tb_predictor_desc* p, int32_t B, const void* h, const void* gamma,
                              const void* beta, const void* W1, const void* b1, const void* W2, const void* b2,
                              float* hidden_act, float* ln_act, void* q_imp, void* stream);
+
+/* ---- a cache in microscaled 4-bit floating point ------------------------------------------------
+ * Rows of K, V and K_imp in OCP's MXFP4 format: a row is cut into blocks of 32 elements, each element a sign and one of
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 (E2M1), each block with a power of two (E8M0, 2^(byte - 127)) that multiplies its elements; byte 255
+ * makes all of them NaN.  4.25 bits an element instead of 16 or 32.
+ * codes : [B][Hkv][N][inner/2]   bytes; element 2i of a row in the low half of byte i, element 2i + 1 in the high half
+ * scales: [B][Hkv][N][inner/32]  bytes
+ * with inner = D (K, V) or Dimp (K_imp; 32 or 64: with 16 there is no whole block -> TB_ERR_UNSUPPORTED).  Strides are in bytes,
+ * the innermost dimension is contiguous; codes must be 16-byte aligned with strides that are multiples of 16, scales may lie
+ * anywhere.  N: rows that the arrays have room for.  K and V of a token next to each other (one allocation of codes
+ * [B][Hkv][N][2][D/2]) are read as one line.
+ * The descriptor of a call gives the shape, and the element type of the queries or of the rows that are converted; its strides are
+ * those of rows in that type, and are not looked at by calls that have none. */
+typedef struct tb_mx_rows {
+  void* codes;
+  void* scales;
+  int64_t N;
+  int64_t code_stride_b, code_stride_h, code_stride_n;
+  int64_t scale_stride_b, scale_stride_h, scale_stride_n;
+} tb_mx_rows;
+
+/* Rows src_row + i of K, V and K_imp (described by desc, rows [0, desc->N)) go to rows dst_row + i of Kq, Vq and Kimpq, 0 <= i <
+ * rows, in one launch: a prompt, or the new token of a decode step.  A pair (K, Kq), (V, Vq), (Kimp, Kimpq) of NULLs is left out.
+ * Per block: with the largest magnitude in [2^e, 2^(e+1)) the scale is 2^max(e - 2, -127), every element goes to the nearest
+ * multiple that a code stands for, halves to the even code, beyond 6 to 6 (OCP Microscaling Formats v1.0); a block of zeros has
+ * scale byte 0, and a block with an infinity or a NaN has byte 255 and codes 0.  Sources and destinations must not overlap.
+ * rows <= 2^20. */
+tb_status tb_quantize_mx(const tb_cache_desc* desc, const void* K, const void* V, const void* Kimp, int64_t src_row, const tb_mx_rows* Kq,
+                         const tb_mx_rows* Vq, const tb_mx_rows* Kimpq, int64_t dst_row, int64_t rows, void* stream);
+
+/* The way back: rows dst_row + i of K, V and K_imp receive the values that rows src_row + i of Kq, Vq and Kimpq stand for.  Exact in
+ * either element type. */
+tb_status tb_dequantize_mx(const tb_cache_desc* desc, const tb_mx_rows* Kq, const tb_mx_rows* Vq, const tb_mx_rows* Kimpq, int64_t src_row,
+                           void* K, void* V, void* Kimp, int64_t dst_row, int64_t rows, void* stream);
+
+/* tb_score over projected keys in 4 bits: the queries are taken as they are (fp32 or bf16), products are exact, sums fp32. */
+tb_status tb_score_mx(const tb_cache_desc* desc, const void* q_imp, const tb_mx_rows* Kimp, float scale, float* scores, int64_t score_stride,
+                      void* stream);
+
+/* tb_sparse_decode_attn over a cache in 4 bits: lists, dense range, results as there.  idx and count may be NULL with max_count = 0
+ * (the dense range alone: decode attention over all rows is tail_begin = 0, tail_end = N).  An attended row with a block that stands
+ * for NaN makes the row's weight or the block's outputs NaN, as the formula does; rows that are not attended add nothing,
+ * whatever they hold.  ws: tb_workspace_bytes(TB_OP_ATTN_MX, ...). */
+tb_status tb_sparse_decode_attn_mx(const tb_cache_desc* desc, const void* q, const tb_mx_rows* K, const tb_mx_rows* V, const int32_t* idx,
+                                   const int32_t* count, int64_t idx_cap, int64_t max_count, int64_t tail_begin, int64_t tail_end,
+                                   float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* The head-less form: one list per batch element for all of its heads, as tb_sparse_decode_attn_shared. */
+tb_status tb_sparse_decode_attn_shared_mx(const tb_cache_desc* desc, const void* q, const tb_mx_rows* K, const tb_mx_rows* V,
+                                          const int32_t* idx, const int32_t* count, int64_t idx_cap, int64_t max_count, int64_t tail_begin,
+                                          int64_t tail_end, float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /* Scratch size in bytes for `op` on this cache shape.  max_count is the longest list the
  * attention will see, tail included; for TB_OP_SELECT and TB_OP_DECODE_STEP it is the list

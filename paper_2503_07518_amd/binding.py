@@ -18,12 +18,15 @@ LIB_PATH = os.path.join(_PKG, "libtokenbutler.so")
 
 TB_OK, TB_ERR_INVALID_ARG, TB_ERR_UNSUPPORTED, TB_ERR_WORKSPACE, TB_ERR_HIP = 0, 1, 2, 3, 4
 TB_F32, TB_BF16 = 0, 1
-TB_OP_SELECT, TB_OP_ATTN, TB_OP_DECODE_STEP = 1, 2, 3
+TB_OP_SELECT, TB_OP_ATTN, TB_OP_DECODE_STEP, TB_OP_ATTN_MX = 1, 2, 3, 4
+MX_BLOCK = 32  # elements that share a scale in a 4-bit cache
 
 EXPORTS = (
     "tb_project_keys", "tb_score", "tb_select_topk", "tb_expand_neighbors", "tb_sparse_decode_attn",
     "tb_sparse_decode_attn_shared", "tb_sparse_decode_attn_static",
-    "tb_gather_kv", "tb_gather_important", "tb_append_kv", "tb_buffered_decode_attn", "tb_append_buffered_decode_attn", "tb_migrate_buffered_decode_attn", "tb_predict_queries", "tb_decode_step", "tb_workspace_bytes", "tb_workspace_init", "tb_read_stream_probe", "tb_status_string", "tb_version",
+    "tb_gather_kv", "tb_gather_important", "tb_append_kv", "tb_buffered_decode_attn", "tb_append_buffered_decode_attn", "tb_migrate_buffered_decode_attn", "tb_predict_queries", "tb_decode_step",
+    "tb_quantize_mx", "tb_dequantize_mx", "tb_score_mx", "tb_sparse_decode_attn_mx", "tb_sparse_decode_attn_shared_mx",
+    "tb_workspace_bytes", "tb_workspace_init", "tb_read_stream_probe", "tb_status_string", "tb_version",
 )
 
 
@@ -40,6 +43,14 @@ class tb_cache_desc(ctypes.Structure):
         ("k_stride_b", ctypes.c_int64), ("k_stride_h", ctypes.c_int64), ("k_stride_n", ctypes.c_int64),
         ("v_stride_b", ctypes.c_int64), ("v_stride_h", ctypes.c_int64), ("v_stride_n", ctypes.c_int64),
         ("ki_stride_b", ctypes.c_int64), ("ki_stride_h", ctypes.c_int64), ("ki_stride_n", ctypes.c_int64),
+    ]
+
+
+class tb_mx_rows(ctypes.Structure):
+    _fields_ = [
+        ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("N", ctypes.c_int64),
+        ("code_stride_b", ctypes.c_int64), ("code_stride_h", ctypes.c_int64), ("code_stride_n", ctypes.c_int64),
+        ("scale_stride_b", ctypes.c_int64), ("scale_stride_h", ctypes.c_int64), ("scale_stride_n", ctypes.c_int64),
     ]
 
 
@@ -82,6 +93,12 @@ def load_library() -> ctypes.CDLL:
     L.tb_migrate_buffered_decode_attn.argtypes = [dp, vp, vp, vp, vp, i64, i64, i32, i32, vp, i64, dp, vp, vp, vp, i64, vp, vp, i64, i64, i64, f32, vp, vp, vp,
                                                   sz, vp]
     L.tb_predict_queries.argtypes = [ctypes.POINTER(tb_predictor_desc), i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    mp = ctypes.POINTER(tb_mx_rows)
+    L.tb_quantize_mx.argtypes = [dp, vp, vp, vp, i64, mp, mp, mp, i64, i64, vp]
+    L.tb_dequantize_mx.argtypes = [dp, mp, mp, mp, i64, vp, vp, vp, i64, i64, vp]
+    L.tb_score_mx.argtypes = [dp, vp, mp, f32, vp, i64, vp]
+    L.tb_sparse_decode_attn_mx.argtypes = [dp, vp, mp, mp, vp, vp, i64, i64, i64, i64, f32, vp, vp, vp, sz, vp]
+    L.tb_sparse_decode_attn_shared_mx.argtypes = L.tb_sparse_decode_attn_mx.argtypes
     L.tb_workspace_bytes.argtypes = [i32, dp, i64]
     L.tb_workspace_bytes.restype = sz
     L.tb_workspace_init.argtypes = [vp, sz, vp]
@@ -165,6 +182,47 @@ def make_desc(N: int, Hq: int, K: Optional[torch.Tensor] = None, V: Optional[tor
             Dimp = 32
         ki = (0, 0, Dimp)
     return tb_cache_desc(B, Hq, Hkv, D, Dimp, _dtype_code(dtype), N, *k, *v, *ki)
+
+
+class MxRows:
+    """Rows in microscaled 4-bit floating point: codes uint8 [B, Hkv, N, inner / 2], scales uint8 [B, Hkv, N, inner / 32]."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        assert codes.dtype == scales.dtype == torch.uint8
+        assert codes.shape[:3] == scales.shape[:3] and codes.shape[3] * 2 == scales.shape[3] * MX_BLOCK
+        self.codes, self.scales = codes, scales
+        self.desc = tb_mx_rows(codes.data_ptr(), scales.data_ptr(), codes.shape[2], *_strides3(codes), *_strides3(scales))
+        self.ref = ctypes.byref(self.desc)
+
+    @property
+    def inner(self) -> int:
+        return self.codes.shape[3] * 2
+
+
+class MxCache:
+    """A layer's cache in microscaled 4-bit floating point, for Ncap tokens: K and V of a token side by side (a line of 128 bytes at
+    D = 128), and the projected keys (Dimp = 0: none)."""
+
+    def __init__(self, B: int, Hkv: int, Ncap: int, D: int, Dimp: int = 0, device="cuda"):
+        codes = torch.zeros((B, Hkv, Ncap, 2, D // 2), dtype=torch.uint8, device=device)
+        scales = torch.zeros((B, Hkv, Ncap, 2, D // MX_BLOCK), dtype=torch.uint8, device=device)
+        self.K, self.V = (MxRows(codes[:, :, :, t], scales[:, :, :, t]) for t in (0, 1))
+        self.Kimp = None
+        if Dimp:
+            self.Kimp = MxRows(torch.zeros((B, Hkv, Ncap, Dimp // 2), dtype=torch.uint8, device=device),
+                               torch.zeros((B, Hkv, Ncap, Dimp // MX_BLOCK), dtype=torch.uint8, device=device))
+
+
+def _mx(rows: Optional[MxRows]):
+    return None if rows is None else rows.ref
+
+
+def make_mx_desc(N: int, Hq: int, dtype: torch.dtype, K: Optional[MxRows] = None, Kimp: Optional[MxRows] = None) -> tb_cache_desc:
+    """Describe a layer whose rows are in 4 bits: its shape, and the element type of the queries."""
+    ref = K if K is not None else Kimp
+    B, Hkv = ref.codes.shape[:2]
+    D, Dimp = 128 if K is None else K.inner, 32 if Kimp is None else Kimp.inner
+    return tb_cache_desc(B, Hq, Hkv, D, Dimp, _dtype_code(dtype), N, 0, 0, D, 0, 0, D, 0, 0, Dimp)
 
 
 def tb_version() -> int:
@@ -329,6 +387,46 @@ def tb_decode_step(desc, q_imp, Kimp, score_scale: float, q, K, V, k: int, sink:
                                          _ptr(V), k, sink, window, sm_scale, _ptr(scores), scores.stride(-2),
                                          _ptr(idx), _ptr(count), idx.stride(-2), _ptr(out), _ptr(lse), _ptr(ws),
                                          ws.numel() * ws.element_size(), _stream(stream)), "tb_decode_step")
+
+
+def tb_quantize_mx(desc, K, V, Kimp, src_row: int, Kq: Optional[MxRows], Vq: Optional[MxRows], Kimpq: Optional[MxRows], dst_row: int,
+                   rows: int, stream=None) -> None:
+    """Rows src_row + i of K, V and Kimp (desc; None: left out) to rows dst_row + i of Kq, Vq and Kimpq, i < rows."""
+    _check(load_library().tb_quantize_mx(ctypes.byref(desc), _ptr(K), _ptr(V), _ptr(Kimp), src_row, _mx(Kq), _mx(Vq), _mx(Kimpq), dst_row,
+                                         rows, _stream(stream)), "tb_quantize_mx")
+
+
+def tb_dequantize_mx(desc, Kq: Optional[MxRows], Vq: Optional[MxRows], Kimpq: Optional[MxRows], src_row: int, K, V, Kimp, dst_row: int,
+                     rows: int, stream=None) -> None:
+    """The values that rows src_row + i of Kq, Vq and Kimpq stand for to rows dst_row + i of K, V and Kimp (desc), i < rows."""
+    _check(load_library().tb_dequantize_mx(ctypes.byref(desc), _mx(Kq), _mx(Vq), _mx(Kimpq), src_row, _ptr(K), _ptr(V), _ptr(Kimp), dst_row,
+                                           rows, _stream(stream)), "tb_dequantize_mx")
+
+
+def tb_score_mx(desc, q_imp, Kimp: MxRows, scale: float, scores, stream=None) -> None:
+    assert q_imp.is_contiguous() and scores.stride(-1) == 1
+    _check(load_library().tb_score_mx(ctypes.byref(desc), _ptr(q_imp), Kimp.ref, scale, _ptr(scores), scores.stride(-2), _stream(stream)),
+           "tb_score_mx")
+
+
+def tb_sparse_decode_attn_mx(desc, q, K: MxRows, V: MxRows, idx, count, max_count: int, sm_scale: float, out, lse, ws, tail_begin: int = 0,
+                             tail_end: int = 0, stream=None) -> None:
+    """idx and count may be None with max_count = 0: the dense range alone."""
+    assert q.is_contiguous() and out.is_contiguous()
+    _check(load_library().tb_sparse_decode_attn_mx(ctypes.byref(desc), _ptr(q), K.ref, V.ref, _ptr(idx), _ptr(count),
+                                                   0 if idx is None else idx.stride(-2), max_count, tail_begin, tail_end, sm_scale, _ptr(out),
+                                                   _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)),
+           "tb_sparse_decode_attn_mx")
+
+
+def tb_sparse_decode_attn_shared_mx(desc, q, K: MxRows, V: MxRows, idx, count, max_count: int, sm_scale: float, out, lse, ws,
+                                    tail_begin: int = 0, tail_end: int = 0, stream=None) -> None:
+    """idx: int32 [B][idx_cap] (or [B][1][idx_cap]), count: int32 [B]; one list for all heads."""
+    assert q.is_contiguous() and out.is_contiguous()
+    _check(load_library().tb_sparse_decode_attn_shared_mx(ctypes.byref(desc), _ptr(q), K.ref, V.ref, _ptr(idx), _ptr(count),
+                                                          0 if idx is None else idx.stride(-2), max_count, tail_begin, tail_end, sm_scale,
+                                                          _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)),
+           "tb_sparse_decode_attn_shared_mx")
 
 
 def policy_count(N: int, k: int, sink: int, window: int) -> int:

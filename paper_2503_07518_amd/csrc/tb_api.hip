@@ -15,6 +15,7 @@ constexpr int64_t kAttnGroupTargetWgs = 256;
 // through the cache (4 x 8 KV heads, 131072 rows: 2048 workgroups 72.5 us, 4096 69.7, 8192 67.2, one block each 71.9), but
 // every piece costs the second stage some padding.
 constexpr int64_t kScoreFilterWgs = 8192;
+constexpr int kAttnWavesPerWg = 4;
 constexpr int64_t kAttnMinTiles = 2;      // a workgroup is worth its hand-over from two tiles per wave on
 
 // `want` splits or a few less: as many as equal shares of whole granules make
@@ -94,6 +95,11 @@ static bool fit_splits(const tb_cache_desc* d, AttnPlan& p, size_t ws_bytes) {
   while (p.nsplit > p.least && ws_bytes < ws_layout(units, d->D, p.nsplit).total) --p.nsplit;
   if (p.nsplit < planned && p.nsplit > p.multiple) p.nsplit -= p.nsplit % p.multiple;
   return ws_bytes >= ws_layout(units, d->D, p.least).total;
+}
+// Rows in 4 bits: a lane takes a block of a row, a tile is kAttnMxLoads rows per lane group.
+static int attn_mx_tile_rows_per_wg(int D) { return kAttnWavesPerWg * kAttnMxLoads * (64 / (D / 32)); }
+static AttnPlan attn_mx_plan(const tb_cache_desc* d, int64_t max_rows) {
+  return attn_plan(static_cast<int64_t>(d->B) * d->Hq, max_rows, attn_mx_tile_rows_per_wg(d->D), false, false);
 }
 // (the buffered form is planned alike, so that it adds up in the same order)
 static AttnPlan attn_plan(const tb_cache_desc* d, int64_t max_rows, bool shared_list = false) {
@@ -372,6 +378,64 @@ tb_status check_attn_args(const tb_cache_desc* d, const void* q, const void* K, 
   if (d->N * d->k_stride_n * elt >= (int64_t{1} << 32) || d->N * d->v_stride_n * elt >= (int64_t{1} << 32))
     return TB_ERR_UNSUPPORTED;
   return TB_OK;
+}
+
+// Rows in 4 bits, `inner` elements each.
+tb_status check_mx(const tb_mx_rows* r, int inner) {
+  if (!r || !r->codes || !r->scales || r->N < 0) return TB_ERR_INVALID_ARG;
+  if (r->code_stride_b < 0 || r->code_stride_h < 0 || r->code_stride_n < inner / 2) return TB_ERR_INVALID_ARG;
+  if (r->scale_stride_b < 0 || r->scale_stride_h < 0 || r->scale_stride_n < inner / 32) return TB_ERR_INVALID_ARG;
+  if (inner % 32) return TB_ERR_UNSUPPORTED;
+  if (!aligned16(r->codes) || (r->code_stride_b | r->code_stride_h | r->code_stride_n) % 16) return TB_ERR_UNSUPPORTED;
+  return TB_OK;
+}
+
+tb_status mx_copy(const tb_cache_desc* d, void* const (&rows_of)[3], int64_t row, const tb_mx_rows* const (&mx)[3], int64_t mx_row, int64_t rows,
+                  bool back, void* stream) {
+  TB_TRY(check_desc(d));
+  if (row < 0 || mx_row < 0 || rows < 0 || rows > d->N - row) return TB_ERR_INVALID_ARG;
+  bool any = false;
+  const int64_t strides[3][3] = {{d->k_stride_b, d->k_stride_h, d->k_stride_n}, {d->v_stride_b, d->v_stride_h, d->v_stride_n}, {d->ki_stride_b, d->ki_stride_h, d->ki_stride_n}};
+  for (int t = 0; t < 3; ++t) {
+    const int inner = t == 2 ? d->Dimp : d->D;
+    if (!rows_of[t] != !mx[t]) return TB_ERR_INVALID_ARG;
+    if (!rows_of[t]) continue;
+    any = true;
+    TB_TRY(check_mx(mx[t], inner));
+    if (rows > mx[t]->N - mx_row) return TB_ERR_INVALID_ARG;
+    TB_TRY(check_strides(d, strides[t][0], strides[t][1], strides[t][2], inner));
+    if (!aligned16(rows_of[t])) return TB_ERR_UNSUPPORTED;
+  }
+  if (!any) return TB_ERR_INVALID_ARG;
+  if (rows > (int64_t{1} << 20)) return TB_ERR_UNSUPPORTED;
+  const MxCopyLaunch L{d, {rows_of[0], rows_of[1], rows_of[2]}, row, {mx[0], mx[1], mx[2]}, mx_row, rows, back};
+  return launch_mx_copy(L, static_cast<hipStream_t>(stream));
+}
+
+tb_status sparse_attn_mx(const tb_cache_desc* d, const void* q, const tb_mx_rows* K, const tb_mx_rows* V, const int32_t* idx, const int32_t* count,
+                         int64_t idx_cap, int64_t max_count, int64_t tail_begin, int64_t tail_end, float sm_scale, float* out, float* lse,
+                         void* ws, size_t ws_bytes, void* stream, bool shared_list) {
+  TB_TRY(check_desc(d));
+  if (!q || !out || idx_cap < 0 || max_count < 0 || (max_count > 0 && (!idx || !count || max_count > idx_cap))) return TB_ERR_INVALID_ARG;
+  if (tail_begin < 0 || tail_begin > tail_end || tail_end > d->N) return TB_ERR_INVALID_ARG;
+  if (d->N == 0 && max_count > 0) return TB_ERR_INVALID_ARG;
+  for (const tb_mx_rows* r : {K, V}) {
+    TB_TRY(check_mx(r, d->D));
+    if (r->N < d->N) return TB_ERR_INVALID_ARG;
+    // rows are addressed with 32-bit byte offsets inside one (b, kv-head) slab
+    if (r->code_stride_n >= (int64_t{1} << 32) || r->scale_stride_n >= (int64_t{1} << 32) || d->N > (int64_t{1} << 30)) return TB_ERR_UNSUPPORTED;
+    if (d->N * r->code_stride_n >= (int64_t{1} << 32) || d->N * r->scale_stride_n >= (int64_t{1} << 32)) return TB_ERR_UNSUPPORTED;
+  }
+  if (!aligned16(q)) return TB_ERR_UNSUPPORTED;
+  if (max_count + (tail_end - tail_begin) > (int64_t{1} << 30)) return TB_ERR_UNSUPPORTED;
+  const int64_t units = static_cast<int64_t>(d->B) * d->Hq;
+  if (units == 0) return TB_OK;
+  AttnPlan plan = attn_mx_plan(d, max_count + (tail_end - tail_begin));
+  if (!ws || !aligned16(ws) || !fit_splits(d, plan, ws_bytes)) return TB_ERR_WORKSPACE;
+  const WsLayout w = ws_layout(units, d->D, plan.nsplit);
+  const AttnMxLaunch L{d, q, K, V, idx, count, idx_cap, max_count, tail_begin, tail_end, sm_scale, out, lse,
+                       reinterpret_cast<float*>(static_cast<char*>(ws) + w.part_off), reinterpret_cast<uint32_t*>(ws), plan, shared_list};
+  return launch_attn_mx(L, static_cast<hipStream_t>(stream));
 }
 
 }  // namespace
@@ -707,9 +771,43 @@ tb_status tb_decode_step(const tb_cache_desc* d, const void* q_imp, const void* 
   return launch_attn(A, st);
 }
 
+tb_status tb_quantize_mx(const tb_cache_desc* d, const void* K, const void* V, const void* Kimp, int64_t src_row, const tb_mx_rows* Kq,
+                         const tb_mx_rows* Vq, const tb_mx_rows* Kimpq, int64_t dst_row, int64_t rows, void* stream) {
+  return mx_copy(d, {const_cast<void*>(K), const_cast<void*>(V), const_cast<void*>(Kimp)}, src_row, {Kq, Vq, Kimpq}, dst_row, rows, false, stream);
+}
+
+tb_status tb_dequantize_mx(const tb_cache_desc* d, const tb_mx_rows* Kq, const tb_mx_rows* Vq, const tb_mx_rows* Kimpq, int64_t src_row,
+                           void* K, void* V, void* Kimp, int64_t dst_row, int64_t rows, void* stream) {
+  return mx_copy(d, {K, V, Kimp}, dst_row, {Kq, Vq, Kimpq}, src_row, rows, true, stream);
+}
+
+tb_status tb_score_mx(const tb_cache_desc* d, const void* q_imp, const tb_mx_rows* Kimp, float scale, float* scores, int64_t score_stride,
+                      void* stream) {
+  TB_TRY(check_desc(d));
+  if (!q_imp || !scores || score_stride < d->N) return TB_ERR_INVALID_ARG;
+  TB_TRY(check_mx(Kimp, d->Dimp));
+  if (Kimp->N < d->N) return TB_ERR_INVALID_ARG;
+  if (score_stride % 4 || !aligned16(q_imp) || !aligned16(scores)) return TB_ERR_UNSUPPORTED;
+  const ScoreMxLaunch L{d, q_imp, Kimp, scale, scores, score_stride};
+  return launch_score_mx(L, static_cast<hipStream_t>(stream));
+}
+
+tb_status tb_sparse_decode_attn_mx(const tb_cache_desc* d, const void* q, const tb_mx_rows* K, const tb_mx_rows* V, const int32_t* idx,
+                                   const int32_t* count, int64_t idx_cap, int64_t max_count, int64_t tail_begin, int64_t tail_end,
+                                   float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  return sparse_attn_mx(d, q, K, V, idx, count, idx_cap, max_count, tail_begin, tail_end, sm_scale, out, lse, ws, ws_bytes, stream, false);
+}
+
+tb_status tb_sparse_decode_attn_shared_mx(const tb_cache_desc* d, const void* q, const tb_mx_rows* K, const tb_mx_rows* V,
+                                          const int32_t* idx, const int32_t* count, int64_t idx_cap, int64_t max_count, int64_t tail_begin,
+                                          int64_t tail_end, float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  return sparse_attn_mx(d, q, K, V, idx, count, idx_cap, max_count, tail_begin, tail_end, sm_scale, out, lse, ws, ws_bytes, stream, true);
+}
+
 size_t tb_workspace_bytes(int32_t op, const tb_cache_desc* d, int64_t max_count) {
   if (check_desc(d) != TB_OK || max_count < 0) return 0;
   const int64_t units = static_cast<int64_t>(d->B) * d->Hq;
+  if (op == TB_OP_ATTN_MX) return ws_layout(units, d->D, attn_mx_plan(d, max_count).max_split).total;
   // two-stage selection of long rows (none for most shapes): max_count bounds the budget
   const size_t sel = select_scratch_upto(units, d->N, max_count);
   const size_t sel_total = sel ? ws_layout(units, d->D, 1).part_off + align_up(sel, 256) : 0;

@@ -120,6 +120,13 @@ __device__ __forceinline__ void merge_waves(const float (*s_m)[1], const float (
   }
 }
 
+// Whether a sum of weights has anything to be divided by: none of an empty list.  NAN_STAYS: a sum that is NaN has, its row becomes NaN
+// (the caches in 4 bits have no infinities, only rows that stand for NaN; without, such a row counts as empty).
+template <bool NAN_STAYS>
+__device__ __forceinline__ bool has_weight(const float l) {
+  return NAN_STAYS ? !(l <= 0.f) : l > 0.f;
+}
+
 // Adds up the splits of GH heads and writes their outputs: the work of the last workgroup to arrive, whose time is
 // added to the whole launch.  A quad of outputs per thread (pair(at): (max, sum) of head and split number
 // at, quad(at, d): its accumulators from element d), the splits dealt round the J thread groups that cover the
@@ -127,7 +134,7 @@ __device__ __forceinline__ void merge_waves(const float (*s_m)[1], const float (
 // a memory round trip per split, and such a load is paid per instruction even when its result is not needed,
 // so the chunk is sized to the split count.  The order of combination is fixed.  (Threads past the NW waves repeat
 // their work.)
-template <int D, int GH, int NW, typename Pair, typename Quad>
+template <int D, int GH, int NW, bool NAN_STAYS = false, typename Pair, typename Quad>
 __device__ __forceinline__ void combine_splits(const int nsplit, float* out, float* lse, float (&s_m)[NW][GH], float (&s_l)[NW][GH],
                                                float (&s_acc)[NW][GH][D], Pair&& pair, Quad&& quad_of) {
   constexpr int kThreads = NW * kWave;
@@ -214,8 +221,8 @@ __device__ __forceinline__ void combine_splits(const int nsplit, float* out, flo
           ot += s_acc[r][eh][ed] * wgt;
         }
       }
-      out[e] = (Lt > 0.f) ? ot / Lt : 0.f;
-      if (ed == 0 && lse) lse[eh] = (Lt > 0.f) ? Mt * kLn2 + logf(Lt) : -INFINITY;
+      out[e] = has_weight<NAN_STAYS>(Lt) ? ot / Lt : 0.f;
+      if (ed == 0 && lse) lse[eh] = has_weight<NAN_STAYS>(Lt) ? Mt * kLn2 + logf(Lt) : -INFINITY;
     }
   }
 }

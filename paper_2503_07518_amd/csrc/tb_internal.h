@@ -198,6 +198,46 @@ constexpr int kAttnGroupWaves = 8;    // waves of a workgroup that serves a KV g
 constexpr int kAttnLoadsPerTile = 4;  // K (and V) gathers of a lane per tile
 tb_status launch_attn(const AttnLaunch& a, hipStream_t st);
 
+// Rows of K, V and K_imp into a cache in microscaled 4-bit floating point, or back (`back`): those of the three arrays that are there.
+struct MxCopyLaunch {
+  const tb_cache_desc* desc;
+  void* rows_of[3];  // K, V, K_imp (NULL: not taken part in)
+  int64_t row;       // the first row of each
+  const tb_mx_rows* mx[3];
+  int64_t mx_row, rows;
+  bool back;
+};
+tb_status launch_mx_copy(const MxCopyLaunch& a, hipStream_t st);
+
+struct ScoreMxLaunch {
+  const tb_cache_desc* desc;
+  const void* q_imp;
+  const tb_mx_rows* Kimp;
+  float scale;
+  float* scores;
+  int64_t score_stride;
+};
+tb_status launch_score_mx(const ScoreMxLaunch& a, hipStream_t st);
+
+struct AttnMxLaunch {
+  const tb_cache_desc* desc;
+  const void* q;
+  const tb_mx_rows* K;
+  const tb_mx_rows* V;
+  const int32_t* idx;
+  const int32_t* count;
+  int64_t idx_cap, max_count, tail_begin, tail_end;
+  float sm_scale;
+  float* out;
+  float* lse;
+  float* partials;
+  uint32_t* counters;
+  AttnPlan plan;
+  bool shared_list;
+};
+constexpr int kAttnMxLoads = 2;  // K (and V) gathers of a lane per tile
+tb_status launch_attn_mx(const AttnMxLaunch& a, hipStream_t st);
+
 // Query predictor of a producer layer (LN + two-layer MLP), see tb_predict.hip.
 struct PredictLaunch {
   int dtype;

@@ -1,0 +1,115 @@
+"""Host-side checks of the 4-bit cache's entry points: what they refuse, before anything is launched."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2503_07518_amd import binding as tb
+
+P = ctypes.c_void_p(0x10000)  # never dereferenced: every call below fails validation first
+ODD = ctypes.c_void_p(0x10008)
+INV, UNS, WS = tb.TB_ERR_INVALID_ARG, tb.TB_ERR_UNSUPPORTED, tb.TB_ERR_WORKSPACE
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    return tb.load_library()
+
+
+def desc(**kw):
+    d = tb.tb_cache_desc(2, 8, 2, 128, 32, tb.TB_BF16, 1000, 2 * 1024 * 128, 1024 * 128, 128, 2 * 1024 * 128, 1024 * 128, 128,
+                         2 * 1024 * 32, 1024 * 32, 32)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+def rows(inner=128, **kw):
+    r = tb.tb_mx_rows(0x10000, 0x20001, 1024, 2 * 1024 * inner // 2, 1024 * inner // 2, inner // 2, 2 * 1024 * inner // 32, 1024 * inner // 32,
+                      inner // 32)
+    for k, v in kw.items():
+        setattr(r, k, v)
+    return r
+
+
+def ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def quantize(lib, d=None, K=P, V=P, Ki=P, src=0, Kq=0, Vq=0, Kiq=0, dst=0, n=8, back=False):
+    Kq, Vq, Kiq = (rows(i) if r == 0 else r for r, i in ((Kq, 128), (Vq, 128), (Kiq, 32)))
+    d = d or desc()
+    if back:
+        return lib.tb_dequantize_mx(ref(d), ref(Kq), ref(Vq), ref(Kiq), dst, K, V, Ki, src, n, None)
+    return lib.tb_quantize_mx(ref(d), K, V, Ki, src, ref(Kq), ref(Vq), ref(Kiq), dst, n, None)
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("want,kw", [
+    (INV, dict(K=None)), (INV, dict(Kq=None)), (INV, dict(K=None, V=None, Ki=None, Kq=None, Vq=None, Kiq=None)),
+    (INV, dict(n=-1)), (INV, dict(src=-1)), (INV, dict(dst=-1)), (INV, dict(src=993)), (INV, dict(dst=1017)), (INV, dict(n=1 << 62, src=5)),
+    (INV, dict(Kq=rows(codes=None))), (INV, dict(Vq=rows(scales=None))), (INV, dict(Kq=rows(N=-1))),
+    (INV, dict(Kq=rows(code_stride_n=48))), (INV, dict(Vq=rows(scale_stride_n=3))), (INV, dict(Vq=rows(code_stride_b=-16))),
+    (INV, dict(d=desc(k_stride_n=64))), (INV, dict(d=desc(dtype=7))), (INV, dict(d=desc(Hq=7))),
+    (UNS, dict(Kq=rows(codes=0x10008))), (UNS, dict(Kq=rows(code_stride_n=72))), (UNS, dict(Vq=rows(code_stride_h=1024 * 64 + 8))),
+    (UNS, dict(K=ODD)), (UNS, dict(Ki=ODD)), (UNS, dict(d=desc(k_stride_n=129))), (UNS, dict(d=desc(D=96))),
+    (UNS, dict(d=desc(Dimp=16, ki_stride_n=16), Kiq=rows(16, scale_stride_n=1, code_stride_n=16))),
+    (UNS, dict(d=desc(N=1 << 22), Kq=rows(N=1 << 22), Vq=rows(N=1 << 22), Kiq=rows(32, N=1 << 22), n=(1 << 20) + 1)),
+])
+def test_conversion_refusals(lib, want, kw, back):
+    assert quantize(lib, back=back, **kw) == want
+
+
+def test_no_rows_is_no_work(lib):
+    assert quantize(lib, n=0) == tb.TB_OK and quantize(lib, d=desc(B=0)) == tb.TB_OK
+    assert quantize(lib, n=0, back=True) == tb.TB_OK
+
+
+@pytest.mark.parametrize("want,kw", [
+    (INV, dict(q=None)), (INV, dict(scores=None)), (INV, dict(k=None)), (INV, dict(stride=999)), (INV, dict(k=rows(32, N=999))),
+    (INV, dict(k=rows(32, code_stride_n=8))), (UNS, dict(stride=1002)), (UNS, dict(q=ODD)), (UNS, dict(scores=ODD)),
+    (UNS, dict(d=desc(Dimp=16), k=rows(16, scale_stride_n=1, code_stride_n=16))), (UNS, dict(k=rows(32, codes=0x10004))), (UNS, dict(d=desc(Hq=6))),
+])
+def test_score_refusals(lib, want, kw):
+    a = dict(d=desc(), q=P, k=rows(32), scores=P, stride=1000)
+    a.update(kw)
+    assert lib.tb_score_mx(ref(a["d"]), a["q"], ref(a["k"]), 1.0, a["scores"], a["stride"], None) == want
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("want,kw", [
+    (INV, dict(q=None)), (INV, dict(K=None)), (INV, dict(V=None)), (INV, dict(out=None)), (INV, dict(idx=None)), (INV, dict(count=None)),
+    (INV, dict(max_count=101)), (INV, dict(max_count=-1)), (INV, dict(cap=-1, max_count=0)), (INV, dict(tail=(-1, 4))), (INV, dict(tail=(5, 4))),
+    (INV, dict(tail=(0, 1001))), (INV, dict(K=rows(N=999))), (INV, dict(V=rows(N=999))), (INV, dict(d=desc(N=0))), (INV, dict(V=rows(scale_stride_n=1))),
+    (UNS, dict(q=ODD)), (UNS, dict(V=rows(codes=0x10008))), (UNS, dict(d=desc(D=256))), (UNS, dict(d=desc(Hq=6))),
+    (UNS, dict(d=desc(N=1 << 20), K=rows(N=1 << 20, code_stride_n=4096), V=rows(N=1 << 20))),
+    (UNS, dict(d=desc(N=1 << 20), K=rows(N=1 << 20), V=rows(N=1 << 20, scale_stride_n=4096))),
+    (UNS, dict(K=rows(code_stride_n=1 << 62))), (UNS, dict(d=desc(N=1 << 31), K=rows(N=1 << 31), V=rows(N=1 << 31))),
+    (WS, dict(ws=None)), (WS, dict(ws=ODD)), (WS, dict(ws_bytes=16)),
+])
+def test_attention_refusals(lib, want, kw, shared):
+    a = dict(d=desc(), q=P, K=rows(), V=rows(), idx=P, count=P, cap=100, max_count=100, tail=(0, 0), out=P, ws=P, ws_bytes=1 << 30)
+    a.update(kw)
+    call = lib.tb_sparse_decode_attn_shared_mx if shared else lib.tb_sparse_decode_attn_mx
+    assert call(ref(a["d"]), a["q"], ref(a["K"]), ref(a["V"]), a["idx"], a["count"], a["cap"], a["max_count"], *a["tail"], 1.0, a["out"], None,
+                a["ws"], a["ws_bytes"], None) == want
+
+
+def test_workspace(lib):
+    d = desc()
+    most = 0
+    for n in range(0, 20000, 97):  # one made for long lists serves all shorter ones
+        need = tb.tb_workspace_bytes(tb.TB_OP_ATTN_MX, d, n)
+        assert need >= 16 * 256 and need >= most
+        most = need
+    assert tb.tb_workspace_bytes(tb.TB_OP_ATTN_MX, desc(D=96), 10) == 0 and tb.tb_workspace_bytes(tb.TB_OP_ATTN_MX, d, -1) == 0
+
+
+def test_rows_of_the_binding():
+    cache = tb.MxCache(2, 3, 50, 128, 64, device="cpu")
+    assert cache.K.inner == cache.V.inner == 128 and cache.Kimp.inner == 64
+    assert cache.V.desc.codes - cache.K.desc.codes == 64 and cache.K.desc.code_stride_n == 128 and cache.K.desc.scale_stride_n == 8
+    d = tb.make_mx_desc(40, 12, torch.float32, K=cache.K, Kimp=cache.Kimp)
+    assert (d.B, d.Hq, d.Hkv, d.D, d.Dimp, d.dtype, d.N) == (2, 12, 3, 128, 64, tb.TB_F32, 40)
+    with pytest.raises(AssertionError):
+        tb.MxRows(torch.zeros((1, 1, 4, 64), dtype=torch.uint8), torch.zeros((1, 1, 4, 3), dtype=torch.uint8))
