@@ -283,6 +283,8 @@ tb_status tb_sparse_decode_attn_mx(const tb_cache_desc* desc, const void* q, con
                                    const int32_t* count, int64_t idx_cap, int64_t max_count, int64_t tail_begin, int64_t tail_end,
                                    float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/* (limits of the two: N <= 2^24, strides between rows below 2^24, a head's rows below 4 GiB.) */
+
 /* The head-less form: one list per batch element for all of its heads, as tb_sparse_decode_attn_shared. */
 tb_status tb_sparse_decode_attn_shared_mx(const tb_cache_desc* desc, const void* q, const tb_mx_rows* K, const tb_mx_rows* V,
                                           const int32_t* idx, const int32_t* count, int64_t idx_cap, int64_t max_count, int64_t tail_begin,

@@ -101,6 +101,19 @@ static int attn_mx_tile_rows_per_wg(int D) { return kAttnWavesPerWg * kAttnMxLoa
 static AttnPlan attn_mx_plan(const tb_cache_desc* d, int64_t max_rows) {
   return attn_plan(static_cast<int64_t>(d->B) * d->Hq, max_rows, attn_mx_tile_rows_per_wg(d->D), false, false);
 }
+// One list (or none) for all heads of a KV group: eight waves of 32 rows a step, up to one workgroup per compute unit; more groups than
+// compute units take several rounds.
+static bool attn_mx_grouped(const tb_cache_desc* d) { return d->Hq > d->Hkv; }
+static AttnPlan attn_mx_group_plan(const tb_cache_desc* d, int64_t max_rows) {
+  const int64_t groups = static_cast<int64_t>(d->B) * d->Hkv;
+  if (max_rows <= 0 || groups <= 0) return AttnPlan{1, 1, 1, 1};
+  const int64_t step = 32 * kAttnGroupWaves, most = std::max<int64_t>(1, max_rows / step);
+  const int64_t want = std::max<int64_t>(1, kAttnGroupTargetWgs / groups);
+  AttnPlan p = split_plan(max_rows, std::min(want, most), step);
+  p.max_split = static_cast<int>(std::min(want, most));
+  p.least = p.nsplit;
+  return p;
+}
 // (the buffered form is planned alike, so that it adds up in the same order)
 static AttnPlan attn_plan(const tb_cache_desc* d, int64_t max_rows, bool shared_list = false) {
   const bool shares = attn_in_shares(d);
@@ -422,19 +435,21 @@ tb_status sparse_attn_mx(const tb_cache_desc* d, const void* q, const tb_mx_rows
   for (const tb_mx_rows* r : {K, V}) {
     TB_TRY(check_mx(r, d->D));
     if (r->N < d->N) return TB_ERR_INVALID_ARG;
-    // rows are addressed with 32-bit byte offsets inside one (b, kv-head) slab
-    if (r->code_stride_n >= (int64_t{1} << 32) || r->scale_stride_n >= (int64_t{1} << 32) || d->N > (int64_t{1} << 30)) return TB_ERR_UNSUPPORTED;
+    // rows are addressed with 32-bit byte offsets inside one (b, kv-head) slab, products of 24-bit numbers
+    if (r->code_stride_n >= (1 << 24) || r->scale_stride_n >= (1 << 24) || d->N > (1 << 24)) return TB_ERR_UNSUPPORTED;
     if (d->N * r->code_stride_n >= (int64_t{1} << 32) || d->N * r->scale_stride_n >= (int64_t{1} << 32)) return TB_ERR_UNSUPPORTED;
   }
   if (!aligned16(q)) return TB_ERR_UNSUPPORTED;
   if (max_count + (tail_end - tail_begin) > (int64_t{1} << 30)) return TB_ERR_UNSUPPORTED;
   const int64_t units = static_cast<int64_t>(d->B) * d->Hq;
   if (units == 0) return TB_OK;
-  AttnPlan plan = attn_mx_plan(d, max_count + (tail_end - tail_begin));
+  const int64_t rows = max_count + (tail_end - tail_begin);
+  const bool grouped = (shared_list || max_count == 0) && attn_mx_grouped(d);
+  AttnPlan plan = grouped ? attn_mx_group_plan(d, rows) : attn_mx_plan(d, rows);
   if (!ws || !aligned16(ws) || !fit_splits(d, plan, ws_bytes)) return TB_ERR_WORKSPACE;
   const WsLayout w = ws_layout(units, d->D, plan.nsplit);
   const AttnMxLaunch L{d, q, K, V, idx, count, idx_cap, max_count, tail_begin, tail_end, sm_scale, out, lse,
-                       reinterpret_cast<float*>(static_cast<char*>(ws) + w.part_off), reinterpret_cast<uint32_t*>(ws), plan, shared_list};
+                       reinterpret_cast<float*>(static_cast<char*>(ws) + w.part_off), reinterpret_cast<uint32_t*>(ws), plan, shared_list, grouped};
   return launch_attn_mx(L, static_cast<hipStream_t>(stream));
 }
 
@@ -807,7 +822,11 @@ tb_status tb_sparse_decode_attn_shared_mx(const tb_cache_desc* d, const void* q,
 size_t tb_workspace_bytes(int32_t op, const tb_cache_desc* d, int64_t max_count) {
   if (check_desc(d) != TB_OK || max_count < 0) return 0;
   const int64_t units = static_cast<int64_t>(d->B) * d->Hq;
-  if (op == TB_OP_ATTN_MX) return ws_layout(units, d->D, attn_mx_plan(d, max_count).max_split).total;
+  if (op == TB_OP_ATTN_MX) {
+    int most = attn_mx_plan(d, max_count).max_split;
+    if (attn_mx_grouped(d)) most = std::max(most, attn_mx_group_plan(d, max_count).max_split);
+    return ws_layout(units, d->D, most).total;
+  }
   // two-stage selection of long rows (none for most shapes): max_count bounds the budget
   const size_t sel = select_scratch_upto(units, d->N, max_count);
   const size_t sel_total = sel ? ws_layout(units, d->D, 1).part_off + align_up(sel, 256) : 0;

@@ -33,7 +33,23 @@ struct AttnMxArgs {
   int32_t shared_list;
 };
 
+constexpr int kGroupMxWaves = kAttnGroupWaves;
 constexpr int kMxLoads = kAttnMxLoads;  // rows per lane group and tile
+
+// Byte offset of a row below 2^24 times a stride below 2^24, up to 32 bits.  (__umul24 is declared to return a signed number.)
+__device__ __forceinline__ uint32_t row_offset(const uint32_t row, const uint32_t stride) { return static_cast<uint32_t>(__umul24(row, stride)); }
+
+// One array of a head's rows as a buffer: addresses are 32-bit offsets into it, and what would lie past its last row is not read.
+typedef __amdgpu_buffer_rsrc_t MxBuffer;
+__device__ __forceinline__ MxBuffer mx_buffer(const uint8_t* p, const uint32_t stride, const int64_t rows, const int row_bytes) {
+  const int64_t bytes = rows > 0 ? (rows - 1) * stride + row_bytes : 0;  // below 2^32
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, static_cast<int>(static_cast<uint32_t>(bytes)), 0x00027000);
+}
+__device__ __forceinline__ uint4 mx_load_block(const MxBuffer b, const uint32_t at) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(b, static_cast<int>(at), 0, 0);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
 
 // A lane group's dot product with a block of K, the lane's part of it.
 template <typename T>
@@ -96,29 +112,44 @@ struct MxQuery<float> {
   }
 };
 
+// What lane (number xor STEP) of a row of 16 lanes holds, by moves inside the vector unit.
 template <int STEP>
 __device__ __forceinline__ float from_lane_xor(const float x) {
-  return __shfl_xor(x, STEP, kWave);
+  auto dpp = [](float v, auto ctrl) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xF, 0xF, false)); };
+  if constexpr (STEP == 8) return dpp(x, std::integral_constant<int, 0x128>{});  // rotated by eight
+  if constexpr (STEP == 4) return dpp(dpp(x, std::integral_constant<int, 0x141>{}), std::integral_constant<int, 0x1B>{});  // both mirrors: of eight, of four
+  return dpp(x, std::integral_constant<int, 0x4E>{});
 }
 
-// Sums acc over the lanes that differ in bits STEP .. 32 of their number; each lane is left with N / (64 / STEP) of the sums: at every step
-// it gives half of what it has to its partner and takes the partner's part of the other half.  `base`: the first of its elements.
+// Sums acc over the lanes that differ in bits LAST .. 32 of their number, each lane being left with some of the sums: at every step it
+// gives half of what it has to its partner and takes the partner's part of the other half (for the upper two bits the swap
+// instructions do that to two registers at once).  `base`: the first of its elements.  30 moves instead of 32 a bit.
 template <int N, int STEP, int LAST>
 __device__ __forceinline__ void scatter_sum(float (&acc)[kMxBlock], const int lane, int& base) {
   if constexpr (STEP >= LAST) {
     const bool upper = (lane & STEP) != 0;
 #pragma unroll
     for (int e = 0; e < N / 2; ++e) {
-      const float keep = upper ? acc[e + N / 2] : acc[e], give = upper ? acc[e] : acc[e + N / 2];
-      acc[e] = keep + from_lane_xor<STEP>(give);
+      if constexpr (STEP >= 16) {
+        const uint32_t lo = __float_as_uint(acc[e]), hi = __float_as_uint(acc[e + N / 2]);
+        const auto v = STEP == 32 ? __builtin_amdgcn_permlane32_swap(lo, hi, false, false) : __builtin_amdgcn_permlane16_swap(lo, hi, false, false);
+        acc[e] = __uint_as_float(v[0]) + __uint_as_float(v[1]);
+      } else {
+        const float keep = upper ? acc[e + N / 2] : acc[e], give = upper ? acc[e] : acc[e + N / 2];
+        acc[e] = keep + from_lane_xor<STEP>(give);
+      }
     }
     base += upper ? N / 2 : 0;
     scatter_sum<N / 2, STEP / 2, LAST>(acc, lane, base);
   }
 }
 
+// fp32 queries take twice the registers
+template <typename T>
+constexpr int kMxWavesPerSimd = std::is_same<T, float>::value ? 3 : 4;
+
 template <typename T, int D>
-__global__ __launch_bounds__(kAttnThreads, 4) void attn_mx_kernel(AttnMxArgs a) {
+__global__ __launch_bounds__(kAttnThreads, kMxWavesPerSimd<T>) void attn_mx_kernel(AttnMxArgs a) {
   constexpr int LPR = D / kMxBlock;            // lanes per row
   constexpr int GPW = kWave / LPR;             // rows per wave instruction
   constexpr int TILE = kMxLoads * GPW;         // rows per wave and tile
@@ -148,68 +179,112 @@ __global__ __launch_bounds__(kAttnThreads, 4) void attn_mx_kernel(AttnMxArgs a) 
     hkv = h / a.g;
   }
   const int64_t u = static_cast<int64_t>(b) * a.Hq + h;
-  const uint8_t* kc = a.codes[0] + b * a.code_b[0] + hkv * a.code_h[0] + sub * kMxCodeBytes;
-  const uint8_t* vc = a.codes[1] + b * a.code_b[1] + hkv * a.code_h[1] + sub * kMxCodeBytes;
-  const uint8_t* ks = a.scales[0] + b * a.scale_b[0] + hkv * a.scale_h[0] + sub;
-  const uint8_t* vs = a.scales[1] + b * a.scale_b[1] + hkv * a.scale_h[1] + sub;
+  MxBuffer codes[2], scales[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    codes[t] = mx_buffer(a.codes[t] + b * a.code_b[t] + hkv * a.code_h[t], a.code_n[t], a.N, D / 2);
+    scales[t] = mx_buffer(a.scales[t] + b * a.scale_b[t] + hkv * a.scale_h[t], a.scale_n[t], a.N, LPR);
+  }
 
   const int64_t lu = a.shared_list ? b : u;  // which list this head reads
   const int32_t* list = a.max_count > 0 ? a.idx + lu * a.idx_cap : nullptr;
-  int64_t cnt = a.max_count > 0 ? a.count[lu] : 0;
-  cnt = cnt < 0 ? 0 : (cnt > a.max_count ? a.max_count : cnt);
-  const int64_t total = cnt + (a.tail_end - a.tail_begin);
+  const int32_t last_slot = static_cast<int32_t>(a.max_count) - 1;
+  const int32_t t_beg = (split * kAttnWaves + wave) * TILE, stride = a.nsplit * kAttnWaves * TILE;  // (slots are below 2^30: launch conditions)
 
+  // A tile's list entries are read ahead of the gathers of the tile before, unconditionally (clamped into the max_count entries that the
+  // call names), and its rows while that tile is computed.
+  struct Entries {
+    int32_t at[kMxLoads];
+  };
+  struct Rows {
+    uint4 k[kMxLoads], v[kMxLoads];
+    uint8_t ks[kMxLoads], vs[kMxLoads];
+  };
+  auto fetch = [&](Entries& e, const int32_t t0) {
+#pragma unroll
+    for (int t = 0; t < kMxLoads; ++t) {
+      const int32_t i = t0 + t * GPW + grp;
+      e.at[t] = a.max_count > 0 ? list[i < last_slot ? i : last_slot] : 0;
+    }
+  };
+  Entries entries;
+  fetch(entries, t_beg);
+  const int32_t counted = a.max_count > 0 ? a.count[lu] : 0;
   MxQuery<T> q;
   q.load(static_cast<const T*>(a.q) + u * D + sub * kMxBlock);
+  __builtin_amdgcn_sched_barrier(0);  // query, count and entries come in one trip to memory
+  const int32_t cnt = __builtin_amdgcn_readfirstlane(max(0, min(counted, last_slot + 1)));
+  const int32_t total = cnt + static_cast<int32_t>(a.tail_end - a.tail_begin);
+  const int32_t first_tail = static_cast<int32_t>(a.tail_begin) - cnt, last_row = static_cast<int32_t>(a.N) - 1;
+  auto gather = [&](Rows& r, const Entries& e, const int32_t t0) {
+#pragma unroll
+    for (int t = 0; t < kMxLoads; ++t) {
+      const int32_t i = t0 + t * GPW + grp;
+      const int32_t n = i < cnt ? e.at[t] : first_tail + i;
+      const uint32_t row = static_cast<uint32_t>(max(0, min(n, last_row)));  // inside the cache whatever the list holds
+      r.k[t] = mx_load_block(codes[0], row_offset(row, a.code_n[0]) + sub * kMxCodeBytes);
+      r.v[t] = mx_load_block(codes[1], row_offset(row, a.code_n[1]) + sub * kMxCodeBytes);
+      r.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(scales[0], static_cast<int>(row_offset(row, a.scale_n[0]) + sub), 0, 0);
+      r.vs[t] = __builtin_amdgcn_raw_buffer_load_b8(scales[1], static_cast<int>(row_offset(row, a.scale_n[1]) + sub), 0, 0);
+    }
+  };
+
   float m = -INFINITY, l = 0.f, acc[kMxBlock];
 #pragma unroll
   for (int e = 0; e < kMxBlock; ++e) acc[e] = 0.f;
-
-  const int64_t stride = static_cast<int64_t>(a.nsplit) * kAttnWaves * TILE;
-  for (int64_t t0 = static_cast<int64_t>(split * kAttnWaves + wave) * TILE; t0 < total; t0 += stride) {
-    uint4 kw[kMxLoads], vw[kMxLoads];
-    uint32_t kb[kMxLoads], vb[kMxLoads];
-    bool valid[kMxLoads];
-#pragma unroll
-    for (int t = 0; t < kMxLoads; ++t) {
-      const int64_t i = t0 + t * GPW + grp;
-      valid[t] = i < total;
-      int64_t n = 0;  // (a slot past the end: the cache's first row, as nothing)
-      if (valid[t]) n = i < cnt ? static_cast<int64_t>(list[i]) : a.tail_begin + (i - cnt);
-      n = n < 0 ? 0 : (n >= a.N ? a.N - 1 : n);  // keep the gather inside the cache whatever the list holds
-      const uint32_t row = static_cast<uint32_t>(n);
-      kw[t] = *reinterpret_cast<const uint4*>(kc + row * a.code_n[0]);
-      vw[t] = *reinterpret_cast<const uint4*>(vc + row * a.code_n[1]);
-      kb[t] = ks[row * a.scale_n[0]];
-      vb[t] = vs[row * a.scale_n[1]];
-    }
+  auto consume = [&](const Rows& r, const int32_t left) {  // left: slots from this tile on
     float sc[kMxLoads], tmax = -INFINITY;
+    uint32_t vs[kMxLoads];
 #pragma unroll
     for (int t = 0; t < kMxLoads; ++t) {
-      const float s = group_allreduce_sum<LPR>(q.dot(kw[t], mx_scale(kb[t]))) * a.sm_scale_log2;
-      sc[t] = valid[t] ? s : -INFINITY;
+      const bool valid = t * GPW + grp < left;
+      const float s = group_allreduce_sum<LPR>(q.dot(r.k[t], mx_scale(r.ks[t]))) * a.sm_scale_log2;
+      sc[t] = valid ? s : -INFINITY;
+      vs[t] = valid ? r.vs[t] : 127u;  // (a slot past the end has weight 0, and a scale under which nothing is NaN)
       tmax = fmaxf(tmax, sc[t]);
     }
     const float m_new = fmaxf(m, tmax);
     const float m_ref = m_new > -INFINITY ? m_new : 0.f;  // nothing seen yet, or nothing but NaN
-    const float alpha = exp2_safe(m - m_ref);
-    l *= alpha;
+    if (__any(m_new > m)) {
+      const float alpha = exp2_safe(m - m_ref);
+      l *= alpha;
 #pragma unroll
-    for (int e = 0; e < kMxBlock; ++e) acc[e] *= alpha;
-    m = m_new;
+      for (int e = 0; e < kMxBlock; ++e) acc[e] *= alpha;
+      m = m_new;
+    }
 #pragma unroll
     for (int t = 0; t < kMxLoads; ++t) {
       const float p = exp2_safe(sc[t] - m_ref);
       l += p;
-      // (a slot past the end has weight 0, and a scale under which nothing is NaN)
-      const float scale = mx_scale(valid[t] ? vb[t] : 127u);
-      const uint32_t w[4] = {vw[t].x, vw[t].y, vw[t].z, vw[t].w};
+      const float scale = mx_scale(vs[t]);
+      const uint32_t w[4] = {r.v[t].x, r.v[t].y, r.v[t].z, r.v[t].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float f[8];
         mx_to_f32(w[i], scale, f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[8 * i + e] = fmaf(p, f[e], acc[8 * i + e]);
+      }
+    }
+  };
+  if (t_beg < total) {
+    Rows rows[2];
+    Entries ahead;
+    fetch(ahead, t_beg + stride);
+    gather(rows[0], entries, t_beg);
+    for (int32_t t0 = t_beg; t0 < total; t0 += 2 * stride) {
+#pragma unroll
+      for (int o = 0; o < 2; ++o) {
+        const int32_t at = t0 + o * stride;
+        if (at >= total) break;
+        if (at + stride < total) {
+          entries = ahead;
+          fetch(ahead, at + 2 * stride);
+          __builtin_amdgcn_sched_barrier(0);
+          gather(rows[1 - o], entries, at + stride);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        consume(rows[o], total - at);
       }
     }
   }
@@ -259,6 +334,273 @@ __global__ __launch_bounds__(kAttnThreads, 4) void attn_mx_kernel(AttnMxArgs a) 
   if (tid == 0) __hip_atomic_store(&a.counters[u * kCounterStrideWords], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// One list for all heads, or the dense range alone: the GH heads of a KV group read the same rows, and a workgroup per (b, kv head,
+// split) takes every row once for all of them, on the matrix cores.  A wave takes 32 rows a step:
+//
+//   scores   (16 rows x D) x (D x columns), v_mfma_f32_16x16x32_bf16: lane (i, kb) = (lane % 16, lane / 16) converts its quarter kb of
+//            row i to bf16, the scale in it; the other operand is the same slice of a query (fp32: three bf16 numbers, so that
+//            products stay exact).  Accumulator v of lane (j, kb) is (row 4 kb + v, column j).
+//   weights  exp2 in fp32, each the exact sum of three bf16 numbers.  A column is a head and one of the three parts: there
+//            are 16 columns, and every head has one per part (two parts, and the third in a product of its own, with eight heads).
+//   output   (columns x 32 rows) x (32 rows x D): lane (j, kb) holds the weights of column j for rows 4 kb + v of both 16-row tiles,
+//            the k slots of this operand in an order of their own that the other one follows: lane (n, kb) has elements EV n .. of the
+//            same rows of V, element e of them is column EV n + e.  The parts are added up when all rows are done.
+//
+// A step's rows are on their way while the one before is computed.
+typedef short mx_s16x8 __attribute__((ext_vector_type(8)));
+typedef float mx_acc4 __attribute__((ext_vector_type(4)));
+
+template <typename T, int D, int GH, bool LIST>
+__global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel(AttnMxArgs a) {
+  constexpr int KW = D / kMxBlock;              // words of a K row per lane
+  constexpr int EV = D / 16;                    // elements of a V row per lane, a word (D = 128) or half of one
+  constexpr int QP = std::is_same<T, float>::value ? 3 : 1;
+  constexpr int PS = GH <= 4 ? 4 : 8;           // columns from a head's part to its next one
+  constexpr int STEP = 32;
+  __shared__ GroupLds<D, GH, kGroupMxWaves> gl;
+  const int lane = lane_id(), wave = wave_id();
+  const int i16 = lane & 15, kb = lane >> 4;
+  const int head = i16 % PS, part = i16 / PS;   // of this lane's column
+  const int split = blockIdx.x, hkv = blockIdx.y, b = blockIdx.z;
+  const int64_t u0 = static_cast<int64_t>(b) * a.Hq + static_cast<int64_t>(hkv) * GH;  // first head of the group
+  MxBuffer codes[2], scales[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    codes[t] = mx_buffer(a.codes[t] + b * a.code_b[t] + hkv * a.code_h[t], a.code_n[t], a.N, D / 2);
+    scales[t] = mx_buffer(a.scales[t] + b * a.scale_b[t] + hkv * a.scale_h[t], a.scale_n[t], a.N, KW);
+  }
+
+  // (a negative scale's sign goes to the query, so that the largest score is the largest dot product)
+  const float scale = fabsf(a.sm_scale_log2);
+  const uint32_t sign = __float_as_uint(a.sm_scale_log2) >> 31 << 15;
+  mx_s16x8 qop[QP][KW];
+#pragma unroll
+  for (int c = 0; c < KW; ++c) {
+    const T* qp = static_cast<const T*>(a.q) + (u0 + (head < GH ? head : 0)) * D + kb * (D / 4) + c * 8;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      uint32_t x[QP];
+      mx_split_bf16(head < GH ? to_float(qp[e]) : 0.f, x);
+#pragma unroll
+      for (int p = 0; p < QP; ++p) qop[p][c][e] = static_cast<short>(x[p] ^ sign);
+    }
+  }
+
+  int64_t cnt = LIST ? __builtin_amdgcn_readfirstlane(a.count[b]) : 0;
+  cnt = cnt < 0 ? 0 : (cnt > a.max_count ? a.max_count : cnt);
+  const int64_t total = cnt + (a.tail_end - a.tail_begin);
+  const int64_t w_beg = static_cast<int64_t>(split * kGroupMxWaves + wave) * STEP;
+  const int64_t stride = static_cast<int64_t>(a.nsplit) * kGroupMxWaves * STEP;
+  const int32_t* list = LIST ? a.idx + b * a.idx_cap : nullptr;
+
+  struct Raw {
+    uint32_t k[2][KW], v[2][4];
+    uint8_t ks[2], vs[2][4];
+  };
+  // a lane's place in a row
+  const uint32_t k_at = kb * (4 * KW), ks_at = kb * KW / 4, v_at = i16 * (EV / 2), vs_at = i16 * EV / kMxBlock;
+  auto load_k = [&](Raw& r, const int t, const uint32_t code_at, const int code_row, const uint32_t scale_at, const int scale_row) {
+    if constexpr (KW == 4) {
+      const auto w = __builtin_amdgcn_raw_buffer_load_b128(codes[0], static_cast<int>(code_at), code_row, 0);
+      __builtin_memcpy(&r.k[t][0], &w, 16);
+    } else {
+      const auto w = __builtin_amdgcn_raw_buffer_load_b64(codes[0], static_cast<int>(code_at), code_row, 0);
+      __builtin_memcpy(&r.k[t][0], &w, 8);
+    }
+    r.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(scales[0], static_cast<int>(scale_at), scale_row, 0);
+  };
+  auto load_v = [&](Raw& r, const int t, const int v, const uint32_t code_at, const int code_row, const uint32_t scale_at, const int scale_row) {
+    if constexpr (EV == 8)
+      r.v[t][v] = __builtin_amdgcn_raw_buffer_load_b32(codes[1], static_cast<int>(code_at), code_row, 0);
+    else
+      r.v[t][v] = __builtin_amdgcn_raw_buffer_load_b16(codes[1], static_cast<int>(code_at), code_row, 0);
+    r.vs[t][v] = __builtin_amdgcn_raw_buffer_load_b8(scales[1], static_cast<int>(scale_at), scale_row, 0);
+  };
+  // Rows of a list: lane r (and r + 32) of a step has its slot r; a slot past the end the last one's row, which is attended to anyway,
+  // with weight 0.
+  auto row_of_lane = [&](const int64_t t0) -> uint32_t {
+    int64_t i = t0 + (lane & 31);
+    i = i < total ? i : total - 1;
+    int64_t n = LIST && i < cnt ? static_cast<int64_t>(list[i]) : a.tail_begin + (i - cnt);
+    n = n < 0 ? 0 : (n >= a.N ? a.N - 1 : n);  // keep the gather inside the cache whatever the list holds
+    return static_cast<uint32_t>(n);
+  };
+  auto load_rows = [&](Raw& r, const uint32_t rows) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint32_t row = static_cast<uint32_t>(__shfl(static_cast<int>(rows), 16 * t + i16, kWave));
+      load_k(r, t, row_offset(row, a.code_n[0]) + k_at, 0, row_offset(row, a.scale_n[0]) + ks_at, 0);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const uint32_t row = static_cast<uint32_t>(__shfl(static_cast<int>(rows), 16 * t + 4 * kb + v, kWave));
+        load_v(r, t, v, row_offset(row, a.code_n[1]) + v_at, 0, row_offset(row, a.scale_n[1]) + vs_at, 0);
+      }
+  };
+  // 32 rows of the range: a lane's place among them does not change, the rest of an address is scalar
+  const uint32_t k_lane = i16 * a.code_n[0] + k_at, ks_lane = i16 * a.scale_n[0] + ks_at;
+  const uint32_t v_lane = 4 * kb * a.code_n[1] + v_at, vs_lane = 4 * kb * a.scale_n[1] + vs_at;
+  auto load_range = [&](Raw& r, const int64_t t0) {
+    const uint32_t n = static_cast<uint32_t>(a.tail_begin + t0);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      load_k(r, t, k_lane, static_cast<int>((n + 16 * t) * a.code_n[0]), ks_lane, static_cast<int>((n + 16 * t) * a.scale_n[0]));
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        load_v(r, t, v, v_lane, static_cast<int>((n + 16 * t + v) * a.code_n[1]), vs_lane, static_cast<int>((n + 16 * t + v) * a.scale_n[1]));
+  };
+
+  float m = -INFINITY, l = 0.f;  // of this lane's head (l: its rows only)
+  mx_acc4 acc[EV];               // accumulator v: column 4 kb + v, element EV i16 + e
+#pragma unroll
+  for (int e = 0; e < EV; ++e) acc[e] = mx_acc4{0.f, 0.f, 0.f, 0.f};
+
+  auto compute = [&](const Raw& r, const int left) {  // left: slots from this step on
+    mx_acc4 s[2];
+    float smax = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = mx_acc4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < KW; ++c) {
+        uint32_t w[4];
+        mx_to_bf16(r.k[t][c], mx_scale(r.ks[t]), w);
+        mx_s16x8 kop;
+        __builtin_memcpy(&kop, &w[0], 16);
+#pragma unroll
+        for (int x = QP - 1; x >= 0; --x) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop, qop[x][c], s[t], 0, 0, 0);
+      }
+    }
+    if (left < STEP) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) s[t][v] = 16 * t + 4 * kb + v < left ? s[t][v] : -INFINITY;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) smax = fmaxf(smax, s[t][v]);
+    smax = fmaxf(smax, __shfl_xor(smax, 16, kWave));
+    smax = fmaxf(smax, __shfl_xor(smax, 32, kWave));
+    const float m_new = fmaxf(m, smax * scale);
+    const float m_ref = m_new > -INFINITY ? m_new : 0.f;  // nothing seen yet, or nothing but NaN
+    if (__any(m_new > m)) {
+      const float alpha = exp2_safe(m - m_ref);
+      l *= alpha;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const float al = __shfl(alpha, 4 * kb + v, kWave);  // (lane j < 16 holds column j)
+#pragma unroll
+        for (int e = 0; e < EV; ++e) acc[e][v] *= al;
+      }
+      m = m_new;
+    }
+    uint32_t w[2][4], low[2][4];  // this column's part of the weights, and their third part (eight heads)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const float x = exp2_safe(fmaf(s[t][v], scale, -m_ref));
+        l += x;
+        const uint32_t first = __float_as_uint(x) & 0xFFFF0000u;
+        const float rest = x - __uint_as_float(first);  // exact
+        const uint32_t second = __float_as_uint(rest) & 0xFFFF0000u;
+        low[t][v] = __float_as_uint(rest - __uint_as_float(second));  // at most 8 bits are left
+        w[t][v] = part == 0 ? first : second;
+        if (PS == 4) w[t][v] = part < 2 ? w[t][v] : (part == 2 ? low[t][v] : 0u);
+        if (PS == 8) low[t][v] = part == 0 ? low[t][v] : 0u;
+      }
+    auto operand = [&](const uint32_t (&x)[2][4]) {
+      const uint32_t packed[4] = {__builtin_amdgcn_perm(x[0][1], x[0][0], 0x07060302u), __builtin_amdgcn_perm(x[0][3], x[0][2], 0x07060302u),
+                                  __builtin_amdgcn_perm(x[1][1], x[1][0], 0x07060302u), __builtin_amdgcn_perm(x[1][3], x[1][2], 0x07060302u)};
+      mx_s16x8 o;
+      __builtin_memcpy(&o, &packed[0], 16);
+      return o;
+    };
+    const mx_s16x8 wop = operand(w), lop = operand(low);
+#pragma unroll
+    for (int e2 = 0; e2 < EV / 2; ++e2) {
+      uint32_t u[2][4];  // elements 2 e2 and 2 e2 + 1 of the eight rows
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float vscale = mx_scale(r.vs[t][v]);
+          u[t][v] = e2 == 0 ? mx_to_bf16<0>(r.v[t][v], vscale) : e2 == 1 ? mx_to_bf16<1>(r.v[t][v], vscale)
+                  : e2 == 2 ? mx_to_bf16<2>(r.v[t][v], vscale) : mx_to_bf16<3>(r.v[t][v], vscale);
+        }
+#pragma unroll
+      for (int o = 0; o < 2; ++o) {
+        const uint32_t sel = o ? 0x07060302u : 0x05040100u;  // one element of two rows side by side
+        const uint32_t x[4] = {__builtin_amdgcn_perm(u[0][1], u[0][0], sel), __builtin_amdgcn_perm(u[0][3], u[0][2], sel),
+                               __builtin_amdgcn_perm(u[1][1], u[1][0], sel), __builtin_amdgcn_perm(u[1][3], u[1][2], sel)};
+        mx_s16x8 vop;
+        __builtin_memcpy(&vop, &x[0], 16);
+        if (PS == 8) acc[2 * e2 + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lop, vop, acc[2 * e2 + o], 0, 0, 0);
+        acc[2 * e2 + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wop, vop, acc[2 * e2 + o], 0, 0, 0);
+      }
+    }
+  };
+  if (w_beg < total) {
+    uint32_t rows = 0;  // of the next step to be loaded
+    auto load = [&](Raw& r, const int64_t t0) {
+      if (!LIST && t0 + STEP <= total) {
+        load_range(r, t0);
+        return;
+      }
+      if (!LIST) rows = row_of_lane(t0);
+      load_rows(r, rows);
+      if (LIST && t0 + stride < total) rows = row_of_lane(t0 + stride);
+    };
+    if (LIST) rows = row_of_lane(w_beg);
+    Raw r[2];
+    load(r[0], w_beg);
+    for (int64_t t0 = w_beg; t0 < total; t0 += 2 * stride) {
+#pragma unroll
+      for (int o = 0; o < 2; ++o) {
+        const int64_t at = t0 + o * stride;
+        if (at >= total) break;
+        if (at + stride < total) load(r[1 - o], at + stride);
+        __builtin_amdgcn_sched_barrier(0);
+        compute(r[o], static_cast<int>(min(total - at, static_cast<int64_t>(STEP))));
+      }
+    }
+  }
+  l += __shfl_xor(l, 16, kWave);
+  l += __shfl_xor(l, 32, kWave);
+  if (l != l) m = fmaxf(m, 0.f);  // rows that stand for NaN, perhaps alone: the merges look at lists with a maximum
+  if (lane < GH) {
+    gl.m[wave][lane] = m;
+    gl.l[wave][lane] = l;
+  }
+  // the parts: four heads have one row of lanes each, eight have two
+#pragma unroll
+  for (int e = 0; e < EV; ++e)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      float x = acc[e][v];
+      if (PS == 4) x += __shfl_xor(x, 16, kWave);
+      x += __shfl_xor(x, 32, kWave);
+      if (kb * 4 < PS && 4 * kb + v < GH) gl.acc[wave][4 * kb + v][EV * i16 + e] = x;
+    }
+  group_finish<D, GH, kGroupMxWaves, true>(a, u0, split, gl);
+}
+
+template <typename T, int D, int GH>
+tb_status launch_group(const AttnMxArgs& a, const AttnMxLaunch& L, hipStream_t st) {
+  const dim3 grid(L.plan.nsplit, L.desc->Hkv, L.desc->B);
+  if (L.max_count > 0)
+    hipLaunchKernelGGL((attn_group_mx_kernel<T, D, GH, true>), grid, dim3(kGroupMxWaves * kWave), 0, st, a);
+  else
+    hipLaunchKernelGGL((attn_group_mx_kernel<T, D, GH, false>), grid, dim3(kGroupMxWaves * kWave), 0, st, a);
+  return hip_status(hipGetLastError());
+}
+
 template <typename T, int D>
 tb_status launch_td(const AttnMxLaunch& L, hipStream_t st) {
   const tb_cache_desc& d = *L.desc;
@@ -270,7 +612,7 @@ tb_status launch_td(const AttnMxLaunch& L, hipStream_t st) {
     a.scales[t] = static_cast<const uint8_t*>(kv[t]->scales);
     a.code_b[t] = kv[t]->code_stride_b;
     a.code_h[t] = kv[t]->code_stride_h;
-    a.code_n[t] = static_cast<uint32_t>(kv[t]->code_stride_n);  // (N times these is below 2^32: launch conditions)
+    a.code_n[t] = static_cast<uint32_t>(kv[t]->code_stride_n);  // (N and these are below 2^24, their products below 2^32: launch conditions)
     a.scale_b[t] = kv[t]->scale_stride_b;
     a.scale_h[t] = kv[t]->scale_stride_h;
     a.scale_n[t] = static_cast<uint32_t>(kv[t]->scale_stride_n);
@@ -294,6 +636,12 @@ tb_status launch_td(const AttnMxLaunch& L, hipStream_t st) {
   a.nsplit = L.plan.nsplit;
   a.n_kv_groups = d.B * d.Hkv;
   a.shared_list = L.shared_list ? 1 : 0;
+  if (L.grouped) {  // the plan was made for one workgroup per KV group
+    if (a.g == 2) return launch_group<T, D, 2>(a, L, st);
+    if (a.g == 4) return launch_group<T, D, 4>(a, L, st);
+    if (a.g == 8) return launch_group<T, D, 8>(a, L, st);
+    return TB_ERR_UNSUPPORTED;
+  }
   const int64_t heads_per_xcd = (static_cast<int64_t>(a.n_kv_groups) + kXcds - 1) / kXcds * a.g;
   a.xcd_map = attn_on_one_xcd(&d) && heads_per_xcd <= 65535 ? 1 : 0;  // (of a grid's third number)
   dim3 grid(a.nsplit, d.Hq, d.B);
