@@ -170,15 +170,20 @@ tb_status launch_copy(const MxCopyLaunch& L, hipStream_t st) {
 }
 
 // ---- scores -------------------------------------------------------------------------------------
-// The g dot products of a projected row are a (rows x d') x (d' x g) contraction on the matrix cores, as for bf16 rows: the 16 or
-// 32 bytes of a row go to the four lanes (i, kb) = (lane % 16, lane / 16) of its column, d' / 4 elements each, which the
-// conversions turn into bf16 with the scale in it (exact); the other operand is the same slice of importance query j = lane % 16
-// (zero for j >= g).  fp32 queries enter as three bf16 numbers that hold all 24 bits, so every product is exact and only the fp32 sum
-// rounds.  Accumulator v of lane (j, kb) is (row 4 kb + v, head j); the scores leave through LDS as 128-bit stores.
-// Bound by the stores (4 g bytes a row against 17 or 34 read) and, at one sequence, by the launch.
+// The g dot products of a projected row are a contraction on the matrix cores, four heads at a time, with the queries as the rows of
+// the first operand and 16 projected rows as the columns of the second.  A lane loads a whole block of its row (64 rows of
+// 16 bytes are 1 KiB of consecutive memory); two swaps of lane halves and two of quarters hand the words round so that lane
+// (i, kb) = (lane % 16, lane / 16) has word kb of rows i, 16 + i, 32 + i, 48 + i, and so the scales; the conversions make them bf16
+// with the scale in it (exact).  fp32 queries enter as three bf16 numbers that hold all 24 bits, so every product is exact and
+// only the fp32 sums round.  The first operand has the four heads four times over, so that accumulator v of lane (i, kb) in the product
+// for rows 16 t .. is head v of row 16 t + i whatever kb: lane L keeps that of its own row, and a score row leaves as 256
+// consecutive bytes.  Bound by the memory, twice as many bytes written (4 g a row) as read with
+// eight heads; at one sequence by the launch.
 typedef short mx_short8 __attribute__((ext_vector_type(8)));
 typedef float mx_f32x4 __attribute__((ext_vector_type(4)));
 constexpr int64_t kScoreNtStoreBytes = 16 << 20;  // score arrays from this size on bypass the caches (as for rows of other types)
+
+constexpr int64_t kScoreManyChunks = 16384;       // chunks of 64 rows from which on a wave takes four
 
 struct ScoreMxArgs {
   const void* q_imp;
@@ -192,78 +197,114 @@ struct ScoreMxArgs {
   int32_t nt_store;
 };
 
-template <typename T, int DIMP, int G>
+// Word w of lane quarter r becomes word r of lane quarter w.
+__device__ __forceinline__ void transpose_quarters(uint32_t (&w)[4]) {
+  auto swap = [](uint32_t& x, uint32_t& y, auto half) {
+    const auto v = decltype(half)::value ? __builtin_amdgcn_permlane32_swap(x, y, false, false) : __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    x = v[0];
+    y = v[1];
+  };
+  swap(w[0], w[2], std::true_type{});
+  swap(w[1], w[3], std::true_type{});
+  swap(w[0], w[1], std::false_type{});
+  swap(w[2], w[3], std::false_type{});
+}
+
+template <typename T, int DIMP, int G, int CHUNKS>
 __global__ __launch_bounds__(kMxThreads) void score_mx_kernel(ScoreMxArgs a) {
-  constexpr int kSlices = DIMP / kMxBlock;           // words of a row per lane, matrix products per 16 rows and part
+  constexpr int kBlocks = DIMP / kMxBlock;
   constexpr int kParts = std::is_same<T, float>::value ? 3 : 1;
-  constexpr int kTiles = 4;                          // of 16 rows per wave
-  constexpr int RPP = kMxThreads / 4, RW = RPP * kTiles;  // rows per pass, rows per workgroup
+  constexpr int kSets = (G + 3) / 4;  // of four heads
   const int lane = lane_id(), wave = wave_id();
   const int i16 = lane & 15, kb = lane >> 4;
   const int hkv = blockIdx.y, b = blockIdx.z;
-  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * RW;
-  const uint8_t* codes = a.codes + b * a.code_b + hkv * a.code_h + kb * (4 * kSlices);
-  const uint8_t* scales = a.scales + b * a.scale_b + hkv * a.scale_h + kb * kSlices / 4;
+  const int64_t row0 = (static_cast<int64_t>(blockIdx.x) * (kMxThreads / kWave) + wave) * (kWave * CHUNKS);
+  const uint8_t* codes = a.codes + b * a.code_b + hkv * a.code_h;
+  const uint8_t* scales = a.scales + b * a.scale_b + hkv * a.scale_h;
 
-  uint32_t word[kTiles][kSlices], byte[kTiles];
+  uint32_t word[CHUNKS][kBlocks][4], byte[CHUNKS][kBlocks];
 #pragma unroll
-  for (int i = 0; i < kTiles; ++i) {
-    int64_t row = row0 + i * RPP + wave * 16 + i16;
+  for (int i = 0; i < CHUNKS; ++i) {
+    int64_t row = row0 + i * kWave + lane;
     row = row < a.N ? row : a.N - 1;  // (the result of a clamped row is not stored)
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(codes + row * a.code_n);
 #pragma unroll
-    for (int c = 0; c < kSlices; ++c) word[i][c] = p[c];
-    byte[i] = scales[row * a.scale_n];
-  }
-  // element e of slice c: d' / 4 kb + 8 c + e
-  mx_short8 qop[kParts][kSlices];
-#pragma unroll
-  for (int c = 0; c < kSlices; ++c) {
-    const T* qp = static_cast<const T*>(a.q_imp) + (static_cast<int64_t>(b) * a.Hq + hkv * G + (i16 < G ? i16 : 0)) * DIMP + kb * (DIMP / 4) + c * 8;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      uint32_t part[kParts];
-      mx_split_bf16(i16 < G ? to_float(qp[e]) : 0.f, part);
-#pragma unroll
-      for (int p = 0; p < kParts; ++p) qop[p][c][e] = static_cast<short>(part[p]);
+    for (int c = 0; c < kBlocks; ++c) {
+      // (streamed once a step: past the caches, which keep the scores for the selection)
+      const uint4 v = load_128<true, uint4>(codes + row * a.code_n + c * kMxCodeBytes);
+      word[i][c][0] = v.x;
+      word[i][c][1] = v.y;
+      word[i][c][2] = v.z;
+      word[i][c][3] = v.w;
+      byte[i][c] = scales[row * a.scale_n + c];
     }
   }
+  // row j of the operand: head j % 4 of a set; element e of lane (j, kb): 32 c + 8 kb + e
+  mx_short8 qop[kSets][kBlocks][kParts];
+#pragma unroll
+  for (int s = 0; s < kSets; ++s)
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) {
+      const int head = 4 * s + (i16 & 3);
+      const T* qp = static_cast<const T*>(a.q_imp) + (static_cast<int64_t>(b) * a.Hq + hkv * G + (head < G ? head : 0)) * DIMP + c * kMxBlock + kb * 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        uint32_t part[kParts];
+        mx_split_bf16(to_float(qp[e]), part);
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) qop[s][c][p][e] = static_cast<short>(part[p]);
+      }
+    }
 
-  __shared__ __attribute__((aligned(16))) float s_out[G][RW];
+  float* out = a.scores + (static_cast<int64_t>(b) * a.Hq + hkv * G) * a.score_stride;
 #pragma unroll
-  for (int i = 0; i < kTiles; ++i) {
-    const float scale = mx_scale(byte[i]);
-    mx_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int64_t row = row0 + i * kWave + lane;
+    mx_f32x4 acc[kSets][4];
 #pragma unroll
-    for (int c = 0; c < kSlices; ++c) {
-      uint32_t u[4];
-      mx_to_bf16(word[i][c], scale, u);
-      mx_short8 kop;
-      __builtin_memcpy(&kop, &u[0], 16);
+    for (int s = 0; s < kSets; ++s)
 #pragma unroll
-      for (int p = kParts - 1; p >= 0; --p) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop, qop[p][c], acc, 0, 0, 0);
+      for (int t = 0; t < 4; ++t) acc[s][t] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) {
+      uint32_t sc[4] = {byte[i][c], byte[i][c], byte[i][c], byte[i][c]};
+      transpose_quarters(word[i][c]);
+      transpose_quarters(sc);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        uint32_t u[4];
+        mx_to_bf16(word[i][c][t], mx_scale(sc[t]), u);
+        mx_short8 kop;
+        __builtin_memcpy(&kop, &u[0], 16);
+#pragma unroll
+        for (int s = 0; s < kSets; ++s)
+#pragma unroll
+          for (int p = kParts - 1; p >= 0; --p) acc[s][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qop[s][c][p], kop, acc[s][t], 0, 0, 0);
+      }
     }
-    if (i16 < G)
-      *reinterpret_cast<float4*>(&s_out[i16 < G ? i16 : 0][i * RPP + wave * 16 + 4 * kb]) =
-          make_float4(acc[0] * a.scale, acc[1] * a.scale, acc[2] * a.scale, acc[3] * a.scale);
-  }
-  __syncthreads();
-  float* sbase = a.scores + (static_cast<int64_t>(b) * a.Hq + hkv * G) * a.score_stride + row0;
-  constexpr int V4 = RW / 4;  // float4 groups per head
-  for (int v = threadIdx.x; v < G * V4; v += kMxThreads) {
-    const int hh = v / V4, r4 = (v % V4) * 4;
-    float* dst = sbase + hh * a.score_stride + r4;
-    if (row0 + r4 + 3 < a.N) {
-      const mx_f32x4 o = *reinterpret_cast<const mx_f32x4*>(&s_out[hh][r4]);
-      if (a.nt_store)
-        __builtin_nontemporal_store(o, reinterpret_cast<mx_f32x4*>(dst));
-      else
-        *reinterpret_cast<mx_f32x4*>(dst) = o;
-    } else {
-      for (int c = 0; c < 4; ++c)
-        if (row0 + r4 + c < a.N) dst[c] = s_out[hh][r4 + c];
+    if (row < a.N) {
+#pragma unroll
+      for (int h = 0; h < G; ++h) {
+        float* dst = out + h * a.score_stride + row;
+        const float lower = kb & 1 ? acc[h / 4][1][h % 4] : acc[h / 4][0][h % 4], upper = kb & 1 ? acc[h / 4][3][h % 4] : acc[h / 4][2][h % 4];
+        const float x = (kb & 2 ? upper : lower) * a.scale;
+        if (a.nt_store)
+          __builtin_nontemporal_store(x, dst);
+        else
+          *dst = x;
+      }
     }
   }
+}
+
+template <typename T, int DIMP, int G>
+tb_status launch_score_tdg(const ScoreMxArgs& a, const tb_cache_desc& d, hipStream_t st) {
+  const int64_t chunks = (d.N + kWave - 1) / kWave, waves = kMxThreads / kWave;
+  auto grid = [&](int64_t per_wave) { return dim3(static_cast<unsigned>((chunks + waves * per_wave - 1) / (waves * per_wave)), d.Hkv, d.B); };
+  if (chunks * d.Hkv * d.B >= kScoreManyChunks)
+    hipLaunchKernelGGL((score_mx_kernel<T, DIMP, G, 4>), grid(4), dim3(kMxThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((score_mx_kernel<T, DIMP, G, 1>), grid(1), dim3(kMxThreads), 0, st, a);
+  return hip_status(hipGetLastError());
 }
 
 template <typename T, int DIMP>
@@ -274,15 +315,13 @@ tb_status launch_score_td(const ScoreMxLaunch& L, hipStream_t st) {
                 k.code_stride_b, k.code_stride_h, k.code_stride_n, k.scale_stride_b, k.scale_stride_h, k.scale_stride_n,
                 L.scores, d.N, L.score_stride, d.Hq, L.scale,
                 static_cast<int64_t>(d.B) * d.Hq * d.N * 4 >= kScoreNtStoreBytes ? 1 : 0};
-  const dim3 grid(static_cast<unsigned>((d.N + kMxThreads - 1) / kMxThreads), d.Hkv, d.B);
   switch (d.Hq / d.Hkv) {
-    case 1: hipLaunchKernelGGL((score_mx_kernel<T, DIMP, 1>), grid, dim3(kMxThreads), 0, st, a); break;
-    case 2: hipLaunchKernelGGL((score_mx_kernel<T, DIMP, 2>), grid, dim3(kMxThreads), 0, st, a); break;
-    case 4: hipLaunchKernelGGL((score_mx_kernel<T, DIMP, 4>), grid, dim3(kMxThreads), 0, st, a); break;
-    case 8: hipLaunchKernelGGL((score_mx_kernel<T, DIMP, 8>), grid, dim3(kMxThreads), 0, st, a); break;
+    case 1: return launch_score_tdg<T, DIMP, 1>(a, d, st);
+    case 2: return launch_score_tdg<T, DIMP, 2>(a, d, st);
+    case 4: return launch_score_tdg<T, DIMP, 4>(a, d, st);
+    case 8: return launch_score_tdg<T, DIMP, 8>(a, d, st);
     default: return TB_ERR_UNSUPPORTED;
   }
-  return hip_status(hipGetLastError());
 }
 
 }  // namespace
