@@ -15,7 +15,6 @@ constexpr int64_t kAttnGroupTargetWgs = 256;
 // through the cache (4 x 8 KV heads, 131072 rows: 2048 workgroups 72.5 us, 4096 69.7, 8192 67.2, one block each 71.9), but
 // every piece costs the second stage some padding.
 constexpr int64_t kScoreFilterWgs = 8192;
-constexpr int kAttnWavesPerWg = 4;
 constexpr int64_t kAttnMinTiles = 2;      // a workgroup is worth its hand-over from two tiles per wave on
 
 // `want` splits or a few less: as many as equal shares of whole granules make
@@ -97,7 +96,7 @@ static bool fit_splits(const tb_cache_desc* d, AttnPlan& p, size_t ws_bytes) {
   return ws_bytes >= ws_layout(units, d->D, p.least).total;
 }
 // Rows in 4 bits: a lane takes a block of a row, a tile is kAttnMxLoads rows per lane group.
-static int attn_mx_tile_rows_per_wg(int D) { return kAttnWavesPerWg * kAttnMxLoads * (64 / (D / 32)); }
+static int attn_mx_tile_rows_per_wg(int D) { return kAttnMxWaves * kAttnMxLoads * (64 / (D / 32)); }
 static AttnPlan attn_mx_plan(const tb_cache_desc* d, int64_t max_rows) {
   return attn_plan(static_cast<int64_t>(d->B) * d->Hq, max_rows, attn_mx_tile_rows_per_wg(d->D), false, false);
 }

@@ -33,6 +33,9 @@ struct AttnMxArgs {
   int32_t shared_list;
 };
 
+// The reference of a running softmax moves when a score is 2^kMxLazy above it, not with every new maximum: weights up to that are as exact in
+// fp32, and sums are seldom rescaled.
+constexpr float kMxLazy = 8.f;
 constexpr int kGroupMxWaves = kAttnGroupWaves;
 constexpr int kMxLoads = kAttnMxLoads;  // rows per lane group and tile
 
@@ -112,6 +115,27 @@ struct MxQuery<float> {
   }
 };
 
+// x and what the lanes of the other half (HALF = 32) or the neighbouring quarter (16) hold, in some order.
+template <int HALF>
+__device__ __forceinline__ void both_halves(const float x, float& lo, float& hi) {
+  const uint32_t u = __float_as_uint(x);
+  const auto v = HALF == 32 ? __builtin_amdgcn_permlane32_swap(u, u, false, false) : __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  lo = __uint_as_float(v[0]);
+  hi = __uint_as_float(v[1]);
+}
+template <int HALF>
+__device__ __forceinline__ float half_sum(const float x) {
+  float lo, hi;
+  both_halves<HALF>(x, lo, hi);
+  return lo + hi;
+}
+template <int HALF>
+__device__ __forceinline__ float half_max(const float x) {
+  float lo, hi;
+  both_halves<HALF>(x, lo, hi);
+  return fmaxf(lo, hi);
+}
+
 // What lane (number xor STEP) of a row of 16 lanes holds, by moves inside the vector unit.
 template <int STEP>
 __device__ __forceinline__ float from_lane_xor(const float x) {
@@ -148,16 +172,16 @@ __device__ __forceinline__ void scatter_sum(float (&acc)[kMxBlock], const int la
 template <typename T>
 constexpr int kMxWavesPerSimd = std::is_same<T, float>::value ? 3 : 4;
 
-template <typename T, int D>
-__global__ __launch_bounds__(kAttnThreads, kMxWavesPerSimd<T>) void attn_mx_kernel(AttnMxArgs a) {
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(NW * kWave, kMxWavesPerSimd<T>) void attn_mx_kernel(AttnMxArgs a) {
   constexpr int LPR = D / kMxBlock;            // lanes per row
   constexpr int GPW = kWave / LPR;             // rows per wave instruction
   constexpr int TILE = kMxLoads * GPW;         // rows per wave and tile
   constexpr int KEEP = kMxBlock / GPW;         // outputs a lane is left with
   static_assert(KEEP * kWave == D, "every output of a wave has one lane");
 
-  __shared__ float s_m[kAttnWaves][1], s_l[kAttnWaves][1];
-  __shared__ __attribute__((aligned(16))) float s_acc[kAttnWaves][1][D];
+  __shared__ float s_m[NW][1], s_l[NW][1];
+  __shared__ __attribute__((aligned(16))) float s_acc[NW][1][D];
   __shared__ uint32_t s_last;
 
   const int tid = threadIdx.x;
@@ -187,9 +211,10 @@ __global__ __launch_bounds__(kAttnThreads, kMxWavesPerSimd<T>) void attn_mx_kern
   }
 
   const int64_t lu = a.shared_list ? b : u;  // which list this head reads
-  const int32_t* list = a.max_count > 0 ? a.idx + lu * a.idx_cap : nullptr;
+  // (without a list none of its entries is read)
+  const MxBuffer list = mx_buffer(reinterpret_cast<const uint8_t*>(a.idx + lu * a.idx_cap), 4, a.max_count, 4);
   const int32_t last_slot = static_cast<int32_t>(a.max_count) - 1;
-  const int32_t t_beg = (split * kAttnWaves + wave) * TILE, stride = a.nsplit * kAttnWaves * TILE;  // (slots are below 2^30: launch conditions)
+  const int32_t t_beg = (split * NW + wave) * TILE, stride = a.nsplit * NW * TILE;  // (slots are below 2^30: launch conditions)
 
   // A tile's list entries are read ahead of the gathers of the tile before, unconditionally (clamped into the max_count entries that the
   // call names), and its rows while that tile is computed.
@@ -204,7 +229,7 @@ __global__ __launch_bounds__(kAttnThreads, kMxWavesPerSimd<T>) void attn_mx_kern
 #pragma unroll
     for (int t = 0; t < kMxLoads; ++t) {
       const int32_t i = t0 + t * GPW + grp;
-      e.at[t] = a.max_count > 0 ? list[i < last_slot ? i : last_slot] : 0;
+      e.at[t] = static_cast<int32_t>(__builtin_amdgcn_raw_buffer_load_b32(list, (i < last_slot ? i : last_slot) * 4, 0, 0));
     }
   };
   Entries entries;
@@ -232,31 +257,34 @@ __global__ __launch_bounds__(kAttnThreads, kMxWavesPerSimd<T>) void attn_mx_kern
   float m = -INFINITY, l = 0.f, acc[kMxBlock];
 #pragma unroll
   for (int e = 0; e < kMxBlock; ++e) acc[e] = 0.f;
-  auto consume = [&](const Rows& r, const int32_t left) {  // left: slots from this tile on
+  auto consume = [&](Rows& r, const int32_t left) {  // left: slots from this tile on
     float sc[kMxLoads], tmax = -INFINITY;
-    uint32_t vs[kMxLoads];
 #pragma unroll
-    for (int t = 0; t < kMxLoads; ++t) {
-      const bool valid = t * GPW + grp < left;
-      const float s = group_allreduce_sum<LPR>(q.dot(r.k[t], mx_scale(r.ks[t]))) * a.sm_scale_log2;
-      sc[t] = valid ? s : -INFINITY;
-      vs[t] = valid ? r.vs[t] : 127u;  // (a slot past the end has weight 0, and a scale under which nothing is NaN)
-      tmax = fmaxf(tmax, sc[t]);
+    for (int t = 0; t < kMxLoads; ++t) sc[t] = group_allreduce_sum<LPR>(q.dot(r.k[t], mx_scale(r.ks[t]))) * a.sm_scale_log2;
+    if (__builtin_expect(left < TILE, 0)) {  // slots past the end: weight 0, and a scale under which nothing is NaN
+#pragma unroll
+      for (int t = 0; t < kMxLoads; ++t)
+        if (t * GPW + grp >= left) {
+          sc[t] = -INFINITY;
+          r.vs[t] = 127;
+        }
     }
-    const float m_new = fmaxf(m, tmax);
-    const float m_ref = m_new > -INFINITY ? m_new : 0.f;  // nothing seen yet, or nothing but NaN
-    if (__any(m_new > m)) {
-      const float alpha = exp2_safe(m - m_ref);
+#pragma unroll
+    for (int t = 0; t < kMxLoads; ++t) tmax = fmaxf(tmax, sc[t]);
+    if (__any(tmax > m + kMxLazy)) {
+      const float m_new = fmaxf(m, tmax);
+      const float alpha = m_new > -INFINITY ? exp2_safe(m - m_new) : 0.f;
       l *= alpha;
 #pragma unroll
       for (int e = 0; e < kMxBlock; ++e) acc[e] *= alpha;
       m = m_new;
     }
+    const float m_ref = m > -INFINITY ? m : 0.f;  // nothing seen yet, or nothing but NaN
 #pragma unroll
     for (int t = 0; t < kMxLoads; ++t) {
       const float p = exp2_safe(sc[t] - m_ref);
       l += p;
-      const float scale = mx_scale(vs[t]);
+      const float scale = mx_scale(r.vs[t]);
       const uint32_t w[4] = {r.v[t].x, r.v[t].y, r.v[t].z, r.v[t].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -312,7 +340,7 @@ __global__ __launch_bounds__(kAttnThreads, kMxWavesPerSimd<T>) void attn_mx_kern
 
   // the waves of the workgroup: thread d < D owns output element d
   float M = -INFINITY, L = 0.f, o = 0.f;
-  if (tid < D) merge_waves<D, kAttnWaves>(&s_m[0], &s_l[0], &s_acc[0], tid, M, L, o);
+  if (tid < D) merge_waves<D, NW>(&s_m[0], &s_l[0], &s_acc[0], tid, M, L, o);
   if (a.nsplit == 1) {
     if (tid < D) a.out[u * D + tid] = has_weight<true>(L) ? o / L : 0.f;
     if (tid == 0 && a.lse) a.lse[u] = has_weight<true>(L) ? M * kLn2 + logf(L) : -INFINITY;
@@ -329,7 +357,7 @@ __global__ __launch_bounds__(kAttnThreads, kMxWavesPerSimd<T>) void attn_mx_kern
   }
   __syncthreads();
   if (!s_last) return;
-  combine_published<D, 1, kAttnWaves, true>(a.partials + u * a.nsplit * D, a.partials + a.pairs_off + u * a.nsplit * 2, a.nsplit, a.out + u * D,
+  combine_published<D, 1, NW, true>(a.partials + u * a.nsplit * D, a.partials + a.pairs_off + u * a.nsplit * 2, a.nsplit, a.out + u * D,
                                             a.lse ? a.lse + u : nullptr, s_m, s_l, s_acc);
   if (tid == 0) __hip_atomic_store(&a.counters[u * kCounterStrideWords], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -371,7 +399,8 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
   }
 
   // (a negative scale's sign goes to the query, so that the largest score is the largest dot product)
-  const float scale = fabsf(a.sm_scale_log2);
+  // (and none is so small that minus infinity times it is not minus infinity)
+  const float scale = a.sm_scale_log2 == 0.f ? 1.17549435e-38f : fabsf(a.sm_scale_log2);
   const uint32_t sign = __float_as_uint(a.sm_scale_log2) >> 31 << 15;
   mx_s16x8 qop[QP][KW];
 #pragma unroll
@@ -386,12 +415,21 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
     }
   }
 
-  int64_t cnt = LIST ? __builtin_amdgcn_readfirstlane(a.count[b]) : 0;
-  cnt = cnt < 0 ? 0 : (cnt > a.max_count ? a.max_count : cnt);
-  const int64_t total = cnt + (a.tail_end - a.tail_begin);
-  const int64_t w_beg = static_cast<int64_t>(split * kGroupMxWaves + wave) * STEP;
-  const int64_t stride = static_cast<int64_t>(a.nsplit) * kGroupMxWaves * STEP;
+  const int32_t w_beg = (split * kGroupMxWaves + wave) * STEP, stride = a.nsplit * kGroupMxWaves * STEP;  // (slots are below 2^30: launch conditions)
   const int32_t* list = LIST ? a.idx + b * a.idx_cap : nullptr;
+  const int32_t last_slot = static_cast<int32_t>(a.max_count) - 1;
+  // Lane r (and r + 32) of a step has the entry of its slot r, read without waiting for the count (clamped into the max_count entries
+  // that the call names): the first one comes with the count.
+  auto entry_of_lane = [&](const int32_t t0) -> int32_t {
+    const int32_t i = t0 + (lane & 31);
+    return list[i < last_slot ? i : last_slot];
+  };
+  int32_t entry = LIST ? entry_of_lane(w_beg) : 0;
+  const int32_t counted = LIST ? a.count[b] : 0;
+  __builtin_amdgcn_sched_barrier(0);
+  const int32_t cnt = LIST ? __builtin_amdgcn_readfirstlane(max(0, min(counted, last_slot + 1))) : 0;
+  const int32_t total = cnt + static_cast<int32_t>(a.tail_end - a.tail_begin);
+  const int32_t first_tail = static_cast<int32_t>(a.tail_begin) - cnt, last_row = static_cast<int32_t>(a.N) - 1;
 
   struct Raw {
     uint32_t k[2][KW], v[2][4];
@@ -416,14 +454,11 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
       r.v[t][v] = __builtin_amdgcn_raw_buffer_load_b16(codes[1], static_cast<int>(code_at), code_row, 0);
     r.vs[t][v] = __builtin_amdgcn_raw_buffer_load_b8(scales[1], static_cast<int>(scale_at), scale_row, 0);
   };
-  // Rows of a list: lane r (and r + 32) of a step has its slot r; a slot past the end the last one's row, which is attended to anyway,
-  // with weight 0.
-  auto row_of_lane = [&](const int64_t t0) -> uint32_t {
-    int64_t i = t0 + (lane & 31);
-    i = i < total ? i : total - 1;
-    int64_t n = LIST && i < cnt ? static_cast<int64_t>(list[i]) : a.tail_begin + (i - cnt);
-    n = n < 0 ? 0 : (n >= a.N ? a.N - 1 : n);  // keep the gather inside the cache whatever the list holds
-    return static_cast<uint32_t>(n);
+  // Row of a lane's slot; of a slot past the end some row, which counts as one of zeros.
+  auto row_of_lane = [&](const int32_t t0, const int32_t e) -> uint32_t {
+    const int32_t i = t0 + (lane & 31);
+    const int32_t n = LIST && i < cnt ? e : first_tail + i;
+    return static_cast<uint32_t>(max(0, min(n, last_row)));  // inside the cache whatever the list holds
   };
   auto load_rows = [&](Raw& r, const uint32_t rows) {
 #pragma unroll
@@ -442,8 +477,8 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
   // 32 rows of the range: a lane's place among them does not change, the rest of an address is scalar
   const uint32_t k_lane = i16 * a.code_n[0] + k_at, ks_lane = i16 * a.scale_n[0] + ks_at;
   const uint32_t v_lane = 4 * kb * a.code_n[1] + v_at, vs_lane = 4 * kb * a.scale_n[1] + vs_at;
-  auto load_range = [&](Raw& r, const int64_t t0) {
-    const uint32_t n = static_cast<uint32_t>(a.tail_begin + t0);
+  auto load_range = [&](Raw& r, const int32_t t0) {
+    const uint32_t n = static_cast<uint32_t>(first_tail + t0);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
       load_k(r, t, k_lane, static_cast<int>((n + 16 * t) * a.code_n[0]), ks_lane, static_cast<int>((n + 16 * t) * a.scale_n[0]));
@@ -454,12 +489,14 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
         load_v(r, t, v, v_lane, static_cast<int>((n + 16 * t + v) * a.code_n[1]), vs_lane, static_cast<int>((n + 16 * t + v) * a.scale_n[1]));
   };
 
+  // upper halves that a column's part leaves out (with eight heads every lane makes the second and third part)
+  const uint32_t less_first = PS == 8 || part >= 1 ? 0xFFFF0000u : 0u, less_second = PS == 8 || part >= 2 ? 0xFFFF0000u : 0u;
   float m = -INFINITY, l = 0.f;  // of this lane's head (l: its rows only)
   mx_acc4 acc[EV];               // accumulator v: column 4 kb + v, element EV i16 + e
 #pragma unroll
   for (int e = 0; e < EV; ++e) acc[e] = mx_acc4{0.f, 0.f, 0.f, 0.f};
 
-  auto compute = [&](const Raw& r, const int left) {  // left: slots from this step on
+  auto compute = [&](Raw& r, const int32_t left) {  // left: slots from this step on
     mx_acc4 s[2];
     float smax = -INFINITY;
 #pragma unroll
@@ -475,22 +512,25 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
         for (int x = QP - 1; x >= 0; --x) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop, qop[x][c], s[t], 0, 0, 0);
       }
     }
-    if (left < STEP) {
+    if (__builtin_expect(left < STEP, 0)) {  // slots past the end: weight 0, and a scale under which nothing is NaN
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) s[t][v] = 16 * t + 4 * kb + v < left ? s[t][v] : -INFINITY;
+        for (int v = 0; v < 4; ++v)
+          if (16 * t + 4 * kb + v >= left) {
+            s[t][v] = -INFINITY;
+            r.vs[t][v] = 127;
+          }
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int v = 0; v < 4; ++v) smax = fmaxf(smax, s[t][v]);
-    smax = fmaxf(smax, __shfl_xor(smax, 16, kWave));
-    smax = fmaxf(smax, __shfl_xor(smax, 32, kWave));
-    const float m_new = fmaxf(m, smax * scale);
-    const float m_ref = m_new > -INFINITY ? m_new : 0.f;  // nothing seen yet, or nothing but NaN
-    if (__any(m_new > m)) {
-      const float alpha = exp2_safe(m - m_ref);
+    smax = half_max<32>(half_max<16>(smax));
+    smax *= scale;
+    if (__any(smax > m + kMxLazy)) {
+      const float m_new = fmaxf(m, smax);
+      const float alpha = m_new > -INFINITY ? exp2_safe(m - m_new) : 0.f;
       l *= alpha;
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
@@ -500,20 +540,19 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
       }
       m = m_new;
     }
-    uint32_t w[2][4], low[2][4];  // this column's part of the weights, and their third part (eight heads)
+    const float m_ref = m > -INFINITY ? m : 0.f;  // nothing seen yet, or nothing but NaN
+    uint32_t w[2][4], low[2][4];  // this column's part of the weights (its upper half), and their third part (eight heads)
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         const float x = exp2_safe(fmaf(s[t][v], scale, -m_ref));
         l += x;
-        const uint32_t first = __float_as_uint(x) & 0xFFFF0000u;
-        const float rest = x - __uint_as_float(first);  // exact
-        const uint32_t second = __float_as_uint(rest) & 0xFFFF0000u;
-        low[t][v] = __float_as_uint(rest - __uint_as_float(second));  // at most 8 bits are left
-        w[t][v] = part == 0 ? first : second;
-        if (PS == 4) w[t][v] = part < 2 ? w[t][v] : (part == 2 ? low[t][v] : 0u);
-        if (PS == 8) low[t][v] = part == 0 ? low[t][v] : 0u;
+        // less the parts before it, exactly
+        const float y = x - __uint_as_float(__float_as_uint(x) & less_first);
+        const float z = y - __uint_as_float(__float_as_uint(y) & less_second);
+        w[t][v] = __float_as_uint(PS == 4 ? z : (part == 0 ? x : y));
+        low[t][v] = PS == 8 && part == 0 ? __float_as_uint(z) : 0u;
       }
     auto operand = [&](const uint32_t (&x)[2][4]) {
       const uint32_t packed[4] = {__builtin_amdgcn_perm(x[0][1], x[0][0], 0x07060302u), __builtin_amdgcn_perm(x[0][3], x[0][2], 0x07060302u),
@@ -547,32 +586,25 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
     }
   };
   if (w_beg < total) {
-    uint32_t rows = 0;  // of the next step to be loaded
-    auto load = [&](Raw& r, const int64_t t0) {
+    auto load = [&](Raw& r, const int32_t t0) {
       if (!LIST && t0 + STEP <= total) {
         load_range(r, t0);
         return;
       }
-      if (!LIST) rows = row_of_lane(t0);
+      const uint32_t rows = row_of_lane(t0, entry);
+      if (LIST) entry = entry_of_lane(t0 + stride);  // (ahead of the gathers: loads return in order)
       load_rows(r, rows);
-      if (LIST && t0 + stride < total) rows = row_of_lane(t0 + stride);
     };
-    if (LIST) rows = row_of_lane(w_beg);
-    Raw r[2];
-    load(r[0], w_beg);
-    for (int64_t t0 = w_beg; t0 < total; t0 += 2 * stride) {
-#pragma unroll
-      for (int o = 0; o < 2; ++o) {
-        const int64_t at = t0 + o * stride;
-        if (at >= total) break;
-        if (at + stride < total) load(r[1 - o], at + stride);
-        __builtin_amdgcn_sched_barrier(0);
-        compute(r[o], static_cast<int>(min(total - at, static_cast<int64_t>(STEP))));
-      }
+    Raw now, next;
+    load(now, w_beg);
+    for (int32_t t0 = w_beg; t0 < total; t0 += stride) {
+      if (t0 + stride < total) load(next, t0 + stride);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(now, total - t0);
+      now = next;
     }
   }
-  l += __shfl_xor(l, 16, kWave);
-  l += __shfl_xor(l, 32, kWave);
+  l = half_sum<32>(half_sum<16>(l));
   if (l != l) m = fmaxf(m, 0.f);  // rows that stand for NaN, perhaps alone: the merges look at lists with a maximum
   if (lane < GH) {
     gl.m[wave][lane] = m;
@@ -583,9 +615,9 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
   for (int e = 0; e < EV; ++e)
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      float x = acc[e][v];
-      if (PS == 4) x += __shfl_xor(x, 16, kWave);
-      x += __shfl_xor(x, 32, kWave);
+      float x = PS == 4 && kb == 3 ? 0.f : acc[e][v];  // (the last four columns repeat the third part)
+      if (PS == 4) x = half_sum<16>(x);
+      x = half_sum<32>(x);
       if (kb * 4 < PS && 4 * kb + v < GH) gl.acc[wave][4 * kb + v][EV * i16 + e] = x;
     }
   group_finish<D, GH, kGroupMxWaves, true>(a, u0, split, gl);
@@ -646,7 +678,7 @@ tb_status launch_td(const AttnMxLaunch& L, hipStream_t st) {
   a.xcd_map = attn_on_one_xcd(&d) && heads_per_xcd <= 65535 ? 1 : 0;  // (of a grid's third number)
   dim3 grid(a.nsplit, d.Hq, d.B);
   if (a.xcd_map) grid = dim3(kXcds, a.nsplit, static_cast<unsigned>(heads_per_xcd));
-  hipLaunchKernelGGL((attn_mx_kernel<T, D>), grid, dim3(kAttnThreads), 0, st, a);
+  hipLaunchKernelGGL((attn_mx_kernel<T, D, kAttnMxWaves>), grid, dim3(kAttnMxWaves * kWave), 0, st, a);
   return hip_status(hipGetLastError());
 }
 

@@ -236,6 +236,7 @@ struct AttnMxLaunch {
   bool shared_list;
   bool grouped;  // one list, or none, served by one workgroup per KV group (plan made for that)
 };
+constexpr int kAttnMxWaves = 4;  // of a workgroup
 constexpr int kAttnMxLoads = 2;  // K (and V) gathers of a lane per tile
 tb_status launch_attn_mx(const AttnMxLaunch& a, hipStream_t st);
 

@@ -183,7 +183,10 @@ typedef short mx_short8 __attribute__((ext_vector_type(8)));
 typedef float mx_f32x4 __attribute__((ext_vector_type(4)));
 constexpr int64_t kScoreNtStoreBytes = 16 << 20;  // score arrays from this size on bypass the caches (as for rows of other types)
 
-constexpr int64_t kScoreManyChunks = 16384;       // chunks of 64 rows from which on a wave takes four
+// Chunks of 64 rows from which on a wave takes four, whose loads are in flight together, instead of one.  One and four, us: 32 heads on 8,
+// 32768 rows (4096 chunks) 3.25 and 3.43, 65536 rows for two sequences 8.6 and 8.8, for four (32768 chunks) 14.7 and 13.9, 4 x 64 heads, 65536
+// rows of 64 elements 33.8 and 28.1, 131072 rows, fp32 57.7 and 46.0; two chunks lie in between.
+constexpr int64_t kScoreManyChunks = 16384;
 
 struct ScoreMxArgs {
   const void* q_imp;

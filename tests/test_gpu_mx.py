@@ -342,6 +342,22 @@ def test_attention_strange_lists(dtype, g, shared):
         assert_attention(got, reference(q, Kv, Vv, N, idx, cnt, most, tail), Vv)
 
 
+@pytest.mark.parametrize("sm", [0.0, -0.11, 1e-30, 3.0])
+@pytest.mark.parametrize("g,kind", [(4, "lists"), (2, "shared"), (8, "shared"), (4, "dense"), (1, "dense")])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_attention_scales(dtype, g, kind, sm):
+    """No scale at all (the mean of the rows), a negative one, and rows past the end in the last step."""
+    say(f"mx attention, sm_scale={sm}, {dtype} g={g} {kind}")
+    B, Hkv, N, D, k = 2, 2, 300, 64, 101
+    (K, Kv), (V, Vv) = random_rows(B, Hkv, N, D, 1), random_rows(B, Hkv, N, D, 2)
+    q = randn((B, Hkv * g, D), dtype, 3, 0.5)
+    idx, cnt = lists(B, 1 if kind == "shared" else Hkv * g, N, k, 4, ragged=False)
+    args = (None, None, 0, (0, N - 1)) if kind == "dense" else (idx, cnt, k, (0, 0))
+    got = attend(q, K, V, N, *args, sm=sm, shared=kind == "shared")
+    torch.cuda.synchronize()
+    assert_attention(got, reference(q, Kv, Vv, N, *args, sm=sm), Vv)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("g,kind", [(1, "lists"), (4, "lists"), (2, "shared"), (4, "shared"), (8, "dense"), (1, "dense")])
 @pytest.mark.parametrize("dtype", [F32, BF16])
