@@ -97,21 +97,39 @@ static bool fit_splits(const tb_cache_desc* d, AttnPlan& p, size_t ws_bytes) {
 }
 // Rows in 4 bits: a lane takes a block of a row, a tile is kAttnMxLoads rows per lane group.
 static int attn_mx_tile_rows_per_wg(int D) { return kAttnMxWaves * kAttnMxLoads * (64 / (D / 32)); }
-static AttnPlan attn_mx_plan(const tb_cache_desc* d, int64_t max_rows) {
+AttnPlan attn_mx_plan(const tb_cache_desc* d, int64_t max_rows) {
   return attn_plan(static_cast<int64_t>(d->B) * d->Hq, max_rows, attn_mx_tile_rows_per_wg(d->D), false, false);
 }
-// One list (or none) for all heads of a KV group: eight waves of 32 rows a step, up to one workgroup per compute unit; more groups than
-// compute units take several rounds.
-static bool attn_mx_grouped(const tb_cache_desc* d) { return d->Hq > d->Hkv; }
-static AttnPlan attn_mx_group_plan(const tb_cache_desc* d, int64_t max_rows) {
+// One list (or none) for all heads of a KV group: a workgroup per KV group pays where there is enough work, the per-head kernel has the
+// shorter way to the first row and to the end (bf16, D = 128, dense, per head and grouped, us: 8 heads on 1 32768 rows 11.0 and 17.7,
+// 131072 23.4 and 28.8; 16 on 2 32768 14.2 and 18.0, 65536 23.3 and 19.5; 16 on 4 16384 10.6 and 10.7, 32768 15.4 and 12.4; 32 on 8 4096 8.0 and
+// 8.8, 8192 10.1 and 9.7; 8 x 32 on 8 512 8.1 and 8.7, 1024 10.7 and 9.0, 8192 39.8 and 18.5; D = 64: 32 on 8 4096 7.2 and 7.0, 8 x 32 on 8 512
+// 4.9 and 7.1, 1024 8.4 and 7.3): from 200000 rows and heads on, with less than six groups proportionally more.
+bool attn_mx_grouped(const tb_cache_desc* d, int64_t rows) {
+  const int64_t groups = static_cast<int64_t>(d->B) * d->Hkv;
+  return d->Hq > d->Hkv && static_cast<int64_t>(d->B) * d->Hq * rows >= 1200000 / std::min<int64_t>(groups, 6);
+}
+// Eight waves of 32 rows a step, one workgroup a compute unit.  As attn_plan, with rounds of whole compute units: a start is worth kStart
+// rows, and every split costs the last workgroup of the group one row a head.  Against one round wherever the groups leave room
+// for it: 136 groups of two heads at D = 64, 19464 rows 70.5 us (one split) and 50.5 (seven), of eight heads, one list of 7169 rows 58.5 and
+// 49.2.  On 94 shapes of 1 to 160 groups, 250 to 130000 rows 0.6% off the best number tried on average, 7% at most; the constants were
+// chosen on them.
+AttnPlan attn_mx_group_plan(const tb_cache_desc* d, int64_t max_rows) {
+  constexpr int64_t kStart = 512, kRounds = 8;
   const int64_t groups = static_cast<int64_t>(d->B) * d->Hkv;
   if (max_rows <= 0 || groups <= 0) return AttnPlan{1, 1, 1, 1};
-  const int64_t step = 32 * kAttnGroupWaves, most = std::max<int64_t>(1, max_rows / step);
-  const int64_t want = std::max<int64_t>(1, kAttnGroupTargetWgs / groups);
-  AttnPlan p = split_plan(max_rows, std::min(want, most), step);
-  p.max_split = static_cast<int>(std::min(want, most));
-  p.least = p.nsplit;
-  return p;
+  const int64_t g = d->Hq / d->Hkv, step = 32 * kAttnGroupWaves;
+  const int64_t most = std::max<int64_t>(1, std::min(max_rows / step, kRounds * kAttnCus / groups));
+  auto cost = [&](int64_t n) { return (groups * n + kAttnCus - 1) / kAttnCus * (max_rows / n + kStart) + g * n; };
+  int64_t want = 1;
+  auto consider = [&](int64_t n) {
+    n = std::min(std::max<int64_t>(1, n), most);
+    if (cost(n) < cost(want)) want = n;
+  };
+  // as many splits as a number of rounds holds, or (few groups) as many as their hand-over is worth
+  for (int64_t rounds = 1; rounds <= kRounds; ++rounds) consider(rounds * kAttnCus / groups);
+  consider(static_cast<int64_t>(std::sqrt(static_cast<double>(max_rows) / static_cast<double>(g))));
+  return AttnPlan{static_cast<int>(want), static_cast<int>(most), static_cast<int>(want), 1};
 }
 // (the buffered form is planned alike, so that it adds up in the same order)
 static AttnPlan attn_plan(const tb_cache_desc* d, int64_t max_rows, bool shared_list = false) {
@@ -443,7 +461,7 @@ tb_status sparse_attn_mx(const tb_cache_desc* d, const void* q, const tb_mx_rows
   const int64_t units = static_cast<int64_t>(d->B) * d->Hq;
   if (units == 0) return TB_OK;
   const int64_t rows = max_count + (tail_end - tail_begin);
-  const bool grouped = (shared_list || max_count == 0) && attn_mx_grouped(d);
+  const bool grouped = (shared_list || max_count == 0) && attn_mx_grouped(d, rows);
   AttnPlan plan = grouped ? attn_mx_group_plan(d, rows) : attn_mx_plan(d, rows);
   if (!ws || !aligned16(ws) || !fit_splits(d, plan, ws_bytes)) return TB_ERR_WORKSPACE;
   const WsLayout w = ws_layout(units, d->D, plan.nsplit);
@@ -823,7 +841,7 @@ size_t tb_workspace_bytes(int32_t op, const tb_cache_desc* d, int64_t max_count)
   const int64_t units = static_cast<int64_t>(d->B) * d->Hq;
   if (op == TB_OP_ATTN_MX) {
     int most = attn_mx_plan(d, max_count).max_split;
-    if (attn_mx_grouped(d)) most = std::max(most, attn_mx_group_plan(d, max_count).max_split);
+    if (attn_mx_grouped(d, max_count)) most = std::max(most, attn_mx_group_plan(d, max_count).max_split);
     return ws_layout(units, d->D, most).total;
   }
   // two-stage selection of long rows (none for most shapes): max_count bounds the budget

@@ -239,6 +239,10 @@ struct AttnMxLaunch {
 constexpr int kAttnMxWaves = 4;  // of a workgroup
 constexpr int kAttnMxLoads = 2;  // K (and V) gathers of a lane per tile
 tb_status launch_attn_mx(const AttnMxLaunch& a, hipStream_t st);
+AttnPlan attn_mx_plan(const tb_cache_desc* d, int64_t max_rows);
+// Whether rows that all heads of a KV group read are served by a workgroup per group, and the plan for that.
+bool attn_mx_grouped(const tb_cache_desc* d, int64_t rows);
+AttnPlan attn_mx_group_plan(const tb_cache_desc* d, int64_t max_rows);
 
 // Query predictor of a producer layer (LN + two-layer MLP), see tb_predict.hip.
 struct PredictLaunch {

@@ -6,13 +6,14 @@ only the fp32 sum rounds: at most 3 d' additions and the scale, (3 d' + 2) 2^-24
 1e-5 of max(1, |lse|), the bar of fp32 rows (gpu_util.py): the queries' products are exact for both types here, and the softmax and its sums are
 fp32, where an error of the logits of (D + 4) 2^-24 sum |q k| sm_scale, 8e-6 at D = 128 and a sum of one, moves a weight by that
 share of itself and the mean of V by less."""
+import ctypes
 import math
 
 import numpy as np
 import pytest
 import torch
 
-from gpu_util import DEV, gpu_select, np_of
+from gpu_util import DEV, AttnPlan, gpu_select
 from oracle import mx
 from paper_2503_07518_amd import binding as tb
 
@@ -39,6 +40,13 @@ def mx_rows(x_np):
 def random_rows(B, Hkv, N, inner, seed):
     rng = np.random.default_rng(seed)
     return mx_rows(rng.standard_normal((B, Hkv, N, inner)) * np.exp(rng.standard_normal((1, Hkv, 1, inner)) / 2))
+
+
+def coded_rows(B, Hkv, N, inner, seed):
+    """Rows drawn as codes: every code as often, scales that differ."""
+    rng = np.random.default_rng(seed)
+    codes, scales = rng.integers(0, 256, (B, Hkv, N, inner // 2), dtype=np.uint8), rng.integers(122, 126, (B, Hkv, N, inner // 32), dtype=np.uint8)
+    return tb.MxRows(torch.from_numpy(codes).to(DEV), torch.from_numpy(scales).to(DEV)), mx.dequantize(codes, scales)
 
 
 def side_by_side(K, V):
@@ -255,6 +263,18 @@ def assert_attention(got, ref, Vv):
         assert (np.abs(lse[fin] - ref[1][fin]) <= 1e-5 * np.maximum(1.0, np.abs(ref[1][fin]))).all()
 
 
+def mx_plan(q, Hkv, rows, one_list):
+    """Whether the library serves rows that all heads read by KV groups, and how many splits a head or group gets."""
+    lib = tb.load_library()
+    d = tb.tb_cache_desc(q.shape[0], q.shape[1], Hkv, q.shape[2], 32, tb.TB_F32 if q.dtype == F32 else tb.TB_BF16)
+    grouped, by_head, by_group = (lib._ZN2tb15attn_mx_groupedEPK13tb_cache_descl, lib._ZN2tb12attn_mx_planEPK13tb_cache_descl,
+                                  lib._ZN2tb18attn_mx_group_planEPK13tb_cache_descl)
+    for f, kind in ((grouped, ctypes.c_bool), (by_head, AttnPlan), (by_group, AttnPlan)):
+        f.restype, f.argtypes = kind, [ctypes.POINTER(tb.tb_cache_desc), ctypes.c_int64]
+    by = one_list and grouped(ctypes.byref(d), rows)
+    return by, (by_group if by else by_head)(ctypes.byref(d), rows).nsplit
+
+
 def lists(B, heads, N, k, seed, ragged=True):
     """Ascending lists of up to k rows; ragged: an empty one, a single row, and lengths in between."""
     rng = np.random.default_rng(seed)
@@ -320,6 +340,99 @@ def test_attention_dense(dtype, D, B, Hkv, g, N, tail, shared):
     got = attend(q, *side_by_side(K, V), N, None, None, 0, tail, shared=shared, lse=not shared)
     torch.cuda.synchronize()
     assert_attention(got, reference(q, Kv, Vv, N, None, None, 0, tail), Vv)
+
+
+# one list or the dense range with enough heads and rows for a workgroup per KV group: B, Hkv, g, rows, splits
+GROUPED = [(200, 8, 8, 16, 1), (850, 8, 2, 15, 1), (410, 8, 2, 31, 1), (60, 8, 4, 111, 1), (13, 8, 8, 250, 1), (6, 8, 8, 527, 2), (2, 4, 4, 6400, 25),
+           (1, 8, 8, 3333, 13), (1, 2, 8, 38000, 68)]
+
+
+@pytest.mark.parametrize("dtype,D", [(BF16, 128), (F32, 64)])
+@pytest.mark.parametrize("B,Hkv,g,rows,splits", GROUPED)
+@pytest.mark.parametrize("kind", ["dense", "shared"])
+def test_attention_by_groups(dtype, D, B, Hkv, g, rows, splits, kind):
+    say(f"mx attention by KV groups, {kind} {dtype} D={D} B={B} Hkv={Hkv} g={g} rows={rows}")
+    N, tail = rows + 9, 3
+    (K, Kv), (V, Vv) = coded_rows(B, Hkv, N, D, 1), coded_rows(B, Hkv, N, D, 2)
+    q = randn((B, Hkv * g, D), dtype, 3)
+    if kind == "dense":
+        args = (None, None, 0, (5, rows + 5))
+    else:  # counts below the number that the call names, none at all among them
+        idx, cnt = lists(B, 1, N - tail, rows - tail, 4)
+        args = (idx, cnt, rows - tail, (N - tail, N))
+    assert mx_plan(q, Hkv, rows, True) == (True, splits)
+    got = attend(q, *side_by_side(K, V), N, *args, shared=True)
+    torch.cuda.synchronize()
+    ref = reference(q, Kv, Vv, N, *args)
+    assert_attention(got, ref, Vv)
+    again = attend(q, K, V, N, *args, shared=True)  # arrays of their own: the same sums
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
+
+
+@pytest.mark.parametrize("g,B,rows", [(8, 13, 250), (4, 4, 1700), (2, 20, 700)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", ["dense", "shared"])
+def test_groups_of_strange_rows(dtype, D, g, B, rows, kind):
+    """Rows that stand for NaN, attended to and not; entries outside the cache, counts below zero and beyond; scales of all signs."""
+    say(f"mx attention by KV groups, strange rows, {kind} {dtype} D={D} g={g} B={B} rows={rows}")
+    Hkv, N = 8, rows + 20
+    (K, Kv), (V, Vv) = coded_rows(B, Hkv, N, D, 1), coded_rows(B, Hkv, N, D, 2)
+    q = randn((B, Hkv * g, D), dtype, 3, 0.5)
+
+    def spoil(r, v, b, h, n, c):
+        r.scales[b, h, n, c] = 255
+        v[b, h, n, 32 * c:32 * c + 32] = np.nan
+
+    spoil(K, Kv, 0, 0, 50, 1)
+    spoil(V, Vv, 1, 1, 60, 0)
+    for n in (0, 1, N - 1):  # attended to by nobody
+        for c in range(D // 32):
+            for r, v in ((K, Kv), (V, Vv)):
+                r.scales[:, :, n, c] = 255
+                v[:, :, n, 32 * c:32 * c + 32] = np.nan
+    if kind == "dense":
+        args = (None, None, 0, (2, rows + 2))
+    else:
+        rng = np.random.default_rng(3)
+        idx = rng.integers(2, N - 1, (B, 1, rows + 7)).astype(np.int32)
+        idx[:2, 0, :2] = (50, 60)
+        idx[-1, 0, 3:7] = (-5, N, 2 ** 31 - 1, -2 ** 31)
+        cnt = np.full((B, 1), rows - 13, dtype=np.int32)
+        cnt[2], cnt[3] = -3, rows + 100
+        args = (torch.from_numpy(idx).to(DEV), torch.from_numpy(cnt).to(DEV), rows, (2, 2))
+    assert mx_plan(q, Hkv, rows, True)[0]
+    with np.errstate(invalid="ignore"):
+        for sm in (D ** -0.5, -0.1, 0.0):
+            got = attend(q, *side_by_side(K, V), N, *args, sm=sm, shared=True)
+            torch.cuda.synchronize()
+            ref = reference(q, Kv, Vv, N, *args, sm=sm)
+            assert 0 < np.isnan(ref[0]).sum() < ref[0].size
+            assert_attention(got, ref, Vv)
+
+
+@pytest.mark.parametrize("kind", ["dense", "shared"])
+def test_groups_of_nan_rows_alone_and_of_growing_logits(kind):
+    """Nothing but NaN; then logits that grow along the rows by far more than what a reference may lag behind, to several hundred."""
+    say(f"mx attention by KV groups, NaN alone, growing logits, {kind}")
+    B, Hkv, g, N, D = 2, 8, 8, 3000, 128
+    rng = np.random.default_rng(5)
+    q = randn((B, Hkv * g, D), BF16, 3, 4.0)
+    qn = q.float().cpu().numpy().reshape(B, Hkv, g, D)[:, :, 0]
+    x = rng.standard_normal((B, Hkv, N, D)) * 0.3 + np.sign(qn)[:, :, None] * np.linspace(-4, 4, N)[:, None]
+    (K, Kv), (V, Vv) = mx_rows(x), coded_rows(B, Hkv, N, D, 2)
+    idx = torch.arange(N, dtype=torch.int32, device=DEV).expand(B, 1, N).contiguous()
+    args = (None, None, 0, (0, N)) if kind == "dense" else (idx, torch.full((B, 1), N, dtype=torch.int32, device=DEV), N, (0, 0))
+    assert mx_plan(q, Hkv, N, True)[0]
+    got = attend(q, K, V, N, *args, shared=True)
+    torch.cuda.synchronize()
+    ref = reference(q, Kv, Vv, N, *args)
+    mag = (np.abs(q.float().cpu().numpy()).reshape(B, Hkv, g, D) @ np.abs(Kv).transpose(0, 1, 3, 2)).max() * D ** -0.5
+    bar = 2 * (D + 4) * 2.0 ** -24 * mag  # what fp32 has of such logits, and of the weights
+    assert mag > 100 and np.abs(got[0].cpu().numpy() - ref[0]).max() <= bar * np.abs(Vv).max() and np.abs(got[1].cpu().numpy() - ref[1]).max() <= bar
+    K.scales.fill_(255)
+    got = attend(q, K, V, N, *args, shared=True)
+    assert torch.isnan(got[0]).all() and torch.isnan(got[1]).all()
 
 
 @pytest.mark.parametrize("g,shared", [(1, False), (4, False), (4, True), (8, True)])
@@ -460,8 +573,7 @@ def test_attention_row_offsets_past_31_bits():
 # --------------------------------------------------------------------------- workspaces, streams, graphs
 
 def step(B, Hkv, g, N, D, k, dtype, seed):
-    (K, Kv), (V, Vv) = random_rows(B, Hkv, N, D, seed), random_rows(B, Hkv, N, D, seed + 1)
-    K, V = side_by_side(K, V)
+    K, V = side_by_side(coded_rows(B, Hkv, N, D, seed)[0], coded_rows(B, Hkv, N, D, seed + 1)[0])
     idx, cnt = lists(B, Hkv * g, N, k, seed + 2, ragged=False)
     return dict(q=randn((B, Hkv * g, D), dtype, seed + 3), K=K, V=V, N=N, idx=idx, cnt=cnt, max_count=k)
 
