@@ -111,6 +111,101 @@ class IntervalDecoder:
         return self.out, self.lse
 
 
+class MxIntervalDecoder:
+    """The interval loop over a cache in microscaled 4-bit floating point (``binding.MxCache``): K, V and the projected keys are held in
+    that form alone.
+
+    ``append`` takes the rows of a prompt, or of one step, in the model's element type: K and V go into the cache at once, the keys are
+    projected by ``W`` in that type before they are rounded to 4 bits -- a prompt's at once, the rows of single steps together on the next
+    prediction step (until then at most ``P`` of them wait).  ``step`` attends over all rows appended so far, as
+    ``IntervalDecoder.step`` does: selected rows on prediction steps, then the widened list and the rows since.
+
+    With ``headless=True`` there is one importance head: the cache's ``Kimp`` has one head, which the caller keeps up to date
+    (``tb_quantize_mx``), ``W`` is not used (None), and one list per batch element serves every head.
+    """
+
+    PROJECT_ROWS = 8192  # of a prompt, whose projected keys pass through a buffer
+
+    def __init__(self, cache: tb.MxCache, W, Hq: int, k: int, P: int, radius: int, sink: int = 0, window: int = 0, sm_scale: float = 1.0,
+                 score_scale: float = 1.0, mode: int = 0, expand_on_predict: bool = False, headless: bool = False, dtype=torch.bfloat16):
+        self.cache, self.W, self.Hq, self.k, self.P, self.radius = cache, W, Hq, k, P, radius
+        self.sink, self.window, self.sm_scale, self.score_scale = sink, window, sm_scale, score_scale
+        self.mode, self.expand_on_predict, self.headless, self.dtype = mode, expand_on_predict, headless, dtype
+        self.B, self.Hkv, self.Ncap = cache.K.codes.shape[:3]
+        self.D, dev = cache.K.inner, cache.K.codes.device
+        assert cache.Kimp is not None and cache.Kimp.codes.shape[1] == (1 if headless else self.Hkv)
+        B, Hl = self.B, 1 if headless else Hq  # heads that carry a list of their own
+        self.sel_cap = sink + k + window
+        self.exp_cap = min(self.Ncap, ((2 * radius + 1) if mode == 0 else 2) * self.sel_cap)
+        self.scores = torch.empty((B, Hl, (self.Ncap + 3) // 4 * 4), dtype=torch.float32, device=dev)
+        self.idx = torch.zeros((B, Hl, self.sel_cap), dtype=torch.int32, device=dev)
+        self.cnt = torch.zeros((B, Hl), dtype=torch.int32, device=dev)
+        self.exp_idx = torch.zeros((B, Hl, self.exp_cap), dtype=torch.int32, device=dev)
+        self.exp_cnt = torch.zeros((B, Hl), dtype=torch.int32, device=dev)
+        self.out = torch.empty((B, Hq, self.D), dtype=torch.float32, device=dev)
+        self.lse = torch.empty((B, Hq), dtype=torch.float32, device=dev)
+        self.ws = tb.new_workspace(tb.TB_OP_ATTN_MX, tb.make_mx_desc(self.Ncap, Hq, dtype, K=cache.K), max(self.exp_cap + P, self.sel_cap))
+        self.sel_ws = tb.new_workspace(tb.TB_OP_SELECT, tb.make_mx_desc(self.Ncap, Hl, dtype, Kimp=cache.Kimp), self.sel_cap)
+        if not headless:
+            self.waiting = torch.empty((B, self.Hkv, P, self.D), dtype=dtype, device=dev)  # keys not projected yet
+            self.projected = torch.empty((B, self.Hkv, max(P, min(self.Ncap, self.PROJECT_ROWS)), W.shape[2]), dtype=dtype, device=dev)
+        self.N = 0        # rows in the cache
+        self.n_waiting = 0  # the last ones of them, whose keys wait
+        self.N_pred = None
+
+    def _project(self, keys: torch.Tensor, first: int) -> None:
+        """Projected keys of rows [first, first + n) from their keys [B, Hkv, n, D]."""
+        n = keys.shape[2]
+        for at in range(0, n, self.projected.shape[2]):
+            part, rows = keys[:, :, at:], min(n - at, self.projected.shape[2])
+            desc = tb.make_desc(rows, self.Hkv, K=part, Kimp=self.projected)
+            tb.tb_project_keys(desc, part, self.W, self.projected, 0, rows)
+            tb.tb_quantize_mx(desc, None, None, self.projected, 0, None, None, self.cache.Kimp, first + at, rows)
+
+    def _project_waiting(self) -> None:
+        if self.n_waiting:
+            self._project(self.waiting[:, :, :self.n_waiting], self.N - self.n_waiting)
+            self.n_waiting = 0
+
+    def append(self, K: torch.Tensor, V: torch.Tensor) -> None:
+        """K, V: [B, Hkv, n, D], the next n rows."""
+        n = K.shape[2]
+        assert K.shape == V.shape == (self.B, self.Hkv, n, self.D) and K.dtype == V.dtype == self.dtype
+        if self.N + n > self.Ncap:
+            raise ValueError(f"{self.N} + {n} rows in a cache for {self.Ncap}")
+        tb.tb_quantize_mx(tb.make_desc(n, self.Hkv, K=K, V=V), K, V, None, 0, self.cache.K, self.cache.V, None, self.N, n)
+        if not self.headless:
+            if self.n_waiting + n > self.P:
+                self._project_waiting()
+            if n > self.P:
+                self._project(K, self.N)
+            else:
+                self.waiting[:, :, self.n_waiting:self.n_waiting + n].copy_(K)
+                self.n_waiting += n
+        self.N += n
+
+    def step(self, t: int, q: torch.Tensor, q_imp: torch.Tensor):
+        """Step t over the rows appended so far.  Returns (out, lse) views valid until the next call."""
+        c, N = self.cache, self.N
+        attend = tb.tb_sparse_decode_attn_shared_mx if self.headless else tb.tb_sparse_decode_attn_mx
+        desc = tb.make_mx_desc(N, self.Hq, self.dtype, K=c.K)
+        if t % self.P == 0:
+            if not self.headless:
+                self._project_waiting()
+            Hl = self.idx.shape[1]
+            lists = tb.make_mx_desc(N, Hl, self.dtype, Kimp=c.Kimp)
+            tb.tb_score_mx(lists, q_imp, c.Kimp, self.score_scale, self.scores)
+            tb.tb_select_topk(lists, self.scores, self.k, self.sink, self.window, self.idx, self.cnt, self.sel_ws)
+            tb.tb_expand_neighbors(self.B, Hl, N, self.radius, self.mode, self.idx, self.cnt, self.exp_idx, self.exp_cnt)
+            self.N_pred = N
+        if t % self.P == 0 and not self.expand_on_predict:
+            attend(desc, q, c.K, c.V, self.idx, self.cnt, self.sel_cap, self.sm_scale, self.out, self.lse, self.ws)
+        else:
+            attend(desc, q, c.K, c.V, self.exp_idx, self.exp_cnt, self.exp_cap, self.sm_scale, self.out, self.lse, self.ws,
+                   tail_begin=self.N_pred, tail_end=N)
+        return self.out, self.lse
+
+
 class RingLayoutDecoder:
     """The three physical buffers of Sec. 3.3 "Inference Setup", driven through the C-ABI calls.
 

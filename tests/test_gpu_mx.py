@@ -16,6 +16,7 @@ import torch
 from gpu_util import DEV, AttnPlan, gpu_select
 from oracle import mx
 from paper_2503_07518_amd import binding as tb
+from paper_2503_07518_amd import interval
 
 pytestmark = pytest.mark.gpu
 
@@ -662,3 +663,63 @@ def test_steps_in_a_graph(kind):
         torch.cuda.synchronize()
         for got, ref in zip((scores, out, lse, K.codes, V.scales), want):
             assert torch.equal(got, ref), f"replay {r}"
+
+
+# --------------------------------------------------------------------------- the interval loop
+
+@pytest.mark.parametrize("dtype,headless,mode,expand", [(BF16, False, 0, False), (F32, False, 1, True), (BF16, True, 0, False)])
+def test_interval_loop(oracle, monkeypatch, dtype, headless, mode, expand):
+    """A prompt, then single rows and steps; every stage against the oracle on what the stage before has left on the GPU."""
+    say(f"mx interval loop {dtype} headless={headless} mode={mode} expand_on_predict={expand}")
+    B, Hkv, g, D, d, N0, k, P, radius, sink, window = 2, 2, 4, 128, 32, 700, 60, 4, 1, 5, 9
+    Hq, Ncap, dn = Hkv * g, N0 + 30, "f32" if dtype == F32 else "bf16"
+    K, V = randn((B, Hkv, Ncap, D), dtype, 1), randn((B, Hkv, Ncap, D), dtype, 2)
+    W = randn((1, D, d), dtype, 3, D ** -0.5)
+    cache = tb.MxCache(B, Hkv, Ncap, D, 0 if headless else d)
+    if headless:
+        one = randn((B, 1, Ncap, d), dtype, 4)
+        cache.Kimp = tb.MxCache(B, 1, Ncap, D, d).Kimp
+        tb.tb_quantize_mx(tb.make_desc(Ncap, 1, Kimp=one), None, None, one, 0, None, None, cache.Kimp, 0, Ncap)
+    monkeypatch.setattr(interval.MxIntervalDecoder, "PROJECT_ROWS", 256)  # the prompt in three pieces
+    loop = interval.MxIntervalDecoder(cache, None if headless else W, Hq, k, P, radius, sink=sink, window=window, sm_scale=D ** -0.5, mode=mode,
+                                      expand_on_predict=expand, headless=headless, dtype=dtype)
+    loop.append(K[:, :, :N0 - 3], V[:, :, :N0 - 3])
+    loop.append(K[:, :, N0 - 3:N0], V[:, :, N0 - 3:N0])
+    kept = None
+    for t in range(11):
+        N = N0 + t
+        if t:
+            loop.append(K[:, :, N - 1:N], V[:, :, N - 1:N])
+        assert loop.N == N
+        q, q_imp = randn((B, Hq, D), dtype, 100 + t), randn((B, 1 if headless else Hq, d), dtype, 200 + t)
+        out, lse = loop.step(t, q, q_imp)
+        torch.cuda.synchronize()
+        for rows, x in ((cache.K, K), (cache.V, V)):
+            codes, scales = mx.quantize(x[:, :, :N].float().cpu().numpy())
+            assert np.array_equal(rows.codes[:, :, :N].cpu().numpy(), codes) and np.array_equal(rows.scales[:, :, :N].cpu().numpy(), scales)
+        Kv, Vv, Iv = (mx.dequantize(r.codes.cpu().numpy(), r.scales.cpu().numpy()) for r in (cache.K, cache.V, cache.Kimp))
+        if t % P == 0:
+            if not headless:  # the projected keys are those of the rows in their own type
+                Kimp = torch.zeros((B, Hkv, N, d), dtype=dtype, device=DEV)
+                tb.tb_project_keys(tb.make_desc(N, Hkv, K=K, Kimp=Kimp), K, W, Kimp, 0, N)
+                near = mx.dequantize(*mx.quantize(Kimp.float().cpu().numpy()))
+                # (another number of rows a call may sum in another order: the values themselves are near, a code next to a border moves)
+                assert np.mean(near == Iv[:, :, :N]) > 0.999
+                assert np.abs(near - Iv[:, :, :N]).max() <= 0.5 * np.abs(near).max()
+            scores = loop.scores[:, :, :N]
+            assert_score(torch.nn.functional.pad(scores, (0, 1), value=float("nan")), q_imp, Iv, N, 1.0)
+            idx, cnt = oracle.select_topk(scores.cpu().numpy(), k, sink, window)
+            assert np.array_equal(loop.cnt.cpu().numpy(), cnt) and np.array_equal(loop.idx.cpu().numpy()[:, :, :idx.shape[2]], idx)
+            exp = oracle.expand_neighbors(idx, cnt, N, radius, mode=mode)
+            for b in range(B):
+                for h in range(idx.shape[1]):
+                    n = int(exp[1][b, h])
+                    assert int(loop.exp_cnt[b, h]) == n and np.array_equal(loop.exp_idx[b, h, :n].cpu().numpy(), exp[0][b, h, :n])
+            kept = N
+        if t % P == 0 and not expand:
+            ref = reference(q, Kv, Vv, N, loop.idx, loop.cnt, loop.sel_cap)
+        else:
+            ref = reference(q, Kv, Vv, N, loop.exp_idx, loop.exp_cnt, loop.exp_cap, (kept, N))
+        assert_attention((out, lse), ref, Vv)
+    with pytest.raises(ValueError):
+        loop.append(K, V)
