@@ -278,12 +278,11 @@ tb_status tb_score_mx(const tb_cache_desc* desc, const void* q_imp, const tb_mx_
 /* tb_sparse_decode_attn over a cache in 4 bits: lists, dense range, results as there.  idx and count may be NULL with max_count = 0
  * (the dense range alone: decode attention over all rows is tail_begin = 0, tail_end = N).  An attended row with a block that stands
  * for NaN makes the row's weight or the block's outputs NaN, as the formula does; rows that are not attended add nothing,
- * whatever they hold.  ws: tb_workspace_bytes(TB_OP_ATTN_MX, ...). */
+ * whatever they hold.  Limits (else TB_ERR_UNSUPPORTED): N <= 2^24, max_count <= 2^29, strides between rows below 2^24 bytes, a
+ * head's rows below 4 GiB.  ws: tb_workspace_bytes(TB_OP_ATTN_MX, ...). */
 tb_status tb_sparse_decode_attn_mx(const tb_cache_desc* desc, const void* q, const tb_mx_rows* K, const tb_mx_rows* V, const int32_t* idx,
                                    const int32_t* count, int64_t idx_cap, int64_t max_count, int64_t tail_begin, int64_t tail_end,
                                    float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes, void* stream);
-
-/* (limits of the two: N <= 2^24, strides between rows below 2^24, a head's rows below 4 GiB.) */
 
 /* The head-less form: one list per batch element for all of its heads, as tb_sparse_decode_attn_shared. */
 tb_status tb_sparse_decode_attn_shared_mx(const tb_cache_desc* desc, const void* q, const tb_mx_rows* K, const tb_mx_rows* V,

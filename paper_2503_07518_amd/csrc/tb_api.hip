@@ -457,7 +457,7 @@ tb_status sparse_attn_mx(const tb_cache_desc* d, const void* q, const tb_mx_rows
     if (d->N * r->code_stride_n >= (int64_t{1} << 32) || d->N * r->scale_stride_n >= (int64_t{1} << 32)) return TB_ERR_UNSUPPORTED;
   }
   if (!aligned16(q)) return TB_ERR_UNSUPPORTED;
-  if (max_count + (tail_end - tail_begin) > (int64_t{1} << 30)) return TB_ERR_UNSUPPORTED;
+  if (max_count > (int64_t{1} << 29)) return TB_ERR_UNSUPPORTED;  // (an offset into a list is 32 bits of bytes)
   const int64_t units = static_cast<int64_t>(d->B) * d->Hq;
   if (units == 0) return TB_OK;
   const int64_t rows = max_count + (tail_end - tail_begin);

@@ -214,7 +214,7 @@ __global__ __launch_bounds__(NW * kWave, kMxWavesPerSimd<T>) void attn_mx_kernel
   // (without a list none of its entries is read)
   const MxBuffer list = mx_buffer(reinterpret_cast<const uint8_t*>(a.idx + lu * a.idx_cap), 4, a.max_count, 4);
   const int32_t last_slot = static_cast<int32_t>(a.max_count) - 1;
-  const int32_t t_beg = (split * NW + wave) * TILE, stride = a.nsplit * NW * TILE;  // (slots are below 2^30: launch conditions)
+  const int32_t t_beg = (split * NW + wave) * TILE, stride = a.nsplit * NW * TILE;  // (slots are below 2^29: launch conditions)
 
   // A tile's list entries are read ahead of the gathers of the tile before, unconditionally (clamped into the max_count entries that the
   // call names), and its rows while that tile is computed.
@@ -229,7 +229,7 @@ __global__ __launch_bounds__(NW * kWave, kMxWavesPerSimd<T>) void attn_mx_kernel
 #pragma unroll
     for (int t = 0; t < kMxLoads; ++t) {
       const int32_t i = t0 + t * GPW + grp;
-      e.at[t] = static_cast<int32_t>(__builtin_amdgcn_raw_buffer_load_b32(list, (i < last_slot ? i : last_slot) * 4, 0, 0));
+      e.at[t] = static_cast<int32_t>(__builtin_amdgcn_raw_buffer_load_b32(list, static_cast<int>(static_cast<uint32_t>(i < last_slot ? i : last_slot) * 4u), 0, 0));
     }
   };
   Entries entries;
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
     }
   }
 
-  const int32_t w_beg = (split * kGroupMxWaves + wave) * STEP, stride = a.nsplit * kGroupMxWaves * STEP;  // (slots are below 2^30: launch conditions)
+  const int32_t w_beg = (split * kGroupMxWaves + wave) * STEP, stride = a.nsplit * kGroupMxWaves * STEP;  // (slots are below 2^29: launch conditions)
   const int32_t* list = LIST ? a.idx + b * a.idx_cap : nullptr;
   const int32_t last_slot = static_cast<int32_t>(a.max_count) - 1;
   // Lane r (and r + 32) of a step has the entry of its slot r, read without waiting for the count (clamped into the max_count entries

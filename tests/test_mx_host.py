@@ -85,6 +85,8 @@ def test_score_refusals(lib, want, kw):
     (UNS, dict(d=desc(N=1 << 20), K=rows(N=1 << 20, code_stride_n=4096), V=rows(N=1 << 20))),
     (UNS, dict(d=desc(N=1 << 20), K=rows(N=1 << 20), V=rows(N=1 << 20, scale_stride_n=4096))),
     (UNS, dict(K=rows(code_stride_n=1 << 62))), (UNS, dict(d=desc(N=1 << 31), K=rows(N=1 << 31), V=rows(N=1 << 31))),
+    (UNS, dict(cap=1 << 30, max_count=(1 << 29) + 1)), (UNS, dict(V=rows(code_stride_n=1 << 24), d=desc(N=10))),
+    (UNS, dict(d=desc(N=(1 << 24) + 1), K=rows(N=1 << 25), V=rows(N=1 << 25))),
     (WS, dict(ws=None)), (WS, dict(ws=ODD)), (WS, dict(ws_bytes=16)),
 ])
 def test_attention_refusals(lib, want, kw, shared):
