@@ -624,13 +624,9 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
 }
 
 template <typename T, int D, int GH>
-tb_status launch_group(const AttnMxArgs& a, const AttnMxLaunch& L, hipStream_t st) {
+tb_status launch_group(AttnMxArgs& a, const AttnMxLaunch& L, hipStream_t st) {
   const dim3 grid(L.plan.nsplit, L.desc->Hkv, L.desc->B);
-  if (L.max_count > 0)
-    hipLaunchKernelGGL((attn_group_mx_kernel<T, D, GH, true>), grid, dim3(kGroupMxWaves * kWave), 0, st, a);
-  else
-    hipLaunchKernelGGL((attn_group_mx_kernel<T, D, GH, false>), grid, dim3(kGroupMxWaves * kWave), 0, st, a);
-  return hip_status(hipGetLastError());
+  return launch_one(L.max_count > 0 ? attn_group_mx_kernel<T, D, GH, true> : attn_group_mx_kernel<T, D, GH, false>, grid, kGroupMxWaves * kWave, st, a);
 }
 
 template <typename T, int D>
@@ -678,8 +674,7 @@ tb_status launch_td(const AttnMxLaunch& L, hipStream_t st) {
   a.xcd_map = attn_on_one_xcd(&d) && heads_per_xcd <= 65535 ? 1 : 0;  // (of a grid's third number)
   dim3 grid(a.nsplit, d.Hq, d.B);
   if (a.xcd_map) grid = dim3(kXcds, a.nsplit, static_cast<unsigned>(heads_per_xcd));
-  hipLaunchKernelGGL((attn_mx_kernel<T, D, kAttnMxWaves>), grid, dim3(kAttnMxWaves * kWave), 0, st, a);
-  return hip_status(hipGetLastError());
+  return launch_one(attn_mx_kernel<T, D, kAttnMxWaves>, grid, kAttnMxWaves * kWave, st, a);
 }
 
 }  // namespace

@@ -162,11 +162,7 @@ tb_status launch_copy(const MxCopyLaunch& L, hipStream_t st) {
   for (int t = 2; t >= 1; --t)
     if (!L.rows_of[t]) k.first_wg[t] = INT32_MAX;
   const dim3 grid(static_cast<unsigned>(wgs), d.Hkv, d.B);
-  if (L.back)
-    hipLaunchKernelGGL((dequantize_mx_kernel<T>), grid, dim3(kMxThreads), 0, st, k);
-  else
-    hipLaunchKernelGGL((quantize_mx_kernel<T>), grid, dim3(kMxThreads), 0, st, k);
-  return hip_status(hipGetLastError());
+  return launch_one(L.back ? dequantize_mx_kernel<T> : quantize_mx_kernel<T>, grid, kMxThreads, st, k);
 }
 
 // ---- scores -------------------------------------------------------------------------------------
@@ -300,14 +296,11 @@ __global__ __launch_bounds__(kMxThreads) void score_mx_kernel(ScoreMxArgs a) {
 }
 
 template <typename T, int DIMP, int G>
-tb_status launch_score_tdg(const ScoreMxArgs& a, const tb_cache_desc& d, hipStream_t st) {
+tb_status launch_score_tdg(ScoreMxArgs& a, const tb_cache_desc& d, hipStream_t st) {
   const int64_t chunks = (d.N + kWave - 1) / kWave, waves = kMxThreads / kWave;
   auto grid = [&](int64_t per_wave) { return dim3(static_cast<unsigned>((chunks + waves * per_wave - 1) / (waves * per_wave)), d.Hkv, d.B); };
-  if (chunks * d.Hkv * d.B >= kScoreManyChunks)
-    hipLaunchKernelGGL((score_mx_kernel<T, DIMP, G, 4>), grid(4), dim3(kMxThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL((score_mx_kernel<T, DIMP, G, 1>), grid(1), dim3(kMxThreads), 0, st, a);
-  return hip_status(hipGetLastError());
+  if (chunks * d.Hkv * d.B >= kScoreManyChunks) return launch_one(score_mx_kernel<T, DIMP, G, 4>, grid(4), kMxThreads, st, a);
+  return launch_one(score_mx_kernel<T, DIMP, G, 1>, grid(1), kMxThreads, st, a);
 }
 
 template <typename T, int DIMP>
