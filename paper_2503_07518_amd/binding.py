@@ -213,10 +213,6 @@ class MxCache:
                                torch.zeros((B, Hkv, Ncap, Dimp // MX_BLOCK), dtype=torch.uint8, device=device))
 
 
-def _mx(rows: Optional[MxRows]):
-    return None if rows is None else rows.ref
-
-
 def make_mx_desc(N: int, Hq: int, dtype: torch.dtype, K: Optional[MxRows] = None, Kimp: Optional[MxRows] = None) -> tb_cache_desc:
     """Describe a layer whose rows are in 4 bits: its shape, and the element type of the queries."""
     ref = K if K is not None else Kimp
@@ -389,44 +385,59 @@ def tb_decode_step(desc, q_imp, Kimp, score_scale: float, q, K, V, k: int, sink:
                                          ws.numel() * ws.element_size(), _stream(stream)), "tb_decode_step")
 
 
+# (The calls of the 4-bit cache spell their arguments out: a function around every pointer costs 0.4 us of a call's 5.5.)
 def tb_quantize_mx(desc, K, V, Kimp, src_row: int, Kq: Optional[MxRows], Vq: Optional[MxRows], Kimpq: Optional[MxRows], dst_row: int,
                    rows: int, stream=None) -> None:
     """Rows src_row + i of K, V and Kimp (desc; None: left out) to rows dst_row + i of Kq, Vq and Kimpq, i < rows."""
-    _check(load_library().tb_quantize_mx(ctypes.byref(desc), _ptr(K), _ptr(V), _ptr(Kimp), src_row, _mx(Kq), _mx(Vq), _mx(Kimpq), dst_row,
-                                         rows, _stream(stream)), "tb_quantize_mx")
+    rc = (_lib or load_library()).tb_quantize_mx(
+        ctypes.byref(desc), None if K is None else K.data_ptr(), None if V is None else V.data_ptr(),
+        None if Kimp is None else Kimp.data_ptr(), src_row, None if Kq is None else Kq.ref, None if Vq is None else Vq.ref,
+        None if Kimpq is None else Kimpq.ref, dst_row, rows, _stream(stream))
+    if rc:
+        _check(rc, "tb_quantize_mx")
 
 
 def tb_dequantize_mx(desc, Kq: Optional[MxRows], Vq: Optional[MxRows], Kimpq: Optional[MxRows], src_row: int, K, V, Kimp, dst_row: int,
                      rows: int, stream=None) -> None:
     """The values that rows src_row + i of Kq, Vq and Kimpq stand for to rows dst_row + i of K, V and Kimp (desc), i < rows."""
-    _check(load_library().tb_dequantize_mx(ctypes.byref(desc), _mx(Kq), _mx(Vq), _mx(Kimpq), src_row, _ptr(K), _ptr(V), _ptr(Kimp), dst_row,
-                                           rows, _stream(stream)), "tb_dequantize_mx")
+    rc = (_lib or load_library()).tb_dequantize_mx(
+        ctypes.byref(desc), None if Kq is None else Kq.ref, None if Vq is None else Vq.ref, None if Kimpq is None else Kimpq.ref, src_row,
+        None if K is None else K.data_ptr(), None if V is None else V.data_ptr(), None if Kimp is None else Kimp.data_ptr(), dst_row, rows,
+        _stream(stream))
+    if rc:
+        _check(rc, "tb_dequantize_mx")
 
 
 def tb_score_mx(desc, q_imp, Kimp: MxRows, scale: float, scores, stream=None) -> None:
     assert q_imp.is_contiguous() and scores.stride(-1) == 1
-    _check(load_library().tb_score_mx(ctypes.byref(desc), _ptr(q_imp), Kimp.ref, scale, _ptr(scores), scores.stride(-2), _stream(stream)),
-           "tb_score_mx")
+    rc = (_lib or load_library()).tb_score_mx(ctypes.byref(desc), q_imp.data_ptr(), Kimp.ref, scale, scores.data_ptr(), scores.stride(-2),
+                                              _stream(stream))
+    if rc:
+        _check(rc, "tb_score_mx")
 
 
 def tb_sparse_decode_attn_mx(desc, q, K: MxRows, V: MxRows, idx, count, max_count: int, sm_scale: float, out, lse, ws, tail_begin: int = 0,
                              tail_end: int = 0, stream=None) -> None:
     """idx and count may be None with max_count = 0: the dense range alone."""
     assert q.is_contiguous() and out.is_contiguous()
-    _check(load_library().tb_sparse_decode_attn_mx(ctypes.byref(desc), _ptr(q), K.ref, V.ref, _ptr(idx), _ptr(count),
-                                                   0 if idx is None else idx.stride(-2), max_count, tail_begin, tail_end, sm_scale, _ptr(out),
-                                                   _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)),
-           "tb_sparse_decode_attn_mx")
+    rc = (_lib or load_library()).tb_sparse_decode_attn_mx(
+        ctypes.byref(desc), q.data_ptr(), K.ref, V.ref, None if idx is None else idx.data_ptr(), None if count is None else count.data_ptr(),
+        0 if idx is None else idx.stride(-2), max_count, tail_begin, tail_end, sm_scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
+        ws.data_ptr(), ws.nbytes, _stream(stream))
+    if rc:
+        _check(rc, "tb_sparse_decode_attn_mx")
 
 
 def tb_sparse_decode_attn_shared_mx(desc, q, K: MxRows, V: MxRows, idx, count, max_count: int, sm_scale: float, out, lse, ws,
                                     tail_begin: int = 0, tail_end: int = 0, stream=None) -> None:
     """idx: int32 [B][idx_cap] (or [B][1][idx_cap]), count: int32 [B]; one list for all heads."""
     assert q.is_contiguous() and out.is_contiguous()
-    _check(load_library().tb_sparse_decode_attn_shared_mx(ctypes.byref(desc), _ptr(q), K.ref, V.ref, _ptr(idx), _ptr(count),
-                                                          0 if idx is None else idx.stride(-2), max_count, tail_begin, tail_end, sm_scale,
-                                                          _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)),
-           "tb_sparse_decode_attn_shared_mx")
+    rc = (_lib or load_library()).tb_sparse_decode_attn_shared_mx(
+        ctypes.byref(desc), q.data_ptr(), K.ref, V.ref, None if idx is None else idx.data_ptr(), None if count is None else count.data_ptr(),
+        0 if idx is None else idx.stride(-2), max_count, tail_begin, tail_end, sm_scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
+        ws.data_ptr(), ws.nbytes, _stream(stream))
+    if rc:
+        _check(rc, "tb_sparse_decode_attn_shared_mx")
 
 
 def policy_count(N: int, k: int, sink: int, window: int) -> int:
