@@ -17,6 +17,7 @@ from gpu_util import DEV, AttnPlan, gpu_select
 from oracle import mx
 from paper_2503_07518_amd import binding as tb
 from paper_2503_07518_amd import interval
+from test_gpu_offload import device_address
 
 pytestmark = pytest.mark.gpu
 
@@ -609,6 +610,90 @@ def test_attention_on_another_stream():
     got = attend(**s, ws=ws, stream=side)
     side.synchronize()
     assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+
+
+def test_attention_on_two_streams_at_once():
+    """Calls that overlap, each on a workspace of its own; some by head, some by KV group."""
+    say("mx attention on two streams at once")
+    s = step(2, 8, 4, 6000, 128, 1500, BF16, 41)
+    dense = dict(q=s["q"], K=s["K"], V=s["V"], N=s["N"], idx=None, cnt=None, max_count=0, tail=(0, s["N"]))
+    ref = [attend(**x) for x in (s, dense)]
+    d = tb.make_mx_desc(s["N"], 32, BF16, K=s["K"])
+    ws = [tb.new_workspace(tb.TB_OP_ATTN_MX, d, s["N"]) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    out = [[(torch.empty_like(ref[0][0]), torch.empty_like(ref[0][1])) for _ in range(40)] for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(40):
+        for w, st in enumerate(streams):
+            x = (s, dense)[(i + w) % 2]
+            tb.tb_sparse_decode_attn_mx(d, x["q"], x["K"], x["V"], x["idx"], x["cnt"], x["max_count"], 128 ** -0.5, *out[w][i], ws[w],
+                                        *x.get("tail", (0, 0)), stream=st)
+    torch.cuda.synchronize()
+    for w in range(2):
+        for i in range(40):
+            want = ref[(i + w) % 2]
+            assert torch.equal(out[w][i][0], want[0]) and torch.equal(out[w][i][1], want[1])
+
+
+def test_two_graphs_share_a_workspace():
+    """Two captured graphs on one workspace, replayed one after the other in either order."""
+    say("mx attention, two graphs on one workspace")
+    s = step(1, 8, 4, 6000, 128, 1500, BF16, 51)
+    dense = dict(q=s["q"], K=s["K"], V=s["V"], idx=None, cnt=None, max_count=0, tail=(3, s["N"]))
+    d = tb.make_mx_desc(s["N"], 32, BF16, K=s["K"])
+    ws = tb.new_workspace(tb.TB_OP_ATTN_MX, d, s["N"])
+    graphs, outs, refs = [], [], []
+    side = torch.cuda.Stream()
+    for x in (s, dense):
+        o = (torch.zeros((1, 32, 128), device=DEV), torch.zeros((1, 32), device=DEV))
+
+        def call():
+            tb.tb_sparse_decode_attn_mx(d, x["q"], x["K"], x["V"], x["idx"], x["cnt"], x["max_count"], 0.09, *o, ws, *x.get("tail", (0, 0)))
+
+        call()
+        torch.cuda.synchronize()
+        refs.append([t.clone() for t in o])
+        g = torch.cuda.CUDAGraph()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(g, stream=side):
+                call()
+        torch.cuda.current_stream().wait_stream(side)
+        graphs.append(g)
+        outs.append(o)
+    for order in ((0, 1), (1, 0), (0, 0, 1, 1), (1, 0, 1)):
+        for o in outs:
+            for t in o:
+                t.fill_(float("nan"))
+        for i in order:
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        for o, r in zip(outs, refs):
+            assert all(torch.equal(a, b) for a, b in zip(o, r)), order
+
+
+def test_cache_in_host_memory():
+    """Codes and scales in pinned host memory, as an offloaded cache has them: written, scored and attended to over the host link."""
+    say("mx cache in pinned host memory")
+    B, Hkv, g, N, D, d, k = 1, 2, 4, 900, 128, 32, 200
+    x = [randn((B, Hkv, N, i), BF16, 60 + i) for i in (D, D + 2, d)]
+    x[1] = x[1][..., :D].contiguous()
+    src = tb.make_desc(N, Hkv * g, K=x[0], V=x[1], Kimp=x[2])
+    q, q_imp = randn((B, Hkv * g, D), F32, 3), randn((B, Hkv * g, d), F32, 4)
+    idx, cnt = lists(B, Hkv * g, N, k, 5)
+    got = []
+    for pinned in (False, True):
+        def rows(inner):
+            return tb.MxRows(*(torch.zeros((B, Hkv, N, n), dtype=torch.uint8, device="cpu" if pinned else DEV, pin_memory=pinned)
+                               for n in (inner // 2, inner // 32)))
+        K, V, Kimp = rows(D), rows(D), rows(d)
+        if pinned and any(device_address(t) != t.data_ptr() for r in (K, V, Kimp) for t in (r.codes, r.scales)):
+            pytest.skip("pinned host memory is not mapped at the same address for the device on this box")
+        tb.tb_quantize_mx(src, *x, 0, K, V, Kimp, 0, N)
+        got.append((score(q_imp, Kimp, N), *attend(q, K, V, N, idx, cnt, k), *attend(q, K, V, N, None, None, 0, (0, N))))
+    torch.cuda.synchronize()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("kind", ["lists", "shared", "dense"])
