@@ -95,10 +95,30 @@ static bool fit_splits(const tb_cache_desc* d, AttnPlan& p, size_t ws_bytes) {
   if (p.nsplit < planned && p.nsplit > p.multiple) p.nsplit -= p.nsplit % p.multiple;
   return ws_bytes >= ws_layout(units, d->D, p.least).total;
 }
-// Rows in 4 bits: a lane takes a block of a row, a tile is kAttnMxLoads rows per lane group.
-static int attn_mx_tile_rows_per_wg(int D) { return kAttnMxWaves * kAttnMxLoads * (64 / (D / 32)); }
+// Rows in 4 bits: a lane takes a block of a row, a tile is kAttnMxLoads rows per lane group.  Splits by a model as attn_plan's, with constants
+// of their own, as a tile holds twice the rows in half the bytes: a start is worth kStart tiles, splitting at all kSplit and
+// every split kHandOver (the hand-over hardly grows with their number), and one workgroup a compute unit does not keep enough loads in flight (kAlone).  D = 128, bf16, us with
+// attn_plan's numbers and now: 8 x 32 heads on 8, 768 rows 11.8 and 9.9 (one split instead of two), 1024 rows 13.1 and 11.3; 32 heads, 512 rows 6.6
+// and 5.7; D = 64, 8 x 32 heads, 2048 rows 14.8 and 12.4.  On 215 shapes of 8 to 700 heads, 30 to 20000 rows 1.4% off the best number tried on
+// average, 17% at most; the constants were chosen on them.
 AttnPlan attn_mx_plan(const tb_cache_desc* d, int64_t max_rows) {
-  return attn_plan(static_cast<int64_t>(d->B) * d->Hq, max_rows, attn_mx_tile_rows_per_wg(d->D), false, false);
+  constexpr double kStart = 2.4, kSplit = 5.0, kHandOver = 0.02, kAlone = 1.4;
+  const int64_t units = static_cast<int64_t>(d->B) * d->Hq, tile = kAttnMxWaves * kAttnMxLoads * (64 / (d->D / 32));
+  if (max_rows <= 0 || units <= 0) return AttnPlan{1, 1, 1, 1};
+  const int64_t most = std::max<int64_t>(1, std::min(max_rows / tile, kAttnMostWgs / units));
+  int64_t want = 1;
+  double least = INFINITY;
+  for (int64_t rounds = 0; rounds * kAttnCus <= kAttnMostWgs; ++rounds) {  // as many splits as these rounds hold
+    const int64_t n = std::min(std::max<int64_t>(1, rounds * kAttnCus / units), most), takes = (units * n + kAttnCus - 1) / kAttnCus;
+    double cost = static_cast<double>(takes) * (static_cast<double>(max_rows) / static_cast<double>(n) + kStart * static_cast<double>(tile));
+    if (takes == 1) cost *= kAlone;
+    if (n > 1) cost += (kSplit + kHandOver * static_cast<double>(n)) * static_cast<double>(tile);
+    if (cost < least) {
+      least = cost;
+      want = n;
+    }
+  }
+  return AttnPlan{static_cast<int>(want), static_cast<int>(most), static_cast<int>(want), 1};
 }
 // One list (or none) for all heads of a KV group: a workgroup per KV group pays where there is enough work, the per-head kernel has the
 // shorter way to the first row and to the end (bf16, D = 128, dense, per head and grouped, us: 8 heads on 1 32768 rows 11.0 and 17.7,
