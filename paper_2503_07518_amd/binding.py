@@ -140,6 +140,20 @@ def _stream(stream=None) -> int:
     return _raw_stream(torch.cuda.current_device())
 
 
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _stream_on(device: int, stream=None) -> int:
+    """The handle of `stream`, or of the current one, for tensors on GPU number `device` (-1: in host memory).  The kernels run on the
+    current device: tensors on another one are refused."""
+    current = _get_device()
+    if device != current and device >= 0:
+        raise ValueError(f"tensors on cuda:{device}, and cuda:{current} is the current device")
+    if stream is not None:
+        return stream.cuda_stream
+    return _stream() if _raw_stream is None else _raw_stream(current)
+
+
 def _dtype_code(dtype: torch.dtype) -> int:
     if dtype == torch.float32:
         return TB_F32
@@ -193,6 +207,7 @@ class MxRows:
         self.codes, self.scales = codes, scales
         self.desc = tb_mx_rows(codes.data_ptr(), scales.data_ptr(), codes.shape[2], *_strides3(codes), *_strides3(scales))
         self.ref = ctypes.byref(self.desc)
+        self.device = codes.get_device()
 
     @property
     def inner(self) -> int:
@@ -389,10 +404,11 @@ def tb_decode_step(desc, q_imp, Kimp, score_scale: float, q, K, V, k: int, sink:
 def tb_quantize_mx(desc, K, V, Kimp, src_row: int, Kq: Optional[MxRows], Vq: Optional[MxRows], Kimpq: Optional[MxRows], dst_row: int,
                    rows: int, stream=None) -> None:
     """Rows src_row + i of K, V and Kimp (desc; None: left out) to rows dst_row + i of Kq, Vq and Kimpq, i < rows."""
+    to = Kq or Vq or Kimpq
     rc = (_lib or load_library()).tb_quantize_mx(
         ctypes.byref(desc), None if K is None else K.data_ptr(), None if V is None else V.data_ptr(),
         None if Kimp is None else Kimp.data_ptr(), src_row, None if Kq is None else Kq.ref, None if Vq is None else Vq.ref,
-        None if Kimpq is None else Kimpq.ref, dst_row, rows, _stream(stream))
+        None if Kimpq is None else Kimpq.ref, dst_row, rows, _stream_on(-1 if to is None else to.device, stream))
     if rc:
         _check(rc, "tb_quantize_mx")
 
@@ -400,10 +416,11 @@ def tb_quantize_mx(desc, K, V, Kimp, src_row: int, Kq: Optional[MxRows], Vq: Opt
 def tb_dequantize_mx(desc, Kq: Optional[MxRows], Vq: Optional[MxRows], Kimpq: Optional[MxRows], src_row: int, K, V, Kimp, dst_row: int,
                      rows: int, stream=None) -> None:
     """The values that rows src_row + i of Kq, Vq and Kimpq stand for to rows dst_row + i of K, V and Kimp (desc), i < rows."""
+    rows_of = Kq or Vq or Kimpq
     rc = (_lib or load_library()).tb_dequantize_mx(
         ctypes.byref(desc), None if Kq is None else Kq.ref, None if Vq is None else Vq.ref, None if Kimpq is None else Kimpq.ref, src_row,
         None if K is None else K.data_ptr(), None if V is None else V.data_ptr(), None if Kimp is None else Kimp.data_ptr(), dst_row, rows,
-        _stream(stream))
+        _stream_on(-1 if rows_of is None else rows_of.device, stream))
     if rc:
         _check(rc, "tb_dequantize_mx")
 
@@ -411,7 +428,7 @@ def tb_dequantize_mx(desc, Kq: Optional[MxRows], Vq: Optional[MxRows], Kimpq: Op
 def tb_score_mx(desc, q_imp, Kimp: MxRows, scale: float, scores, stream=None) -> None:
     assert q_imp.is_contiguous() and scores.stride(-1) == 1
     rc = (_lib or load_library()).tb_score_mx(ctypes.byref(desc), q_imp.data_ptr(), Kimp.ref, scale, scores.data_ptr(), scores.stride(-2),
-                                              _stream(stream))
+                                              _stream_on(scores.get_device(), stream))
     if rc:
         _check(rc, "tb_score_mx")
 
@@ -423,7 +440,7 @@ def tb_sparse_decode_attn_mx(desc, q, K: MxRows, V: MxRows, idx, count, max_coun
     rc = (_lib or load_library()).tb_sparse_decode_attn_mx(
         ctypes.byref(desc), q.data_ptr(), K.ref, V.ref, None if idx is None else idx.data_ptr(), None if count is None else count.data_ptr(),
         0 if idx is None else idx.stride(-2), max_count, tail_begin, tail_end, sm_scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
-        ws.data_ptr(), ws.nbytes, _stream(stream))
+        ws.data_ptr(), ws.nbytes, _stream_on(out.get_device(), stream))
     if rc:
         _check(rc, "tb_sparse_decode_attn_mx")
 
@@ -435,7 +452,7 @@ def tb_sparse_decode_attn_shared_mx(desc, q, K: MxRows, V: MxRows, idx, count, m
     rc = (_lib or load_library()).tb_sparse_decode_attn_shared_mx(
         ctypes.byref(desc), q.data_ptr(), K.ref, V.ref, None if idx is None else idx.data_ptr(), None if count is None else count.data_ptr(),
         0 if idx is None else idx.stride(-2), max_count, tail_begin, tail_end, sm_scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
-        ws.data_ptr(), ws.nbytes, _stream(stream))
+        ws.data_ptr(), ws.nbytes, _stream_on(out.get_device(), stream))
     if rc:
         _check(rc, "tb_sparse_decode_attn_shared_mx")
 

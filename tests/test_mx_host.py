@@ -115,3 +115,22 @@ def test_rows_of_the_binding():
     assert (d.B, d.Hq, d.Hkv, d.D, d.Dimp, d.dtype, d.N) == (2, 12, 3, 128, 64, tb.TB_F32, 40)
     with pytest.raises(AssertionError):
         tb.MxRows(torch.zeros((1, 1, 4, 64), dtype=torch.uint8), torch.zeros((1, 1, 4, 3), dtype=torch.uint8))
+
+
+def test_tensors_on_another_device_are_refused(monkeypatch):
+    monkeypatch.setattr(tb, "_get_device", lambda: 2)
+    monkeypatch.setattr(tb, "_raw_stream", lambda device: 1000 + device)
+
+    class Stream:
+        cuda_stream = 77
+    assert tb._stream_on(2) == tb._stream_on(-1) == 1002 and tb._stream_on(2, Stream) == 77
+    for stream in (None, Stream):
+        with pytest.raises(ValueError):
+            tb._stream_on(0, stream)
+    cache = tb.MxCache(1, 1, 8, 64, 32, device="cpu")
+    cache.K.device = cache.Kimp.device = 1  # (as tensors on cuda:1 have it)
+    x = torch.zeros((1, 1, 8, 64))
+    for call in (lambda: tb.tb_quantize_mx(tb.make_desc(8, 1, K=x, V=x), x, x, None, 0, cache.K, cache.V, None, 0, 8),
+                 lambda: tb.tb_dequantize_mx(tb.make_desc(8, 1, K=x, V=x), cache.K, cache.V, None, 0, x, x, None, 0, 8)):
+        with pytest.raises(ValueError):
+            call()
