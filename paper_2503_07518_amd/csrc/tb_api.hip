@@ -117,6 +117,7 @@ AttnPlan attn_mx_plan(const tb_cache_desc* d, int64_t max_rows) {
       least = cost;
       want = n;
     }
+    if (n == most) break;
   }
   return AttnPlan{static_cast<int>(want), static_cast<int>(most), static_cast<int>(want), 1};
 }
@@ -147,7 +148,7 @@ AttnPlan attn_mx_group_plan(const tb_cache_desc* d, int64_t max_rows) {
     if (cost(n) < cost(want)) want = n;
   };
   // as many splits as a number of rounds holds, or (few groups) as many as their hand-over is worth
-  for (int64_t rounds = 1; rounds <= kRounds; ++rounds) consider(rounds * kAttnCus / groups);
+  for (int64_t rounds = 1; rounds <= kRounds && (rounds - 1) * kAttnCus / groups < most; ++rounds) consider(rounds * kAttnCus / groups);
   consider(static_cast<int64_t>(std::sqrt(static_cast<double>(max_rows) / static_cast<double>(g))));
   return AttnPlan{static_cast<int>(want), static_cast<int>(most), static_cast<int>(want), 1};
 }
