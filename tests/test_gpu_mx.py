@@ -344,6 +344,34 @@ def test_attention_dense(dtype, D, B, Hkv, g, N, tail, shared):
     assert_attention(got, reference(q, Kv, Vv, N, None, None, 0, tail), Vv)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind,B,Hkv,g,N", [("lists", 3, 2, 4, 500), ("lists", 2, 8, 1, 700), ("shared", 13, 8, 8, 250), ("dense", 13, 8, 8, 251)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_attention_strides(dtype, kind, B, Hkv, g, N, D):
+    """One cache for the whole batch (a stride of 0), heads inside rows, scales at odd addresses with odd strides, K and V unlike."""
+    say(f"mx attention, strides, {kind} {dtype} D={D} B={B} Hkv={Hkv} g={g} N={N}")
+    (K1, Kv), (V1, Vv) = coded_rows(1, Hkv, N, D, 1), coded_rows(1, Hkv, N, D, 2)
+    kc = torch.zeros((N, Hkv, D // 2 + 16), dtype=torch.uint8, device=DEV)
+    ks = torch.full((N, Hkv, D // 32 + 1), 255, dtype=torch.uint8, device=DEV)
+    vs = torch.full((Hkv, N, D // 32 + 2), 255, dtype=torch.uint8, device=DEV)
+    kc[..., 16:].copy_(K1.codes[0].transpose(0, 1))
+    ks[..., 1:].copy_(K1.scales[0].transpose(0, 1))
+    vs[..., 1:-1].copy_(V1.scales[0])
+    K = tb.MxRows(kc[..., 16:].transpose(0, 1)[None].expand(B, -1, -1, -1), ks[..., 1:].transpose(0, 1)[None].expand(B, -1, -1, -1))
+    V = tb.MxRows(V1.codes.expand(B, -1, -1, -1), vs[..., 1:-1][None].expand(B, -1, -1, -1))
+    Kv, Vv = (np.broadcast_to(x, (B,) + x.shape[1:]) for x in (Kv, Vv))
+    q = randn((B, Hkv * g, D), dtype, 3)
+    args = (None, None, 0, (1, N))
+    if kind != "dense":
+        k = N - 9 if kind == "shared" else 222
+        idx, cnt = lists(B, 1 if kind == "shared" else Hkv * g, N, k, 4)
+        args = (idx, cnt, k, (N - 9, N))
+    assert mx_plan(q, Hkv, N, kind != "lists")[0] == (kind != "lists")
+    got = attend(q, K, V, N, *args, shared=kind == "shared")
+    torch.cuda.synchronize()
+    assert_attention(got, reference(q, Kv, Vv, N, *args), Vv)
+
+
 # one list or the dense range with enough heads and rows for a workgroup per KV group: B, Hkv, g, rows, splits
 GROUPED = [(200, 8, 8, 16, 1), (850, 8, 2, 15, 1), (410, 8, 2, 31, 1), (60, 8, 4, 111, 1), (13, 8, 8, 250, 1), (6, 8, 8, 527, 2), (2, 4, 4, 6400, 25),
            (1, 8, 8, 3333, 13), (1, 2, 8, 38000, 68)]
