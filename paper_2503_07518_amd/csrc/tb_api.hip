@@ -128,7 +128,7 @@ AttnPlan attn_mx_plan(const tb_cache_desc* d, int64_t max_rows) {
 // 4.9 and 7.1, 1024 8.4 and 7.3): from 200000 rows and heads on, with less than six groups proportionally more.
 bool attn_mx_grouped(const tb_cache_desc* d, int64_t rows) {
   const int64_t groups = static_cast<int64_t>(d->B) * d->Hkv;
-  return d->Hq > d->Hkv && static_cast<int64_t>(d->B) * d->Hq * rows >= 1200000 / std::min<int64_t>(groups, 6);
+  return groups > 0 && d->Hq > d->Hkv && static_cast<int64_t>(d->B) * d->Hq * rows >= 1200000 / std::min<int64_t>(groups, 6);
 }
 // Eight waves of 32 rows a step, one workgroup a compute unit.  As attn_plan, with rounds of whole compute units: a start is worth kStart
 // rows, and every split costs the last workgroup of the group one row a head.  Against one round wherever the groups leave room

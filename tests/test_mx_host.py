@@ -107,6 +107,15 @@ def test_workspace(lib):
     assert tb.tb_workspace_bytes(tb.TB_OP_ATTN_MX, desc(D=96), 10) == 0 and tb.tb_workspace_bytes(tb.TB_OP_ATTN_MX, d, -1) == 0
 
 
+@pytest.mark.parametrize("kw", [dict(B=0), dict(Hq=0), dict(Hq=0, Hkv=0), dict(B=0, Hq=0, Hkv=0)])
+def test_workspace_of_an_empty_batch(lib, kw):
+    """(KV heads without a query head are a grouping that no entry point supports)"""
+    for n in (0, 1, 100, 1 << 20):
+        assert tb.tb_workspace_bytes(tb.TB_OP_ATTN_MX, desc(**kw), n) == tb.tb_workspace_bytes(tb.TB_OP_ATTN_MX, desc(**kw), 0)
+    assert lib.tb_sparse_decode_attn_mx(ref(desc(**kw)), P, ref(rows()), ref(rows()), P, P, 100, 100, 0, 0, 1.0, P, None, None, 0, None) == (
+        UNS if kw == dict(Hq=0) else tb.TB_OK)
+
+
 def test_rows_of_the_binding():
     cache = tb.MxCache(2, 3, 50, 128, 64, device="cpu")
     assert cache.K.inner == cache.V.inner == 128 and cache.Kimp.inner == 64
