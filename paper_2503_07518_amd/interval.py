@@ -144,7 +144,8 @@ class MxIntervalDecoder:
         self.exp_cnt = torch.zeros((B, Hl), dtype=torch.int32, device=dev)
         self.out = torch.empty((B, Hq, self.D), dtype=torch.float32, device=dev)
         self.lse = torch.empty((B, Hq), dtype=torch.float32, device=dev)
-        self.ws = tb.new_workspace(tb.TB_OP_ATTN_MX, tb.make_mx_desc(self.Ncap, Hq, dtype, K=cache.K), max(self.exp_cap + P, self.sel_cap))
+        # (any number of rows may be appended between two predictions)
+        self.ws = tb.new_workspace(tb.TB_OP_ATTN_MX, tb.make_mx_desc(self.Ncap, Hq, dtype, K=cache.K), max(self.exp_cap + self.Ncap, self.sel_cap))
         self.sel_ws = tb.new_workspace(tb.TB_OP_SELECT, tb.make_mx_desc(self.Ncap, Hl, dtype, Kimp=cache.Kimp), self.sel_cap)
         if not headless:
             self.waiting = torch.empty((B, self.Hkv, P, self.D), dtype=dtype, device=dev)  # keys not projected yet
@@ -170,6 +171,8 @@ class MxIntervalDecoder:
     def append(self, K: torch.Tensor, V: torch.Tensor) -> None:
         """K, V: [B, Hkv, n, D], the next n rows."""
         n = K.shape[2]
+        if n == 0:
+            return
         assert K.shape == V.shape == (self.B, self.Hkv, n, self.D) and K.dtype == V.dtype == self.dtype
         if self.N + n > self.Ncap:
             raise ValueError(f"{self.N} + {n} rows in a cache for {self.Ncap}")

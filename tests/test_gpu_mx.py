@@ -836,3 +836,30 @@ def test_interval_loop(oracle, monkeypatch, dtype, headless, mode, expand):
         assert_attention((out, lse), ref, Vv)
     with pytest.raises(ValueError):
         loop.append(K, V)
+
+
+@pytest.mark.parametrize("headless", [False, True])
+def test_interval_loop_many_rows_between_predictions(headless):
+    """More rows than P, and none at all, between two predictions: a conversation goes on with a prompt."""
+    say(f"mx interval loop, many rows between predictions, headless={headless}")
+    B, Hkv, g, D, d, N0, N1, k, P, radius = 1, 2, 2, 64, 32, 300, 5000, 40, 4, 1
+    Hq = Hkv * g
+    K, V = randn((B, Hkv, N1, D), BF16, 1), randn((B, Hkv, N1, D), BF16, 2)
+    cache = tb.MxCache(B, Hkv, N1, D, 0 if headless else d)
+    if headless:
+        one = randn((B, 1, N1, d), BF16, 4)
+        cache.Kimp = tb.MxCache(B, 1, N1, D, d).Kimp
+        tb.tb_quantize_mx(tb.make_desc(N1, 1, Kimp=one), None, None, one, 0, None, None, cache.Kimp, 0, N1)
+    loop = interval.MxIntervalDecoder(cache, None if headless else randn((1, D, d), BF16, 3, D ** -0.5), Hq, k, P, radius, sm_scale=D ** -0.5,
+                                      headless=headless)
+    Kv, Vv = (mx.dequantize(*mx.quantize(x.float().cpu().numpy())) for x in (K, V))
+    have = 0
+    for t, N in enumerate((N0, N0 + 1, N0 + 1, N1, N1)):
+        loop.append(K[:, :, have:N], V[:, :, have:N])
+        have = N
+        q, q_imp = randn((B, Hq, D), BF16, 100 + t), randn((B, 1 if headless else Hq, d), BF16, 200 + t)
+        got = loop.step(t, q, q_imp)
+        torch.cuda.synchronize()
+        assert loop.N == N
+        args = (loop.idx, loop.cnt, loop.sel_cap) if t % P == 0 else (loop.exp_idx, loop.exp_cnt, loop.exp_cap, (N0, N))
+        assert_attention(got, reference(q, Kv, Vv, N, *args), Vv)
