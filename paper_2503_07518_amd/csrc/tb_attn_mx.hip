@@ -40,8 +40,9 @@ struct AttnMxArgs {
   int32_t shared_list;
 };
 
-// The reference of a running softmax moves when a score is 2^kMxLazy above it, not with every new maximum: weights up to that are as exact in
-// fp32, and sums are seldom rescaled.
+// The reference of a running softmax is put 2^kMxLazy above the largest score and moves when a score is above it, not with every new
+// maximum: sums are seldom rescaled.  No weight is above 1, so that sums pass fp32's largest number no sooner than with the maximum itself
+// as the reference; at the other end what is below 2^-118 of the largest weight may count as nothing, instead of below 2^-126.
 constexpr float kMxLazy = 8.f;
 constexpr int kGroupMxWaves = kAttnGroupWaves;
 constexpr int kMxLoads = kAttnMxLoads;  // rows per lane group and tile
@@ -278,8 +279,8 @@ __global__ __launch_bounds__(NW * kWave, kMxWavesPerSimd<T>) void attn_mx_kernel
     }
 #pragma unroll
     for (int t = 0; t < kMxLoads; ++t) tmax = fmaxf(tmax, sc[t]);
-    if (__any(tmax > m + kMxLazy)) {
-      const float m_new = fmaxf(m, tmax);
+    if (__any(tmax > m)) {
+      const float m_new = tmax > m ? tmax + kMxLazy : m;
       const float alpha = m_new > -INFINITY ? exp2_safe(m - m_new) : 0.f;
       l *= alpha;
 #pragma unroll
@@ -540,8 +541,8 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
       for (int v = 0; v < 4; ++v) smax = fmaxf(smax, s[t][v]);
     smax = half_max<32>(half_max<16>(smax));
     smax *= scale;
-    if (__any(smax > m + kMxLazy)) {
-      const float m_new = fmaxf(m, smax);
+    if (__any(smax > m)) {
+      const float m_new = smax > m ? smax + kMxLazy : m;
       const float alpha = m_new > -INFINITY ? exp2_safe(m - m_new) : 0.f;
       l *= alpha;
 #pragma unroll

@@ -1,0 +1,76 @@
+"""The 4-bit cache at the ends of what fp32 holds, and where the softmax's reference has to follow the scores through every grouping.
+
+Logits rise along the rows by amounts that the reference of a running softmax may lag behind, so that it moves several times in every
+wave with accumulators that hold something.  Bar: a logit is off by at most D roundings of its fp32 sum and four of the scale and the
+exponential's argument, (D + 4) 2^-24 sum |q k| sm_scale; a weight by that share of itself, the mean of V by twice that of the largest
+|V|; the sums of weights and rows by 1e-5 of it (160 roundings; a lane adds up at most 60 rows, and ten sums meet at the end)."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import DEV
+from paper_2503_07518_amd import binding as tb
+from test_gpu_mx import BF16, F32, attend, mx_plan, mx_rows, reference, say
+
+pytestmark = pytest.mark.gpu
+
+ROWS = 2800
+RISE = 60.0  # from the first to the last row's logit, in powers of two
+
+
+def rising(dtype, B, Hkv, g, D, byte, seed):
+    """Rows whose logits rise for every head: element i of row n is the sign of the head's query there for i below D n / ROWS, its opposite
+    from there on.  V: values above zero under one scale.  One cache for the whole batch; four different queries of it."""
+    rng = np.random.default_rng(seed)
+    sign = rng.choice([-1.0, 1.0], (Hkv, 1, D))
+    z = np.abs(rng.standard_normal((4, Hkv, g, D))) + 0.2
+    z *= RISE / 2 * np.log(2) / (z.sum(-1, keepdims=True) * D ** -0.5)
+    q = torch.from_numpy((sign * z).reshape(4, Hkv * g, D)).to(dtype).repeat(B // 4, 1, 1).to(DEV)
+    turned = np.arange(D)[None] < (np.arange(ROWS) * D / ROWS)[:, None]
+    K, Kv = mx_rows((np.where(turned, 1.0, -1.0) * sign)[None])
+    codes = torch.from_numpy(rng.integers(1, 8, (1, Hkv, ROWS, D // 2, 2)).astype(np.uint8))
+    V = tb.MxRows((codes[..., 0] | codes[..., 1] << 4).to(DEV), torch.full((1, Hkv, ROWS, D // 32), byte, dtype=torch.uint8, device=DEV))
+    Vv = np.array([0, .5, 1, 1.5, 2, 3, 4, 6])[codes.numpy()].reshape(1, Hkv, ROWS, D) * 2.0 ** (byte - 127)
+
+    def whole_batch(r):
+        return tb.MxRows(r.codes.expand(B, -1, -1, -1), r.scales.expand(B, -1, -1, -1))
+
+    return q, whole_batch(K), whole_batch(V), Kv, Vv
+
+
+def check(dtype, D, g, kind, byte):
+    B, Hkv = (64, 4) if kind != "lists" else (128, 4) if g == 1 else (64, 2)
+    q, K, V, Kv, Vv = rising(dtype, B, Hkv, g, D, byte, 10 * g + D)
+    heads = {"lists": Hkv * g, "shared": 1, "dense": 0}[kind]
+    args = (None, None, 0, (0, ROWS))
+    if heads:
+        args = (torch.arange(ROWS, dtype=torch.int32, device=DEV).expand(B, heads, -1).contiguous(),
+                torch.full((B, heads), ROWS, dtype=torch.int32, device=DEV), ROWS, (0, 0))
+    by_group, splits = mx_plan(q, Hkv, ROWS, kind != "lists")
+    assert by_group == (kind != "lists")
+    step = splits * (256 if by_group else 128 * 128 // D)  # rows from a wave's tile to its next one
+    assert RISE * step / ROWS < 8, "every step passes the reference's lag at once"
+    out, lse = (t.cpu().numpy() for t in attend(q, K, V, ROWS, *args, shared=kind == "shared"))
+    for b in range(4, B):
+        assert np.array_equal(out[b], out[b % 4]) and np.array_equal(lse[b], lse[b % 4])
+    Kv, Vv = (np.broadcast_to(x, (4,) + x.shape[1:]) for x in (Kv, Vv))
+    few = args if not heads else (args[0][:4], args[1][:4], *args[2:])
+    ref = reference(q[:4], Kv, Vv, ROWS, *few)
+    assert np.exp(ref[1]).max() < 2.0 ** (RISE / 2 + 8), "the weights, of which the largest is 1, add up to less than 2^8"
+    bar = 2 * (D + 4) * 2.0 ** -24 * (np.abs(q[:4].float().cpu().numpy()).sum(-1).max() * D ** -0.5) + 1e-5
+    assert bool(np.isfinite(out).all())
+    assert np.abs(out[:4] - ref[0]).max() <= bar * Vv.max()
+    assert np.abs(lse[:4] - ref[1]).max() <= bar * np.abs(ref[1]).max()
+
+
+KINDS = [("lists", 1), ("lists", 4), ("lists", 8), ("shared", 2), ("shared", 4), ("shared", 8), ("dense", 2), ("dense", 4), ("dense", 8)]
+
+
+@pytest.mark.parametrize("kind,g", KINDS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rising_logits_of_large_values(dtype, D, kind, g):
+    """V of up to 6 * 2^117: times a sum of weights below 2^8, of which the largest is 1, less than 2^127.6.  With weights that are 2^4 times as
+    large the sums would be infinite (some 80 rows count, the mean of V is 2.6 * 2^117)."""
+    say(f"mx attention, rising logits, V near 2^120, {kind} {dtype} D={D} g={g}")
+    check(dtype, D, g, kind, 244)
