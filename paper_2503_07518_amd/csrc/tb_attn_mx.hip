@@ -412,8 +412,8 @@ __global__ __launch_bounds__(kGroupMxWaves * kWave, 2) void attn_group_mx_kernel
   }
 
   // (a negative scale's sign goes to the query, so that the largest score is the largest dot product)
-  // (and none is so small that minus infinity times it is not minus infinity)
-  const float scale = a.sm_scale_log2 == 0.f ? 1.17549435e-38f : fabsf(a.sm_scale_log2);
+  // (none at all is the smallest number there is: minus infinity times it is minus infinity, and any product of a query and a row is below 2^-20)
+  const float scale = a.sm_scale_log2 == 0.f ? 1.40129846e-45f : fabsf(a.sm_scale_log2);
   const uint32_t sign = __float_as_uint(a.sm_scale_log2) >> 31 << 15;
   mx_s16x8 qop[QP][KW];
 #pragma unroll

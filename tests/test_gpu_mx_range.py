@@ -9,8 +9,9 @@ import pytest
 import torch
 
 from gpu_util import DEV
+from oracle import mx
 from paper_2503_07518_amd import binding as tb
-from test_gpu_mx import BF16, F32, attend, mx_plan, mx_rows, reference, say
+from test_gpu_mx import BF16, F32, assert_attention, attend, coded_rows, mx_plan, mx_rows, randn, reference, say
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +75,29 @@ def test_rising_logits_of_large_values(dtype, D, kind, g):
     large the sums would be infinite (some 80 rows count, the mean of V is 2.6 * 2^117)."""
     say(f"mx attention, rising logits, V near 2^120, {kind} {dtype} D={D} g={g}")
     check(dtype, D, g, kind, 244)
+
+
+@pytest.mark.parametrize("kind,g", KINDS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_no_scale_and_large_products(dtype, kind, g):
+    """sm_scale = 0 is the mean of the rows however large the products of queries and keys are (up to 2^126 here)."""
+    say(f"mx attention, sm_scale=0, products near 2^126, {kind} {dtype} g={g}")
+    B, Hkv, D, N = 13, 8, 128, 1200
+    (K, Kv), (V, Vv) = coded_rows(1, Hkv, N, D, 1), coded_rows(1, Hkv, N, D, 2)
+    K.scales.fill_(127 + 113)
+    q = randn((B, Hkv * g, D), dtype, 3, 2.0 ** 6)
+    codes = mx.dequantize(K.codes.cpu().numpy(), K.scales.cpu().numpy())[0]
+    dots = np.abs(codes[:, None] @ q.float().cpu().numpy().reshape(B, Hkv, g, D).astype(np.float64).transpose(1, 0, 3, 2))
+    assert 2.0 ** 125 < dots.max() < 2.0 ** 127
+    whole = [tb.MxRows(r.codes.expand(B, -1, -1, -1), r.scales.expand(B, -1, -1, -1)) for r in (K, V)]
+    heads = {"lists": Hkv * g, "shared": 1, "dense": 0}[kind]
+    rows = N - 7
+    args = (None, None, 0, (7, N))
+    if heads:
+        args = (torch.arange(7, N, dtype=torch.int32, device=DEV).expand(B, heads, -1).contiguous(),
+                torch.full((B, heads), rows, dtype=torch.int32, device=DEV), rows, (0, 0))
+    assert mx_plan(q, Hkv, rows, kind != "lists")[0] == (kind != "lists")
+    for sm in (0.0, -0.0):
+        got = attend(q, *whole, N, *args, sm=sm, shared=kind == "shared")
+        mean = np.repeat(Vv[:, :, 7:].mean(2), g, 1)
+        assert_attention(got, (np.broadcast_to(mean, (B, Hkv * g, D)), np.full((B, Hkv * g), np.log(rows))), Vv)
