@@ -115,10 +115,11 @@ class MxIntervalDecoder:
     """The interval loop over a cache in microscaled 4-bit floating point (``binding.MxCache``): K, V and the projected keys are held in
     that form alone.
 
-    ``append`` takes the rows of a prompt, or of one step, in the model's element type: K and V go into the cache at once, the keys are
-    projected by ``W`` in that type before they are rounded to 4 bits -- a prompt's at once, the rows of single steps together on the next
-    prediction step (until then at most ``P`` of them wait).  ``step`` attends over all rows appended so far, as
-    ``IntervalDecoder.step`` does: selected rows on prediction steps, then the widened list and the rows since.
+    ``append`` takes the rows of a prompt, or of one step, in the model's element type (``dtype``, the one of ``W`` and the queries, too):
+    K and V go into the cache at once, the keys are projected by ``W`` in that type before they are rounded to 4 bits -- a prompt's at
+    once, the rows of single steps together on the next prediction step (until then at most ``P`` of them wait).  ``step`` attends over
+    all rows appended so far, as ``IntervalDecoder.step`` does: selected rows on prediction steps, then the widened list and the rows
+    since.
 
     With ``headless=True`` there is one importance head: the cache's ``Kimp`` has one head, which the caller keeps up to date
     (``tb_quantize_mx``), ``W`` is not used (None), and one list per batch element serves every head.
@@ -134,6 +135,7 @@ class MxIntervalDecoder:
         self.B, self.Hkv, self.Ncap = cache.K.codes.shape[:3]
         self.D, dev = cache.K.inner, cache.K.codes.device
         assert cache.Kimp is not None and cache.Kimp.codes.shape[1] == (1 if headless else self.Hkv)
+        assert headless or (W.dtype == dtype and W.dim() == 3 and W.shape[1:] == (self.D, cache.Kimp.inner))
         B, Hl = self.B, 1 if headless else Hq  # heads that carry a list of their own
         self.sel_cap = sink + k + window
         self.exp_cap = min(self.Ncap, ((2 * radius + 1) if mode == 0 else 2) * self.sel_cap)
@@ -190,6 +192,8 @@ class MxIntervalDecoder:
     def step(self, t: int, q: torch.Tensor, q_imp: torch.Tensor):
         """Step t over the rows appended so far.  Returns (out, lse) views valid until the next call."""
         c, N = self.cache, self.N
+        assert q.dtype == q_imp.dtype == self.dtype
+        assert q.shape == (self.B, self.Hq, self.D) and q_imp.shape == (self.B, self.idx.shape[1], c.Kimp.inner)
         attend = tb.tb_sparse_decode_attn_shared_mx if self.headless else tb.tb_sparse_decode_attn_mx
         desc = tb.make_mx_desc(N, self.Hq, self.dtype, K=c.K)
         if t % self.P == 0:
