@@ -109,6 +109,8 @@ def load_library() -> ctypes.CDLL:
     for name in EXPORTS:
         if name not in ("tb_workspace_bytes", "tb_status_string", "tb_version"):
             getattr(L, name).restype = ctypes.c_int
+    global _several_devices
+    _several_devices = torch.cuda.device_count() != 1
     _lib = L
     return L
 
@@ -141,14 +143,20 @@ def _stream(stream=None) -> int:
 
 
 _get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_several_devices = True  # (set when the library is loaded: with one GPU no tensor is on another, and up to 0.8 us a call are saved)
 
 
-def _stream_on(device: int, stream=None) -> int:
-    """The handle of `stream`, or of the current one, for tensors on GPU number `device` (-1: in host memory).  The kernels run on the
-    current device: tensors on another one are refused."""
+def _stream_on(device: int, stream=None, also=()) -> int:
+    """The handle of `stream`, or of the current one, for tensors on GPU number `device` (-1: in host memory) and those in `also` (None:
+    left out).  The kernels run on the current device: tensors on another one are refused."""
     current = _get_device()
     if device != current and device >= 0:
         raise ValueError(f"tensors on cuda:{device}, and cuda:{current} is the current device")
+    for t in also:
+        if t is not None:
+            device = t.get_device()
+            if device != current and device >= 0:
+                raise ValueError(f"tensors on cuda:{device}, and cuda:{current} is the current device")
     if stream is not None:
         return stream.cuda_stream
     return _stream() if _raw_stream is None else _raw_stream(current)
@@ -207,7 +215,14 @@ class MxRows:
         self.codes, self.scales = codes, scales
         self.desc = tb_mx_rows(codes.data_ptr(), scales.data_ptr(), codes.shape[2], *_strides3(codes), *_strides3(scales))
         self.ref = ctypes.byref(self.desc)
-        self.device = codes.get_device()
+        on = (codes.get_device(), scales.get_device())
+        self.device = max(on)
+        if -1 not in on and on[0] != on[1]:
+            raise ValueError(f"codes on cuda:{on[0]}, scales on cuda:{on[1]}")
+
+    def get_device(self) -> int:
+        """The GPU that the rows are on (-1: in host memory)."""
+        return self.device
 
     @property
     def inner(self) -> int:
@@ -408,7 +423,8 @@ def tb_quantize_mx(desc, K, V, Kimp, src_row: int, Kq: Optional[MxRows], Vq: Opt
     rc = (_lib or load_library()).tb_quantize_mx(
         ctypes.byref(desc), None if K is None else K.data_ptr(), None if V is None else V.data_ptr(),
         None if Kimp is None else Kimp.data_ptr(), src_row, None if Kq is None else Kq.ref, None if Vq is None else Vq.ref,
-        None if Kimpq is None else Kimpq.ref, dst_row, rows, _stream_on(-1 if to is None else to.device, stream))
+        None if Kimpq is None else Kimpq.ref, dst_row, rows, _stream_on(
+            -1 if to is None else to.device, stream, (K, V, Kimp, Vq, Kimpq) if _several_devices else ()))
     if rc:
         _check(rc, "tb_quantize_mx")
 
@@ -420,7 +436,7 @@ def tb_dequantize_mx(desc, Kq: Optional[MxRows], Vq: Optional[MxRows], Kimpq: Op
     rc = (_lib or load_library()).tb_dequantize_mx(
         ctypes.byref(desc), None if Kq is None else Kq.ref, None if Vq is None else Vq.ref, None if Kimpq is None else Kimpq.ref, src_row,
         None if K is None else K.data_ptr(), None if V is None else V.data_ptr(), None if Kimp is None else Kimp.data_ptr(), dst_row, rows,
-        _stream_on(-1 if rows_of is None else rows_of.device, stream))
+        _stream_on(-1 if rows_of is None else rows_of.device, stream, (K, V, Kimp, Vq, Kimpq) if _several_devices else ()))
     if rc:
         _check(rc, "tb_dequantize_mx")
 
@@ -428,7 +444,7 @@ def tb_dequantize_mx(desc, Kq: Optional[MxRows], Vq: Optional[MxRows], Kimpq: Op
 def tb_score_mx(desc, q_imp, Kimp: MxRows, scale: float, scores, stream=None) -> None:
     assert q_imp.is_contiguous() and scores.stride(-1) == 1
     rc = (_lib or load_library()).tb_score_mx(ctypes.byref(desc), q_imp.data_ptr(), Kimp.ref, scale, scores.data_ptr(), scores.stride(-2),
-                                              _stream_on(scores.get_device(), stream))
+                                              _stream_on(scores.get_device(), stream, (q_imp, Kimp) if _several_devices else ()))
     if rc:
         _check(rc, "tb_score_mx")
 
@@ -440,7 +456,7 @@ def tb_sparse_decode_attn_mx(desc, q, K: MxRows, V: MxRows, idx, count, max_coun
     rc = (_lib or load_library()).tb_sparse_decode_attn_mx(
         ctypes.byref(desc), q.data_ptr(), K.ref, V.ref, None if idx is None else idx.data_ptr(), None if count is None else count.data_ptr(),
         0 if idx is None else idx.stride(-2), max_count, tail_begin, tail_end, sm_scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
-        ws.data_ptr(), ws.nbytes, _stream_on(out.get_device(), stream))
+        ws.data_ptr(), ws.nbytes, _stream_on(out.get_device(), stream, (q, K, V, idx, count, lse, ws) if _several_devices else ()))
     if rc:
         _check(rc, "tb_sparse_decode_attn_mx")
 
@@ -452,7 +468,7 @@ def tb_sparse_decode_attn_shared_mx(desc, q, K: MxRows, V: MxRows, idx, count, m
     rc = (_lib or load_library()).tb_sparse_decode_attn_shared_mx(
         ctypes.byref(desc), q.data_ptr(), K.ref, V.ref, None if idx is None else idx.data_ptr(), None if count is None else count.data_ptr(),
         0 if idx is None else idx.stride(-2), max_count, tail_begin, tail_end, sm_scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
-        ws.data_ptr(), ws.nbytes, _stream_on(out.get_device(), stream))
+        ws.data_ptr(), ws.nbytes, _stream_on(out.get_device(), stream, (q, K, V, idx, count, lse, ws) if _several_devices else ()))
     if rc:
         _check(rc, "tb_sparse_decode_attn_shared_mx")
 
