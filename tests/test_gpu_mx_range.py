@@ -11,7 +11,7 @@ import torch
 from gpu_util import DEV
 from oracle import mx
 from paper_2503_07518_amd import binding as tb
-from test_gpu_mx import BF16, F32, assert_attention, attend, coded_rows, mx_plan, mx_rows, randn, reference, say
+from test_gpu_mx import BF16, F32, assert_attention, attend, coded_rows, mx_plan, mx_rows, randn, reference, say, score
 
 pytestmark = pytest.mark.gpu
 
@@ -101,3 +101,65 @@ def test_no_scale_and_large_products(dtype, kind, g):
         got = attend(q, *whole, N, *args, sm=sm, shared=kind == "shared")
         mean = np.repeat(Vv[:, :, 7:].mean(2), g, 1)
         assert_attention(got, (np.broadcast_to(mean, (B, Hkv * g, D)), np.full((B, Hkv * g), np.log(rows))), Vv)
+
+
+def strange_queries(dtype, B, Hkv, g, D, rows):
+    """Queries, most of them ordinary, and rows in whose columns 3 and 40 there is no zero: column 3 has both signs, column 40 is below zero."""
+    K, _ = coded_rows(B, Hkv, rows, D, 1)
+    codes = K.codes
+    codes[..., 1] = (codes[..., 1] & 0x0F) | 0x10 | (codes[..., 1] & 0xE0)   # element 3, the high half of byte 1: no zero
+    codes[..., 20] = codes[..., 20] & 0xF0 | 0x09 | codes[..., 20] & 0x06     # element 40, the low half of byte 20: a sign, no zero
+    q = randn((B, Hkv * g, D), dtype, 3, 0.5)
+    heads = q.view(B, Hkv, g, D)
+    heads[0, 0, 0, 3] = np.inf          # scores of both infinities: NaN
+    heads[0, Hkv - 1, g - 1, 5] = np.nan
+    heads[B - 1, 0, g - 1, 40] = np.inf   # minus infinity alone: as an empty list
+    heads[B - 1, Hkv - 1, 0, 40] = -np.inf  # plus infinity alone: NaN
+    return q, K, mx.dequantize(K.codes.cpu().numpy(), K.scales.cpu().numpy())
+
+
+@pytest.mark.parametrize("kind,g", KINDS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_infinite_and_nan_queries(dtype, D, kind, g):
+    """What the formula makes of them, in their own head alone."""
+    say(f"mx attention, infinite and NaN queries, {kind} {dtype} D={D} g={g}")
+    B, Hkv, rows = 13, 8, 1200
+    q, K, Kv = strange_queries(dtype, B, Hkv, g, D, rows)
+    V, Vv = coded_rows(B, Hkv, rows, D, 2)
+    heads = {"lists": Hkv * g, "shared": 1, "dense": 0}[kind]
+    args = (None, None, 0, (0, rows))
+    if heads:
+        args = (torch.arange(rows, dtype=torch.int32, device=DEV).expand(B, heads, -1).contiguous(),
+                torch.full((B, heads), rows, dtype=torch.int32, device=DEV), rows, (0, 0))
+    assert mx_plan(q, Hkv, rows, kind != "lists")[0] == (kind != "lists")
+    got = attend(q, K, V, rows, *args, shared=kind == "shared")
+    with np.errstate(invalid="ignore"):
+        ref = reference(q, Kv, Vv, rows, *args)
+    empty = (B - 1, g - 1)
+    assert np.isnan(ref[0][empty]).all()
+    ref[0][empty], ref[1][empty] = 0.0, -np.inf
+    strange = [(0, 0), (0, Hkv * g - 1), (B - 1, (Hkv - 1) * g)]
+    assert np.isnan(ref[1]).sum() == len(set(strange)) and all(np.isnan(ref[0][at]).all() for at in strange)
+    assert_attention(got, ref, Vv)
+
+
+@pytest.mark.parametrize("g", [1, 2, 4, 8])
+@pytest.mark.parametrize("d", [32, 64])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scores_of_infinite_and_nan_queries(dtype, d, g):
+    say(f"mx score, infinite and NaN queries, {dtype} d'={d} g={g}")
+    B, Hkv, N = 2, 2, 700
+    K, Kv = coded_rows(B, Hkv, N, d, 1)
+    q = randn((B, Hkv * g, d), dtype, 3)
+    q[0, 0, 3], q[1, 0, 7], q[1, -1, 0] = np.inf, -np.inf, np.nan
+    q[0, -1, 5] = 3e38 if dtype == F32 else 2.0 ** 127
+    got = score(q, K, N).cpu().numpy()[..., :N]
+    with np.errstate(invalid="ignore"):
+        ref = np.einsum("bkgd,bknd->bkgn", q.float().cpu().numpy().astype(np.float64).reshape(B, Hkv, g, d), Kv).reshape(B, Hkv * g, N)
+    assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.isnan(ref).sum() > N and np.isinf(ref).sum() > N
+    assert np.array_equal(got[np.isinf(ref)], ref[np.isinf(ref)])
+    fin = np.isfinite(ref) & (np.abs(ref) < 3.4e38)
+    mag = np.einsum("bkgd,bknd->bkgn", np.abs(np.nan_to_num(q.float().cpu().numpy().astype(np.float64), posinf=0, neginf=0)).reshape(B, Hkv, g, d),
+                    np.abs(Kv)).reshape(ref.shape)
+    assert (np.abs(got[fin] - ref[fin]) <= (3 * d + 2) * 2.0 ** -24 * mag[fin]).all()
