@@ -121,7 +121,7 @@ __device__ __forceinline__ void merge_waves(const float (*s_m)[1], const float (
 }
 
 // Whether a sum of weights has anything to be divided by: none of an empty list.  NAN_STAYS: a sum that is NaN has, its row becomes NaN
-// (the caches in 4 bits have no infinities, only rows that stand for NaN; without, such a row counts as empty).
+// (of rows in 4 bits, which are finite or stand for NaN as the library writes them; without, such a row counts as empty).
 template <bool NAN_STAYS>
 __device__ __forceinline__ bool has_weight(const float l) {
   return NAN_STAYS ? !(l <= 0.f) : l > 0.f;

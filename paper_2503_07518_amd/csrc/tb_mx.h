@@ -26,7 +26,7 @@ __device__ __forceinline__ void mx_to_f32(const uint32_t word, const float scale
   lo = v.x;
   hi = v.y;
 }
-// ... as two bf16 numbers (exact: two significant bits, the exponent range of fp32).
+// ... as two bf16 numbers (exact: two significant bits, the exponent range of fp32; what is beyond it, under bytes 253 and 254, is an infinity).
 template <int PAIR>
 __device__ __forceinline__ uint32_t mx_to_bf16(const uint32_t word, const float scale) {
   const mx_bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, PAIR);

@@ -163,3 +163,19 @@ def test_scores_of_infinite_and_nan_queries(dtype, d, g):
     mag = np.einsum("bkgd,bknd->bkgn", np.abs(np.nan_to_num(q.float().cpu().numpy().astype(np.float64), posinf=0, neginf=0)).reshape(B, Hkv, g, d),
                     np.abs(Kv)).reshape(ref.shape)
     assert (np.abs(got[fin] - ref[fin]) <= (3 * d + 2) * 2.0 ** -24 * mag[fin]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_every_code_under_every_scale(dtype):
+    """Bytes 253 and 254, which the library does not write, have codes beyond the largest number of either type: infinities."""
+    say(f"mx, every code under every scale byte, {dtype}")
+    codes = torch.arange(256, dtype=torch.uint8).view(16, 16).repeat(256, 1).reshape(1, 16, 256, 16).contiguous()
+    scales = torch.arange(256, dtype=torch.uint8).repeat_interleave(16).reshape(1, 16, 256, 1).contiguous()
+    rows = tb.MxRows(codes.repeat(1, 1, 1, 2).to(DEV), scales.repeat(1, 1, 1, 2).to(DEV))
+    out = torch.zeros((1, 16, 256, 64), dtype=dtype, device=DEV)
+    tb.tb_dequantize_mx(tb.make_desc(256, 16, K=out), rows, None, None, 0, out, None, None, 0, 256)
+    got = out.float().cpu().numpy()
+    with np.errstate(over="ignore"):
+        want = mx.dequantize(rows.codes.cpu().numpy(), rows.scales.cpu().numpy()).astype(np.float32)
+    assert np.array_equal(got, want, equal_nan=True)
+    assert np.isinf(want).any(axis=-1).reshape(256, 16).any(1).nonzero()[0].tolist() == [253, 254]
