@@ -295,8 +295,8 @@ tb_status tb_sparse_decode_attn_shared_mx(const tb_cache_desc* desc, const void*
  * attention will see, tail included; for TB_OP_SELECT and TB_OP_DECODE_STEP it is the list
  * length the selection policy produces, lo + kk + N - hi (TB_OP_SELECT returns 0 for every
  * shape whose rows are selected by one workgroup each).  Returns 0 on invalid
- * input.  A workspace of the TB_OP_DECODE_STEP size serves all three operations on that
- * shape, and a workspace of any of the sizes serves fewer rows and shorter lists as well: make it
+ * input.  A workspace of the TB_OP_DECODE_STEP size serves TB_OP_SELECT and TB_OP_ATTN on that
+ * shape, too, and a workspace of any of the sizes serves fewer rows and shorter lists as well: make it
  * for a cache's capacity.  The workspace pointer must be 16-byte aligned. */
 size_t tb_workspace_bytes(int32_t op, const tb_cache_desc* desc, int64_t max_count);
 

@@ -483,9 +483,9 @@ tb_status sparse_attn_mx(const tb_cache_desc* d, const void* q, const tb_mx_rows
   if (units == 0) return TB_OK;
   const int64_t rows = max_count + (tail_end - tail_begin);
   const bool grouped = (shared_list || max_count == 0) && attn_mx_grouped(d, rows);
-  AttnPlan plan = grouped ? attn_mx_group_plan(d, rows) : attn_mx_plan(d, rows);
-  if (!ws || !aligned16(ws) || !fit_splits(d, plan, ws_bytes)) return TB_ERR_WORKSPACE;
-  const WsLayout w = ws_layout(units, d->D, plan.nsplit);
+  const AttnPlan plan = grouped ? attn_mx_group_plan(d, rows) : attn_mx_plan(d, rows);
+  const WsLayout w = ws_layout(units, d->D, plan.nsplit);  // (a workspace made for fewer splits is refused)
+  if (!ws || !aligned16(ws) || ws_bytes < w.total) return TB_ERR_WORKSPACE;
   const AttnMxLaunch L{d, q, K, V, idx, count, idx_cap, max_count, tail_begin, tail_end, sm_scale, out, lse,
                        reinterpret_cast<float*>(static_cast<char*>(ws) + w.part_off), reinterpret_cast<uint32_t*>(ws), plan, shared_list, grouped};
   return launch_attn_mx(L, static_cast<hipStream_t>(stream));
