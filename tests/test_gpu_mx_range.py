@@ -179,3 +179,25 @@ def test_every_code_under_every_scale(dtype):
         want = mx.dequantize(rows.codes.cpu().numpy(), rows.scales.cpu().numpy()).astype(np.float32)
     assert np.array_equal(got, want, equal_nan=True)
     assert np.isinf(want).any(axis=-1).reshape(256, 16).any(1).nonzero()[0].tolist() == [253, 254]
+
+
+@pytest.mark.parametrize("kind,g", KINDS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_subnormal_rows_and_large_queries(dtype, D, kind, g):
+    """Rows under the smallest scales, most of their elements subnormal numbers, and queries near the largest number: logits of a few units."""
+    say(f"mx attention, subnormal rows, {kind} {dtype} D={D} g={g}")
+    B, Hkv, rows = 13, 8, 1200
+    (K, _), (V, Vv) = coded_rows(B, Hkv, rows, D, 1), coded_rows(B, Hkv, rows, D, 2)
+    K.scales.copy_(K.scales % 3)
+    Kv = mx.dequantize(K.codes.cpu().numpy(), K.scales.cpu().numpy())
+    q = randn((B, Hkv * g, D), dtype, 3, 2.0 ** 123)
+    heads = {"lists": Hkv * g, "shared": 1, "dense": 0}[kind]
+    args = (None, None, 0, (0, rows))
+    if heads:
+        args = (torch.arange(rows, dtype=torch.int32, device=DEV).expand(B, heads, -1).contiguous(),
+                torch.full((B, heads), rows, dtype=torch.int32, device=DEV), rows, (0, 0))
+    assert mx_plan(q, Hkv, rows, kind != "lists")[0] == (kind != "lists")
+    ref = reference(q, Kv, Vv, rows, *args)
+    assert ref[1].max() > np.log(rows) + 0.1, "the rows make a difference"
+    assert_attention(attend(q, K, V, rows, *args, shared=kind == "shared"), ref, Vv)
