@@ -95,12 +95,13 @@ static bool fit_splits(const tb_cache_desc* d, AttnPlan& p, size_t ws_bytes) {
   if (p.nsplit < planned && p.nsplit > p.multiple) p.nsplit -= p.nsplit % p.multiple;
   return ws_bytes >= ws_layout(units, d->D, p.least).total;
 }
-// Rows in 4 bits: a lane takes a block of a row, a tile is kAttnMxLoads rows per lane group.  Splits by a model as attn_plan's, with constants
-// of their own, as a tile holds twice the rows in half the bytes: a start is worth kStart tiles, splitting at all kSplit and
-// every split kHandOver (the hand-over hardly grows with their number), and one workgroup a compute unit does not keep enough loads in flight (kAlone).  D = 128, bf16, us with
-// attn_plan's numbers and now: 8 x 32 heads on 8, 768 rows 11.8 and 9.9 (one split instead of two), 1024 rows 13.1 and 11.3; 32 heads, 512 rows 6.6
-// and 5.7; D = 64, 8 x 32 heads, 2048 rows 14.8 and 12.4.  On 215 shapes of 8 to 700 heads, 30 to 20000 rows 1.4% off the best number tried on
-// average, 17% at most; the constants were chosen on them.
+// Rows in 4 bits: a lane takes a block of a row, a tile is kAttnMxLoads rows per lane group.  Splits by a model as attn_plan's, with
+// constants of their own, as a tile holds twice the rows in half the bytes: a start is worth kStart tiles, splitting at all kSplit and every
+// split kHandOver (the hand-over hardly grows with their number), and one workgroup a compute unit does not keep enough loads in flight
+// (kAlone).  D = 128, bf16, us with attn_plan's numbers and now: 8 x 32 heads on 8, 768 rows 11.8 and 9.9 (one split instead of two), 1024
+// rows 13.1 and 11.3; 32 heads, 512 rows 6.6 and 5.7; D = 64, 8 x 32 heads, 2048 rows 14.8 and 12.4.  On 215 shapes of 8 to 700 heads, 30 to
+// 20000 rows 1.4% off the best number tried on average, 17% at most; the constants were chosen on them.  On 60 others, drawn at random (2 to
+// 704 heads, 30 to 20000 rows, 17 of them fp32), 1.8% and 16% (fp32, 6 x 8 heads on 1, 20000 rows: 30.7 us, 26.4 with 16 splits).
 AttnPlan attn_mx_plan(const tb_cache_desc* d, int64_t max_rows) {
   constexpr double kStart = 2.4, kSplit = 5.0, kHandOver = 0.02, kAlone = 1.4;
   const int64_t units = static_cast<int64_t>(d->B) * d->Hq, tile = kAttnMxWaves * kAttnMxLoads * (64 / (d->D / 32));
@@ -123,9 +124,11 @@ AttnPlan attn_mx_plan(const tb_cache_desc* d, int64_t max_rows) {
 }
 // One list (or none) for all heads of a KV group: a workgroup per KV group pays where there is enough work, the per-head kernel has the
 // shorter way to the first row and to the end (bf16, D = 128, dense, per head and grouped, us: 8 heads on 1 32768 rows 11.0 and 17.7,
-// 131072 23.4 and 28.8; 16 on 2 32768 14.2 and 18.0, 65536 23.3 and 19.5; 16 on 4 16384 10.6 and 10.7, 32768 15.4 and 12.4; 32 on 8 4096 8.0 and
-// 8.8, 8192 10.1 and 9.7; 8 x 32 on 8 512 8.1 and 8.7, 1024 10.7 and 9.0, 8192 39.8 and 18.5; D = 64: 32 on 8 4096 7.2 and 7.0, 8 x 32 on 8 512
-// 4.9 and 7.1, 1024 8.4 and 7.3): from 200000 rows and heads on, with less than six groups proportionally more.
+// 131072 23.4 and 28.8; 16 on 2 32768 14.2 and 18.0, 65536 23.3 and 19.5; 16 on 4 16384 10.6 and 10.7, 32768 15.4 and 12.4; 32 on 8 4096 8.0
+// and 8.8, 8192 10.1 and 9.7; 8 x 32 on 8 512 8.1 and 8.7, 1024 10.7 and 9.0, 8192 39.8 and 18.5; D = 64: 32 on 8 4096 7.2 and 7.0, 8 x 32 on 8
+// 512 4.9 and 7.1, 1024 8.4 and 7.3): from 200000 rows and heads on, with less than six groups proportionally more.  On 70 other shapes within
+// a factor of four of that, dense or with one list, half of them fp32, the choice was 1.7% off the faster form on average, and far off
+// where many heads have few rows (13 x 64 heads on 8, D = 64, 71 rows 8.0 us per head, as chosen, and 5.0 grouped).
 bool attn_mx_grouped(const tb_cache_desc* d, int64_t rows) {
   const int64_t groups = static_cast<int64_t>(d->B) * d->Hkv;
   return groups > 0 && d->Hq > d->Hkv && static_cast<int64_t>(d->B) * d->Hq * rows >= 1200000 / std::min<int64_t>(groups, 6);
@@ -134,7 +137,8 @@ bool attn_mx_grouped(const tb_cache_desc* d, int64_t rows) {
 // rows, and every split costs the last workgroup of the group one row a head.  Against one round wherever the groups leave room
 // for it: 136 groups of two heads at D = 64, 19464 rows 70.5 us (one split) and 50.5 (seven), of eight heads, one list of 7169 rows 58.5 and
 // 49.2.  On 94 shapes of 1 to 160 groups, 250 to 130000 rows 0.6% off the best number tried on average, 7% at most; the constants were
-// chosen on them.
+// chosen on them.  On 45 others, drawn at random (2 to 288 groups, 1100 to 114000 rows, 20 of them fp32), 4.0% and 33% (192 groups of two
+// heads, 4930 rows 42.8 us, 32.1 with one split; the next ones 11%).
 AttnPlan attn_mx_group_plan(const tb_cache_desc* d, int64_t max_rows) {
   constexpr int64_t kStart = 512, kRounds = 8;
   const int64_t groups = static_cast<int64_t>(d->B) * d->Hkv;

@@ -10,11 +10,12 @@
 // Work split, hand-over and the placement of a KV group's heads on one XCD as in tb_attn.hip.  A wave's tile is two rows per lane group;
 // its rows are on their way while the tile before is computed, and its list entries ahead of those.
 //
-// Bound by the memory where lists are long: 16 x 32 heads on 8, D = 128, 2048 of 16384 rows 29.6 us, where the loads alone take 28 (129 MB
+// Bound by the memory where lists are long: 16 x 32 heads on 8, D = 128, 2048 of 16384 rows 29.6 us, where the loads alone take 28 (132 MB
 // from HBM, random lines of 128 bytes and every line of the scales: without the scales' 17 MB 23), widened lists of 4 x 32 heads, some 11500
-// of 65536 rows, 37.8 of 35.5.  Elsewhere by the chain of trips to memory (list, rows, hand-over): 32 heads, 3277 of 32768 rows 9.0, of
-// which 4 are a launch without rows and 2 the hand-over.  Sixteen rows of 128 elements cost about 100 vector instructions.  Both scales of a row in one load instead of two: no difference.  Non-temporal gathers: 35.8 instead of 32.5 for the first of
-// these; three or four rows per lane group, eight or sixteen waves a workgroup: slower.
+// of 65536 rows, 37.8 of 35.5.  Elsewhere by the chain of trips to memory (list, rows, hand-over): 32 heads, 3277 of 32768 rows 8.9, of
+// which 4 are a launch without rows and 2 the hand-over.  Sixteen rows of 128 elements cost about 100 vector instructions.  Both scales of a
+// row in one load instead of two: no difference.  Non-temporal gathers: 35.8 instead of 32.5 for the first of these; three or four rows per
+// lane group, eight or sixteen waves a workgroup: slower.
 #include "tb_attn_merge.h"
 #include "tb_mx.h"
 
@@ -386,7 +387,7 @@ __global__ __launch_bounds__(NW * kWave, kMxWavesPerSimd<T>) void attn_mx_kernel
 // the rest of an address is scalar.
 //
 // Bound by the memory: 8 x 32 heads on 8, D = 128, all of 32768 rows 60 us (285 MB, 4.8 TB/s; the loads alone 57), 3 x 64 on 8, 20011 rows
-// 17.9 (65 MB), of which 6.3 are what a single step takes and 2.2 the hand-over; one list of 3661 rows for 4 x 32 heads 11.0.  Per head
+// 17.7 (65 MB), of which 6.3 are what a single step takes and 2.2 the hand-over; one list of 3661 rows for 4 x 32 heads 10.6.  Per head
 // these took 70.9 (20011 rows) and 18.5.  Loads two steps ahead, V's codes by 128-bit loads and swaps: no difference.
 typedef short mx_s16x8 __attribute__((ext_vector_type(8)));
 typedef float mx_acc4 __attribute__((ext_vector_type(4)));

@@ -35,7 +35,7 @@ __device__ __forceinline__ int mx_array_of(const MxCopyArgs& k, const int wg) {
 // magnitude from the bits (an integer maximum, in which a NaN or an infinity comes out on top) by two DPP moves.  With the largest in
 // [2^e, 2^(e+1)) the scale is 2^(e-2), so that the exponent field less 2 is the scale's byte: 6, the largest code, times it is
 // below 2^(e+1).  A stream: bound by the memory, for a single token by the launch.  K, V and K_imp of 32768 tokens (8 KV heads, D = 128, d' = 32,
-// bf16) 36.6 us, 5.2 TB/s of what is read and written, as a plain copy; a new token of 16 sequences 3.3.
+// bf16) 36.2 us, 5.3 TB/s of what is read and written, as a plain copy; a new token of 16 sequences 3.1.
 template <typename T>
 __global__ __launch_bounds__(kMxThreads) void quantize_mx_kernel(MxCopyArgs k) {
   constexpr int kLoads = kMxEltsPerThread / Pack16<T>::kElts;
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kMxThreads) void quantize_mx_kernel(MxCopyArgs k) {
 }
 
 // The values that rows stand for: a word of codes in, 16 or 32 bytes out.  The same rows 28.6 us (6.7 TB/s, codes from the last-level
-// cache) and 2.9.
+// cache) and 2.6.
 template <typename T>
 __global__ __launch_bounds__(kMxThreads) void dequantize_mx_kernel(MxCopyArgs k) {
   const int which = mx_array_of(k, blockIdx.x);
@@ -176,7 +176,7 @@ tb_status launch_copy(const MxCopyLaunch& L, hipStream_t st) {
 // only the fp32 sums round.  The first operand has the four heads four times over, so that accumulator v of lane (i, kb) in the product
 // for rows 16 t .. is head v of row 16 t + i whatever kb: lane L keeps that of its own row, and a score row leaves as 256
 // consecutive bytes.  Bound by the memory, twice as many bytes written (4 g a row) as read with eight heads: 4 x 64 heads on 8,
-// 131072 rows 38.2 us (205 MB, 5.4 TB/s); at one sequence by the launch: 32 heads on 8, 32768 rows 3.3.
+// 131072 rows 37.9 us (206 MB, 5.4 TB/s); at one sequence by the launch: 32 heads on 8, 32768 rows 3.5.
 typedef short mx_short8 __attribute__((ext_vector_type(8)));
 typedef float mx_f32x4 __attribute__((ext_vector_type(4)));
 constexpr int64_t kScoreNtStoreBytes = 16 << 20;  // score arrays from this size on bypass the caches (as for rows of other types)
