@@ -280,8 +280,9 @@ tb_status tb_score_mx(const tb_cache_desc* desc, const void* q_imp, const tb_mx_
 /* tb_sparse_decode_attn over a cache in 4 bits: lists, dense range, results as there.  idx and count may be NULL with max_count = 0
  * (the dense range alone: decode attention over all rows is tail_begin = 0, tail_end = N).  An attended row with a block that stands
  * for NaN makes the row's weight or the block's outputs NaN, as the formula does; rows that are not attended add nothing,
- * whatever they hold.  A head whose scores are all minus infinity has the results of an empty list.  Limits (else TB_ERR_UNSUPPORTED): N <= 2^24, max_count <= 2^29, strides between rows below 2^24 bytes, a
- * head's rows below 4 GiB.  ws: tb_workspace_bytes(TB_OP_ATTN_MX, ...). */
+ * whatever they hold.  A head whose scores are all minus infinity has the results of an empty list.  Limits (else
+ * TB_ERR_UNSUPPORTED): N <= 2^24, max_count <= 2^29, strides between rows below 2^24 bytes, a head's rows below 4 GiB.
+ * ws: tb_workspace_bytes(TB_OP_ATTN_MX, ...). */
 tb_status tb_sparse_decode_attn_mx(const tb_cache_desc* desc, const void* q, const tb_mx_rows* K, const tb_mx_rows* V, const int32_t* idx,
                                    const int32_t* count, int64_t idx_cap, int64_t max_count, int64_t tail_begin, int64_t tail_end,
                                    float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes, void* stream);

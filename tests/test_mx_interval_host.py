@@ -29,8 +29,8 @@ def loop(W=None, dtype=BF16, headless=False, Kimp=d):
     return MxIntervalDecoder(cache, W, Hq, 4, P, 1, headless=headless, dtype=dtype)
 
 
-@pytest.mark.parametrize("kw", [dict(W=torch.zeros((1, D, d))), dict(W=torch.zeros((1, D, d), dtype=BF16), dtype=F32), dict(W=torch.zeros((1, 2 * D, d), dtype=BF16)),
-                                dict(W=torch.zeros((1, D, 2 * d), dtype=BF16)), dict(Kimp=2 * d), dict(W=torch.zeros((D, d), dtype=BF16))])
+@pytest.mark.parametrize("kw", [dict(W=torch.zeros((1, D, d))), dict(W=torch.zeros((1, D, d), dtype=BF16), dtype=F32),
+                                dict(W=torch.zeros((1, 2 * D, d), dtype=BF16)), dict(W=torch.zeros((1, D, 2 * d), dtype=BF16)), dict(Kimp=2 * d), dict(W=torch.zeros((D, d), dtype=BF16))])
 def test_projections_of_another_type_or_shape(kw):
     with pytest.raises(AssertionError):
         loop(**kw)
