@@ -54,7 +54,7 @@ typedef struct tb_cache_desc {
 } tb_cache_desc;
 
 /* Operation selector for tb_workspace_bytes. */
-enum { TB_OP_SELECT = 1, TB_OP_ATTN = 2, TB_OP_DECODE_STEP = 3, TB_OP_ATTN_MX = 4 };
+enum { TB_OP_SELECT = 1, TB_OP_ATTN = 2, TB_OP_DECODE_STEP = 3, TB_OP_ATTN_MX = 4, TB_OP_PAGED_ATTN = 5 };
 
 /* Key-cache projection (Sec. 3.1, "Key-cache projection": K_imp = K W_K, W_K in R^{D x Dimp}).
  * Fills K_imp[b,h,n,:] = round(K[b,h,n,:] . W[hw]) for n_begin <= n < n_end, fp32 accumulation,
@@ -292,10 +292,69 @@ tb_status tb_sparse_decode_attn_shared_mx(const tb_cache_desc* desc, const void*
                                           const int32_t* idx, const int32_t* count, int64_t idx_cap, int64_t max_count, int64_t tail_begin,
                                           int64_t tail_end, float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- a cache in pages --------------------------------------------------------------------------
+ * K and V held as pages of `page` rows of every KV head, handed out to sequences in any order: row n of sequence b is row n % page of
+ * page table[b * table_stride + n / page].
+ * K, V : [pages][Hkv][page][D]   element (p,h,r,d) at  p*stride_p + h*stride_h + r*stride_n + d, strides in elements (alignment as above)
+ * table: int32, on the device, table_len entries a sequence.  An entry outside [0, pages) is a hole: nothing is written there, and its
+ *        rows are attended to by nobody.  Sequences may share pages that are only read.
+ * page is a power of two from 16 to 65536.
+ * Calls take the element type, B, Hq, Hkv and D from the descriptor, and N, the most rows that a sequence has (at most table_len * page);
+ * the descriptor's strides are not looked at. */
+typedef struct tb_paged_cache {
+  void* K;
+  void* V;
+  const int32_t* table;
+  int32_t pages, page, table_len;
+  int64_t table_stride;
+  int64_t k_stride_p, k_stride_h, k_stride_n;
+  int64_t v_stride_p, v_stride_h, v_stride_n;
+} tb_paged_cache;
+
+/* Rows of tokens, [T][heads][D]: element (t,h,d) at t*stride_t + h*stride_h + d, strides in elements (alignment as above), so that
+ * queries, keys and values may lie side by side as a projection leaves them. */
+typedef struct tb_token_rows {
+  void* rows;
+  int64_t stride_t, stride_h;
+} tb_token_rows;
+
+/* New tokens of the sequences reach the cache, their queries and keys rotated by their positions on the way.
+ * The T tokens of a call are those of sequence 0, then of sequence 1, ...: sequence b has the tokens cu[b] .. cu[b+1]-1 (cu: int32 [B+1],
+ * cu[0] = 0; NULL: T / B tokens each), which are the last of its lens[b] rows (int32 [B], on the device as cu is): token number i of n
+ * is row lens[b] - n + i.  Tokens whose row is not in [0, N), and those from cu[B] on, take no part: nothing of theirs is read or written.
+ *   angle(t, i) = positions[t] * inv_freq[i]   0 <= i < rot / 2; positions: int32 [T], NULL: the token's row; inv_freq: fp32 [rot / 2]
+ *   (x[j], x[k]) -> (x[j] cos - x[k] sin, x[k] cos + x[j] sin)   of q and k, (j, k) = (i, i + rot / 2), or (2i, 2i + 1) if interleaved
+ * with one rounding at the end, angles in 64 bits; elements from rot on stay as they are.  rot: 0 (no rotation) to D, a multiple of 16.
+ * k goes to K and, unless NULL, to k_out (what tb_project_keys takes); v to V; q, unless NULL, to q_out.  q_out may be q, and k_out k
+ * (the same rows with the same strides); otherwise outputs overlap nothing.  No two tokens of a call may have the same row of the same page. */
+tb_status tb_append_paged_kv(const tb_cache_desc* desc, const tb_paged_cache* cache, int64_t T, const int32_t* cu, const int32_t* lens,
+                             const int32_t* positions, const float* inv_freq, int32_t rot, int32_t interleaved, const tb_token_rows* q,
+                             const tb_token_rows* k, const tb_token_rows* v, const tb_token_rows* q_out, const tb_token_rows* k_out,
+                             void* stream);
+
+/* Attention of the new tokens over their sequences, those tokens' own rows among them (tb_append_paged_kv has put them there):
+ *   out[t,h,:] = sum_n softmax_n(sm_scale * q[t,h] . K[b,h/g,n]) * V[b,h/g,n],   max(0, p - window + 1) <= n <= p (window = 0: 0 <= n <= p)
+ * where p is the token's row; T, cu and lens as above.  One token of every sequence is a dense decode step, many are a prompt or a chunk of
+ * one; a call may hold both.  max_new: host-side bound on a sequence's new tokens (tokens past it are left out, as are those past cu[B]:
+ * their outputs are not written).
+ * out has the element type of q (one rounding; weights are rounded to that type, too, before they meet V); lse: fp32 [T][Hq] or NULL.  A
+ * token that attends to nothing, or with scores of minus infinity alone, has out = 0 and lse = -inf.  Rows that a token does not attend to
+ * add nothing to its result, whatever they hold.
+ * ws: tb_workspace_bytes(TB_OP_PAGED_ATTN, desc, T). */
+tb_status tb_paged_attn(const tb_cache_desc* desc, const tb_paged_cache* cache, int64_t T, const int32_t* cu, const int32_t* lens,
+                        int64_t max_new, const tb_token_rows* q, int64_t window, float sm_scale, const tb_token_rows* out, float* lse,
+                        void* ws, size_t ws_bytes, void* stream);
+
+/* tb_sparse_decode_attn over a cache in pages: lists and dense range name rows of the sequences, results as there (of a list's entries
+ * in holes: as if they were not listed).  K and V may be up to 64 GiB each (else TB_ERR_UNSUPPORTED).  ws: tb_workspace_bytes(TB_OP_ATTN, ...). */
+tb_status tb_sparse_decode_attn_paged(const tb_cache_desc* desc, const tb_paged_cache* cache, const void* q, const int32_t* idx,
+                                      const int32_t* count, int64_t idx_cap, int64_t max_count, int64_t tail_begin, int64_t tail_end,
+                                      float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* Scratch size in bytes for `op` on this cache shape.  max_count is the longest list the
  * attention will see, tail included; for TB_OP_SELECT and TB_OP_DECODE_STEP it is the list
  * length the selection policy produces, lo + kk + N - hi (TB_OP_SELECT returns 0 for every
- * shape whose rows are selected by one workgroup each).  Returns 0 on invalid
+ * shape whose rows are selected by one workgroup each); for TB_OP_PAGED_ATTN it is the most tokens of a call.  Returns 0 on invalid
  * input.  A workspace of the TB_OP_DECODE_STEP size serves TB_OP_SELECT and TB_OP_ATTN on that
  * shape, too, and a workspace of any of the sizes serves fewer rows and shorter lists as well: make it
  * for a cache's capacity.  The workspace pointer must be 16-byte aligned. */

@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_PKG, "libtokenbutler.so")
 
 TB_OK, TB_ERR_INVALID_ARG, TB_ERR_UNSUPPORTED, TB_ERR_WORKSPACE, TB_ERR_HIP = 0, 1, 2, 3, 4
 TB_F32, TB_BF16 = 0, 1
-TB_OP_SELECT, TB_OP_ATTN, TB_OP_DECODE_STEP, TB_OP_ATTN_MX = 1, 2, 3, 4
+TB_OP_SELECT, TB_OP_ATTN, TB_OP_DECODE_STEP, TB_OP_ATTN_MX, TB_OP_PAGED_ATTN = 1, 2, 3, 4, 5
 MX_BLOCK = 32  # elements that share a scale in a 4-bit cache
 
 EXPORTS = (
@@ -26,6 +26,7 @@ EXPORTS = (
     "tb_sparse_decode_attn_shared", "tb_sparse_decode_attn_static",
     "tb_gather_kv", "tb_gather_important", "tb_append_kv", "tb_buffered_decode_attn", "tb_append_buffered_decode_attn", "tb_migrate_buffered_decode_attn", "tb_predict_queries", "tb_decode_step",
     "tb_quantize_mx", "tb_dequantize_mx", "tb_score_mx", "tb_sparse_decode_attn_mx", "tb_sparse_decode_attn_shared_mx",
+    "tb_append_paged_kv", "tb_paged_attn", "tb_sparse_decode_attn_paged",
     "tb_workspace_bytes", "tb_workspace_init", "tb_read_stream_probe", "tb_status_string", "tb_version",
 )
 
@@ -52,6 +53,19 @@ class tb_mx_rows(ctypes.Structure):
         ("code_stride_b", ctypes.c_int64), ("code_stride_h", ctypes.c_int64), ("code_stride_n", ctypes.c_int64),
         ("scale_stride_b", ctypes.c_int64), ("scale_stride_h", ctypes.c_int64), ("scale_stride_n", ctypes.c_int64),
     ]
+
+
+class tb_paged_cache(ctypes.Structure):
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("table", ctypes.c_void_p),
+        ("pages", ctypes.c_int32), ("page", ctypes.c_int32), ("table_len", ctypes.c_int32), ("table_stride", ctypes.c_int64),
+        ("k_stride_p", ctypes.c_int64), ("k_stride_h", ctypes.c_int64), ("k_stride_n", ctypes.c_int64),
+        ("v_stride_p", ctypes.c_int64), ("v_stride_h", ctypes.c_int64), ("v_stride_n", ctypes.c_int64),
+    ]
+
+
+class tb_token_rows(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_void_p), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
 
 
 class tb_predictor_desc(ctypes.Structure):
@@ -99,6 +113,10 @@ def load_library() -> ctypes.CDLL:
     L.tb_score_mx.argtypes = [dp, vp, mp, f32, vp, i64, vp]
     L.tb_sparse_decode_attn_mx.argtypes = [dp, vp, mp, mp, vp, vp, i64, i64, i64, i64, f32, vp, vp, vp, sz, vp]
     L.tb_sparse_decode_attn_shared_mx.argtypes = L.tb_sparse_decode_attn_mx.argtypes
+    pp, rp = ctypes.POINTER(tb_paged_cache), ctypes.POINTER(tb_token_rows)
+    L.tb_append_paged_kv.argtypes = [dp, pp, i64, vp, vp, vp, vp, i32, i32, rp, rp, rp, rp, rp, vp]
+    L.tb_paged_attn.argtypes = [dp, pp, i64, vp, vp, i64, rp, i64, f32, rp, vp, vp, sz, vp]
+    L.tb_sparse_decode_attn_paged.argtypes = [dp, pp, vp, vp, vp, i64, i64, i64, i64, f32, vp, vp, vp, sz, vp]
     L.tb_workspace_bytes.argtypes = [i32, dp, i64]
     L.tb_workspace_bytes.restype = sz
     L.tb_workspace_init.argtypes = [vp, sz, vp]
@@ -249,6 +267,41 @@ def make_mx_desc(N: int, Hq: int, dtype: torch.dtype, K: Optional[MxRows] = None
     B, Hkv = ref.codes.shape[:2]
     D, Dimp = 128 if K is None else K.inner, 32 if Kimp is None else Kimp.inner
     return tb_cache_desc(B, Hq, Hkv, D, Dimp, _dtype_code(dtype), N, 0, 0, D, 0, 0, D, 0, 0, Dimp)
+
+
+class PagedCache:
+    """A layer's cache in pages: K, V [pages, Hkv, page, D], table int32 [B, entries]; row n of sequence b is row n % page of page
+    table[b, n // page].  The tensors stay the caller's: pages are handed out by writing into the table."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor):
+        assert K.shape == V.shape and K.dtype == V.dtype and table.dtype == torch.int32 and table.dim() == 2
+        assert table.shape[1] < 2 or table.stride(1) == 1
+        self.K, self.V, self.table = K, V, table
+        self.desc = tb_paged_cache(K.data_ptr(), V.data_ptr(), table.data_ptr(), K.shape[0], K.shape[2], table.shape[1],
+                                   table.stride(0) if table.shape[0] > 1 else table.shape[1], *_strides3(K), *_strides3(V))
+        self.ref = ctypes.byref(self.desc)
+        self.device = K.get_device()
+        if not self.device == V.get_device() == table.get_device():
+            raise ValueError(f"K on {K.device}, V on {V.device}, table on {table.device}")
+
+    def get_device(self) -> int:
+        """The GPU that the pages are on (-1: in host memory)."""
+        return self.device
+
+
+def make_paged_desc(N: int, Hq: int, cache: PagedCache) -> tb_cache_desc:
+    """Describe a layer whose cache is in pages; N: the most rows that a sequence has."""
+    _, Hkv, _, D = cache.K.shape
+    return tb_cache_desc(cache.table.shape[0], Hq, Hkv, D, 32, _dtype_code(cache.K.dtype), N, 0, 0, D, 0, 0, D, 0, 0, 32)
+
+
+def _token_rows(t: Optional[torch.Tensor]):
+    """Rows [T, heads, D] of tokens."""
+    if t is None:
+        return None
+    st = t.stride()
+    assert len(st) == 3 and st[2] == 1, "rows of tokens are [T, heads, D] with D contiguous"
+    return tb_token_rows(t.data_ptr(), st[0], st[1])
 
 
 def tb_version() -> int:
@@ -471,6 +524,60 @@ def tb_sparse_decode_attn_shared_mx(desc, q, K: MxRows, V: MxRows, idx, count, m
         ws.data_ptr(), ws.nbytes, _stream_on(out.get_device(), stream, (q, K, V, idx, count, lse, ws) if _several_devices else ()))
     if rc:
         _check(rc, "tb_sparse_decode_attn_shared_mx")
+
+
+def _check_tokens(desc, cache: PagedCache, cu, lens) -> None:
+    assert lens.dtype == torch.int32 and lens.is_contiguous() and lens.shape == (desc.B,) and desc.B == cache.table.shape[0]
+    assert cu is None or (cu.dtype == torch.int32 and cu.is_contiguous() and cu.shape == (desc.B + 1,))
+
+
+def tb_append_paged_kv(desc, cache: PagedCache, q, k, v, cu, lens, inv_freq, q_out=None, k_out=None, positions=None,
+                       interleaved: bool = False, stream=None) -> None:
+    """Rows of the new tokens k, v [T, Hkv, D] into the cache, k (also to k_out) and q [T, Hq, D] (to q_out; both may be None) rotated by
+    positions[t] * inv_freq[i] (int32 [T], None: the token's row; fp32 [rot / 2], None: no rotation).  cu: int32 [B + 1], None: as many
+    tokens of every sequence; lens: int32 [B], the rows of the sequences with the new tokens."""
+    T, Hkv, D = k.shape
+    assert v.shape == k.shape and k.dtype == v.dtype == cache.K.dtype and (Hkv, D) == (desc.Hkv, desc.D)
+    assert (q is None) == (q_out is None) and (q is None or (q.shape == q_out.shape == (T, desc.Hq, D) and q.dtype == q_out.dtype == k.dtype))
+    assert k_out is None or (k_out.shape == k.shape and k_out.dtype == k.dtype)
+    assert inv_freq is None or (inv_freq.dtype == torch.float32 and inv_freq.is_contiguous() and inv_freq.dim() == 1)
+    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.shape == (T,))
+    _check_tokens(desc, cache, cu, lens)
+    rc = (_lib or load_library()).tb_append_paged_kv(
+        ctypes.byref(desc), cache.ref, T, None if cu is None else cu.data_ptr(), lens.data_ptr(), None if positions is None else positions.data_ptr(),
+        None if inv_freq is None else inv_freq.data_ptr(), 0 if inv_freq is None else 2 * inv_freq.shape[0], interleaved, _token_rows(q), _token_rows(k),
+        _token_rows(v), _token_rows(q_out), _token_rows(k_out),
+        _stream_on(cache.device, stream, (q, k, v, cu, lens, inv_freq, q_out, k_out, positions) if _several_devices else ()))
+    if rc:
+        _check(rc, "tb_append_paged_kv")
+
+
+def tb_paged_attn(desc, cache: PagedCache, q, cu, lens, max_new: int, sm_scale: float, out, lse, ws, window: int = 0, stream=None) -> None:
+    """Causal attention of the new tokens q [T, Hq, D] over their sequences' rows (their own have been appended), to the last `window` of
+    them unless that is 0.  cu and lens as for tb_append_paged_kv; max_new: the most new tokens of a sequence; out: as q; lse: fp32 [T, Hq]
+    or None."""
+    assert q.shape == out.shape and q.dtype == out.dtype == cache.K.dtype and q.shape[1:] == (desc.Hq, desc.D)
+    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2])
+    _check_tokens(desc, cache, cu, lens)
+    rc = (_lib or load_library()).tb_paged_attn(
+        ctypes.byref(desc), cache.ref, q.shape[0], None if cu is None else cu.data_ptr(), lens.data_ptr(), max_new, _token_rows(q), window, sm_scale,
+        _token_rows(out), None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes,
+        _stream_on(cache.device, stream, (q, cu, lens, out, lse, ws) if _several_devices else ()))
+    if rc:
+        _check(rc, "tb_paged_attn")
+
+
+def tb_sparse_decode_attn_paged(desc, cache: PagedCache, q, idx, count, max_count: int, sm_scale: float, out, lse, ws, tail_begin: int = 0,
+                                tail_end: int = 0, stream=None) -> None:
+    """tb_sparse_decode_attn over a cache in pages."""
+    assert q.is_contiguous() and out.is_contiguous() and q.dtype == cache.K.dtype
+    assert q.shape == out.shape == (desc.B, desc.Hq, desc.D) and desc.B == cache.table.shape[0]
+    rc = (_lib or load_library()).tb_sparse_decode_attn_paged(
+        ctypes.byref(desc), cache.ref, q.data_ptr(), idx.data_ptr(), count.data_ptr(), idx.stride(-2), max_count, tail_begin, tail_end, sm_scale,
+        out.data_ptr(), None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes,
+        _stream_on(cache.device, stream, (q, idx, count, out, lse, ws) if _several_devices else ()))
+    if rc:
+        _check(rc, "tb_sparse_decode_attn_paged")
 
 
 def policy_count(N: int, k: int, sink: int, window: int) -> int:

@@ -495,6 +495,32 @@ tb_status sparse_attn_mx(const tb_cache_desc* d, const void* q, const tb_mx_rows
   return launch_attn_mx(L, static_cast<hipStream_t>(stream));
 }
 
+// A cache in pages; what a call asks of it whatever it reads.
+tb_status check_paged(const tb_cache_desc* d, const tb_paged_cache* c) {
+  TB_TRY(check_desc(d));
+  if (!c || !c->K || !c->V || !c->table || c->pages < 1 || c->table_len < 0 || c->table_stride < 0) return TB_ERR_INVALID_ARG;
+  if (c->page <= 0 || d->N > static_cast<int64_t>(c->table_len) * c->page) return TB_ERR_INVALID_ARG;
+  if (c->page < 16 || c->page > 65536 || (c->page & (c->page - 1)) != 0 || d->N > (int64_t{1} << 30)) return TB_ERR_UNSUPPORTED;
+  TB_TRY(check_strides(d, c->k_stride_p, c->k_stride_h, c->k_stride_n, d->D));
+  TB_TRY(check_strides(d, c->v_stride_p, c->v_stride_h, c->v_stride_n, d->D));
+  // (a page's rows of a head are addressed with 32-bit offsets)
+  if (c->k_stride_n * c->page >= (int64_t{1} << 29) || c->v_stride_n * c->page >= (int64_t{1} << 29)) return TB_ERR_UNSUPPORTED;
+  if (!aligned16(c->K) || !aligned16(c->V)) return TB_ERR_UNSUPPORTED;
+  return TB_OK;
+}
+
+// (rows that are read may be the same ones for several heads or tokens, those that are written may not)
+tb_status check_token_rows(const tb_cache_desc* d, const tb_token_rows* r, int64_t T, int32_t heads, bool written) {
+  if (!r || !r->rows) return TB_ERR_INVALID_ARG;
+  if (written && ((heads > 1 && r->stride_h < d->D) || (T > 1 && r->stride_t < d->D))) return TB_ERR_INVALID_ARG;
+  return aligned16(r->rows) ? check_strides(d, r->stride_t, r->stride_h, d->D, d->D) : TB_ERR_UNSUPPORTED;
+}
+
+tb_status check_tokens(const tb_cache_desc* d, int64_t T, const int32_t* cu, const int32_t* lens) {
+  if (T < 0 || !lens || (!cu && (d->B == 0 ? T != 0 : T % d->B != 0))) return TB_ERR_INVALID_ARG;
+  return T <= (int64_t{1} << 24) ? TB_OK : TB_ERR_UNSUPPORTED;  // (of a grid's numbers)
+}
+
 }  // namespace
 }  // namespace tb
 
@@ -861,6 +887,60 @@ tb_status tb_sparse_decode_attn_shared_mx(const tb_cache_desc* d, const void* q,
   return sparse_attn_mx(d, q, K, V, idx, count, idx_cap, max_count, tail_begin, tail_end, sm_scale, out, lse, ws, ws_bytes, stream, true);
 }
 
+tb_status tb_append_paged_kv(const tb_cache_desc* d, const tb_paged_cache* cache, int64_t T, const int32_t* cu, const int32_t* lens,
+                             const int32_t* positions, const float* inv_freq, int32_t rot, int32_t interleaved, const tb_token_rows* q,
+                             const tb_token_rows* k, const tb_token_rows* v, const tb_token_rows* q_out, const tb_token_rows* k_out,
+                             void* stream) {
+  TB_TRY(check_paged(d, cache));
+  TB_TRY(check_tokens(d, T, cu, lens));
+  if (rot < 0 || rot > d->D || (rot > 0 && !inv_freq) || !q != !q_out) return TB_ERR_INVALID_ARG;
+  if (rot % 16) return TB_ERR_UNSUPPORTED;
+  for (const tb_token_rows* r : {k, v}) TB_TRY(check_token_rows(d, r, T, d->Hkv, false));
+  if (q) TB_TRY(check_token_rows(d, q, T, d->Hq, false));
+  if (q) TB_TRY(check_token_rows(d, q_out, T, d->Hq, true));
+  if (k_out) TB_TRY(check_token_rows(d, k_out, T, d->Hkv, true));
+  if (T == 0 || d->B == 0 || d->Hkv == 0) return TB_OK;
+  return launch_append_paged(AppendPagedLaunch{d, cache, T, cu, lens, positions, inv_freq, rot, interleaved != 0, q, k, v, q_out, k_out},
+                             static_cast<hipStream_t>(stream));
+}
+
+tb_status tb_paged_attn(const tb_cache_desc* d, const tb_paged_cache* cache, int64_t T, const int32_t* cu, const int32_t* lens,
+                        int64_t max_new, const tb_token_rows* q, int64_t window, float sm_scale, const tb_token_rows* out, float* lse,
+                        void* ws, size_t ws_bytes, void* stream) {
+  TB_TRY(check_paged(d, cache));
+  TB_TRY(check_tokens(d, T, cu, lens));
+  if (max_new < 0 || window < 0) return TB_ERR_INVALID_ARG;
+  TB_TRY(check_token_rows(d, q, T, d->Hq, false));
+  TB_TRY(check_token_rows(d, out, T, d->Hq, true));
+  if (T == 0 || max_new == 0 || d->B == 0 || d->Hq == 0) return TB_OK;
+  if (!ws || !aligned16(ws) || ws_bytes < paged_attn_ws_bytes(d, T)) return TB_ERR_WORKSPACE;
+  return launch_paged_attn(PagedAttnLaunch{d, cache, T, cu, lens, std::min(max_new, T), q, window, sm_scale, out, lse, ws},
+                           static_cast<hipStream_t>(stream));
+}
+
+tb_status tb_sparse_decode_attn_paged(const tb_cache_desc* d, const tb_paged_cache* cache, const void* q, const int32_t* idx,
+                                      const int32_t* count, int64_t idx_cap, int64_t max_count, int64_t tail_begin, int64_t tail_end,
+                                      float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  TB_TRY(check_paged(d, cache));
+  if (!q || !idx || !count || !out || idx_cap < 0 || max_count < 0 || max_count > idx_cap) return TB_ERR_INVALID_ARG;
+  if (tail_begin < 0 || tail_begin > tail_end || tail_end > d->N) return TB_ERR_INVALID_ARG;
+  if (d->N == 0 && max_count > 0) return TB_ERR_INVALID_ARG;
+  if (!aligned16(q) || max_count + (tail_end - tail_begin) > (int64_t{1} << 30)) return TB_ERR_UNSUPPORTED;
+  // (rows are addressed with 32-bit offsets in units of 16 bytes)
+  const int64_t elt = d->dtype == TB_F32 ? 4 : 2, most = (int64_t{1} << 36) / elt;
+  if (cache->k_stride_p > most / std::max(cache->pages, 1) - cache->page * cache->k_stride_n ||
+      cache->v_stride_p > most / std::max(cache->pages, 1) - cache->page * cache->v_stride_n)
+    return TB_ERR_UNSUPPORTED;
+  const int64_t units = static_cast<int64_t>(d->B) * d->Hq;
+  if (units == 0) return TB_OK;
+  AttnPlan plan = attn_plan(d, max_count + (tail_end - tail_begin));
+  if (!ws || !aligned16(ws) || !fit_splits(d, plan, ws_bytes)) return TB_ERR_WORKSPACE;
+  const WsLayout w = ws_layout(units, d->D, plan.nsplit);
+  return launch_sparse_paged(SparsePagedLaunch{d, cache, q, idx, count, idx_cap, max_count, tail_begin, tail_end, sm_scale, out, lse,
+                                               reinterpret_cast<float*>(static_cast<char*>(ws) + w.part_off), reinterpret_cast<uint32_t*>(ws), plan},
+                             static_cast<hipStream_t>(stream));
+}
+
 size_t tb_workspace_bytes(int32_t op, const tb_cache_desc* d, int64_t max_count) {
   if (check_desc(d) != TB_OK || max_count < 0) return 0;
   const int64_t units = static_cast<int64_t>(d->B) * d->Hq;
@@ -869,6 +949,7 @@ size_t tb_workspace_bytes(int32_t op, const tb_cache_desc* d, int64_t max_count)
     if (attn_mx_grouped(d, max_count)) most = std::max(most, attn_mx_group_plan(d, max_count).max_split);
     return ws_layout(units, d->D, most).total;
   }
+  if (op == TB_OP_PAGED_ATTN) return paged_attn_ws_bytes(d, max_count);
   // two-stage selection of long rows (none for most shapes): max_count bounds the budget
   const size_t sel = select_scratch_upto(units, d->N, max_count);
   const size_t sel_total = sel ? ws_layout(units, d->D, 1).part_off + align_up(sel, 256) : 0;

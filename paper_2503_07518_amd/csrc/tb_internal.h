@@ -244,6 +244,52 @@ AttnPlan attn_mx_plan(const tb_cache_desc* d, int64_t max_rows);
 bool attn_mx_grouped(const tb_cache_desc* d, int64_t rows);
 AttnPlan attn_mx_group_plan(const tb_cache_desc* d, int64_t max_rows);
 
+// A cache in pages (tb_paged.hip, tb_paged_attn.hip).
+struct AppendPagedLaunch {
+  const tb_cache_desc* desc;
+  const tb_paged_cache* cache;
+  int64_t T;
+  const int32_t *cu, *lens, *positions;
+  const float* inv_freq;
+  int32_t rot;
+  bool interleaved;
+  const tb_token_rows *q, *k, *v, *q_out, *k_out;
+};
+tb_status launch_append_paged(const AppendPagedLaunch& a, hipStream_t st);
+
+struct SparsePagedLaunch {
+  const tb_cache_desc* desc;
+  const tb_paged_cache* cache;
+  const void* q;
+  const int32_t* idx;
+  const int32_t* count;
+  int64_t idx_cap, max_count, tail_begin, tail_end;
+  float sm_scale;
+  float* out;
+  float* lse;
+  float* partials;
+  uint32_t* counters;
+  AttnPlan plan;
+};
+tb_status launch_sparse_paged(const SparsePagedLaunch& a, hipStream_t st);
+
+struct PagedAttnLaunch {
+  const tb_cache_desc* desc;
+  const tb_paged_cache* cache;
+  int64_t T;
+  const int32_t *cu, *lens;
+  int64_t max_new;
+  const tb_token_rows* q;
+  int64_t window;
+  float sm_scale;
+  const tb_token_rows* out;
+  float* lse;
+  void* ws;
+};
+tb_status launch_paged_attn(const PagedAttnLaunch& a, hipStream_t st);
+// Bytes of workspace that calls of up to T tokens take: counters [B * Hkv], 256 B apart, then partial results.
+size_t paged_attn_ws_bytes(const tb_cache_desc* d, int64_t T);
+
 // Query predictor of a producer layer (LN + two-layer MLP), see tb_predict.hip.
 struct PredictLaunch {
   int dtype;

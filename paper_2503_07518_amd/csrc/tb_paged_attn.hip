@@ -1,0 +1,856 @@
+// Causal attention of new tokens over the rows of their sequences, held in pages.
+//
+//   chunk_kernel  many tokens: a workgroup takes 128 rows of (token, head of a KV group), so that a tile of K and V in LDS serves all
+//                 heads of the group, and runs over the rows that they see.
+//   token_kernel  up to 16 such rows a sequence (a decode step): bound by the rows of K and V, which go from memory to the matrix
+//                 cores without a stop in LDS; the rows of a sequence are split over workgroups.
+//
+// Both keep scores transposed: keys are the rows of the first product, queries its columns, so that a lane holds scores of one query
+// alone, and the accumulators of the first product are, as they lie, the weights' operand of the second: the order in which the
+// keys take its k slots is the accumulators' own, and the operand from V follows it.
+#include <algorithm>
+#include <cmath>
+
+#include "tb_attn_merge.h"
+#include "tb_paged.h"
+
+namespace tb {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+struct PagedAttnArgs {
+  Pages pages;
+  Tokens tok;
+  const char* q;
+  char* out;
+  int64_t q_t, q_h, out_t, out_h;  // strides in bytes
+  float* lse;
+  float scale_log2;  // not negative: its sign goes to the queries
+  uint32_t q_and, q_xor;
+  int32_t Hq, Hkv, gs;  // 1 << gs query heads a KV head
+  int32_t max_new, window;
+  int32_t nsplit;
+  int32_t few;  // chunk_kernel: sequences with up to so many rows are the token_kernel's
+  int32_t tiles;  // chunk_kernel: of a KV head, at most
+  float* partials;
+  int64_t pairs_off;
+  uint32_t* counters;
+};
+
+constexpr uint32_t kExponent = 0x7F800000u;  // of an infinite or NaN number
+
+__device__ __attribute__((aligned(16))) uint32_t zero_row[128];  // what a row that is not there reads as
+
+// Two bf16 signs at a time, or one of fp32: queries of a negative scale are turned round, those of a scale of 0 cleared.
+__device__ __forceinline__ u32x4 with_sign(u32x4 v, const PagedAttnArgs& a) { return (v & a.q_and) ^ a.q_xor; }
+
+// The largest exponent of eight bf16 or four fp32, at its place in an fp32 number.
+template <typename T>
+__device__ __forceinline__ uint32_t largest_exponent(const u32x4& v, uint32_t e) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    e = max(e, v[i] & kExponent);
+    if constexpr (!std::is_same<T, float>::value) e = max(e, v[i] << 16 & kExponent);
+  }
+  return e;
+}
+// Infinite and NaN elements replaced by zeros.
+template <typename T>
+__device__ __forceinline__ u32x4 finite_or_zero(u32x4 v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (std::is_same<T, float>::value)
+      v[i] = (v[i] & kExponent) == kExponent ? 0u : v[i];
+    else
+      v[i] = bf16x2_finite_or_zero(v[i]);
+  }
+  return v;
+}
+// What an element that is infinite or NaN adds to a sum that it has a weight in; 0 from others.
+__device__ __forceinline__ float not_finite_or_zero(float f) { return (__float_as_uint(f) & kExponent) == kExponent ? f : 0.f; }
+
+__device__ __forceinline__ f32x16 mfma32(u32x4 x, u32x4 y, f32x16 c) {
+  bf16x8 p, q;
+  __builtin_memcpy(&p, &x, 16);
+  __builtin_memcpy(&q, &y, 16);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(p, q, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(u32x4 x, u32x4 y, f32x4 c) {
+  bf16x8 p, q;
+  __builtin_memcpy(&p, &x, 16);
+  __builtin_memcpy(&q, &y, 16);
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, q, c, 0, 0, 0);
+}
+
+// What the other half of the wave holds.
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, kWave); }
+
+// ---- many tokens ----------------------------------------------------------------------------------
+// A wave holds 32 rows as columns of v_mfma_f32_32x32x16_bf16 (or 32x32x2_f32, which keeps fp32 as it is): their queries (32 or 64 registers), their
+// outputs transposed (D / 32 blocks of 32 columns of V), running reference and sum.  Four waves share the tiles of K and V, two of each in LDS:
+// while one is worked on, the next one comes straight from memory (global_load_lds, 16 bytes a lane).  Rows in LDS are
+// permuted in pieces of 16 bytes by their number so that neither the rows of K (a piece of 32 rows at once) nor the transposing reads
+// of V (a column of four rows) meet on a bank.
+constexpr int kChunkRows = 128;  // of a workgroup
+constexpr int kChunkThreads = 256;
+constexpr int kChunkWaves = kChunkThreads / kWave;
+// The reference of a row's softmax follows its maximum only when that has moved by more than this (weights stay below 2^8): the
+// accumulators are seldom rescaled.
+constexpr float kLazy = 8.f;
+
+template <typename T, int D>
+struct ChunkShape {
+  static constexpr int ROW = D * sizeof(T);                     // bytes
+  static constexpr int KEYS = ROW >= 512 ? 32 : 64;             // of a tile
+  static constexpr int PIECES = ROW / 16;                       // of 16 bytes in a row
+  static constexpr int AT_ONCE = 1024 / ROW;                    // rows that a wave loads at once
+  static constexpr int LOADS = KEYS * ROW / 1024 / kChunkWaves;  // of a wave for a tile of K or V
+  static constexpr int TILE = KEYS * ROW;
+  static constexpr int PAIRS = PIECES / 2;  // of pieces: what a lane half each takes of a row
+  static constexpr bool F32 = std::is_same<T, float>::value;
+  __device__ static __forceinline__ int k_swizzle(int row) { return PIECES == 8 ? row >> 1 & 7 : row & 15; }
+  __device__ static __forceinline__ int v_swizzle(int row) {
+    if (F32) return (row >> 2 & 1) << 3;
+    return PIECES == 8 ? (row >> 1 & 1) << 2 : (row & 3) << 2;
+  }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a) {
+  using S = ChunkShape<T, D>;
+  constexpr int KB = S::KEYS / 32, DB = D / 32;  // blocks of 32 keys, of 32 columns of V
+  __shared__ __attribute__((aligned(1024))) char s_k0[S::TILE], s_k1[S::TILE], s_v0[S::TILE], s_v1[S::TILE];
+
+  const int lane = lane_id(), wave = wave_id();
+  const int col = lane & 31, half = lane >> 5;
+  const int hkv = blockIdx.x % a.Hkv;
+  const int split = blockIdx.y;
+
+  // the tile of tokens: those that see the most rows begin first
+  const int tq_log = 7 - a.gs;  // tokens of a tile: 128 rows >> gs
+  int32_t at = blockIdx.x / a.Hkv, b = 0;
+  Sequence s;
+  int32_t n;  // of its tokens that take part
+  if (a.tok.cu) {
+    auto tiles_of = [&](int32_t i) -> uint32_t {
+      if (i >= a.tok.B) return 0;
+      const int32_t of = min(sequence(a.tok, i).n, a.max_new);
+      return of <= a.few >> a.gs ? 0 : (of + (1 << tq_log) - 1) >> tq_log;
+    };
+    uint32_t all = 0;
+    for (int32_t i = 0; i < a.tok.B; i += kWave) all += __builtin_amdgcn_readlane(wave_incl_scan_u32(tiles_of(i + lane)), kWave - 1);
+    if (static_cast<uint32_t>(at) >= all) return;
+    uint32_t want = all - 1 - at;
+    for (b = 0; b < a.tok.B; b += kWave) {
+      const uint32_t upto = wave_incl_scan_u32(tiles_of(b + lane));
+      const uint32_t here = __builtin_amdgcn_readlane(upto, kWave - 1);
+      if (want < here) {
+        const int skip = static_cast<int>(popc64(ballot64(upto <= want)));
+        if (skip) want -= __builtin_amdgcn_readlane(upto, skip - 1);
+        b += skip;
+        break;
+      }
+      want -= here;
+    }
+    at = static_cast<int32_t>(want);
+    b = __builtin_amdgcn_readfirstlane(b);
+  } else {
+    const int32_t tiles_each = (min(a.tok.each, a.max_new) + (1 << tq_log) - 1) >> tq_log;
+    at = a.tok.B * tiles_each - 1 - at;
+    if (at < 0) return;
+    b = at / tiles_each;
+    at -= b * tiles_each;
+  }
+  s = sequence(a.tok, b);
+  n = min(s.n, a.max_new);
+
+  // rows of the sequence that its tokens see
+  const int32_t i0 = at << tq_log;
+  const int32_t p_first = max(s.row + i0, 0), p_last = min(s.row + min(i0 + (1 << tq_log), n) - 1, a.tok.N - 1);
+  if (p_first > p_last) return;
+  const int32_t see_first = a.window ? max(p_first - a.window + 1, 0) : 0;
+  int32_t tile = see_first / S::KEYS, tile_end = p_last / S::KEYS + 1;
+  if (a.nsplit > 1) {
+    const int32_t per = (tile_end - tile + a.nsplit - 1) / a.nsplit;
+    tile = min(tile + split * per, tile_end);
+    tile_end = min(tile + per, tile_end);
+  }
+
+  // this lane's row: a token and a head of the group
+  const int row = wave * 32 + col;
+  const int32_t my_i = i0 + (row >> a.gs);
+  const int32_t my_p = s.row + my_i;
+  const int32_t my_low = a.window ? my_p - a.window : -1;  // it sees the rows behind this one, up to its own
+  const bool mine = my_i < n && my_p >= 0 && my_p < a.tok.N;
+  const int32_t my_t = s.first + (mine ? my_i : i0);
+  const int my_h = (hkv << a.gs) + (row & ((1 << a.gs) - 1));
+  // and the rows that the wave's see
+  const int32_t w_first = max(s.row + i0 + (wave * 32 >> a.gs), p_first), w_last = min(s.row + i0 + ((wave * 32 + 31) >> a.gs), p_last);
+  const int32_t w_see = a.window ? max(w_first - a.window + 1, 0) : 0;
+  u32x4 q[S::PAIRS];
+#pragma unroll
+  for (int c = 0; c < S::PAIRS; ++c) {
+    q[c] = u32x4{0u, 0u, 0u, 0u};
+    if (mine) q[c] = with_sign(*reinterpret_cast<const u32x4*>(a.q + my_t * a.q_t + my_h * a.q_h + (2 * c + half) * 16), a);
+  }
+
+  // pages of a tile's rows: lane r has that of row r, -1 behind the last one that is seen.  (Rows that are loaded together lie in one page, and
+  // the first of them may come before those that are seen.)
+  const int32_t* table = a.pages.table + b * a.pages.table_stride;
+  auto pages_of_tile = [&](int32_t t) -> int32_t {
+    const int32_t r = t * S::KEYS + (lane & (S::KEYS - 1));
+    return r <= p_last ? table[r >> a.pages.shift] : -1;
+  };
+  // the tile's rows that somebody sees and that are in no hole
+  auto rows_there = [&](int32_t t, int32_t page) -> unsigned long long {
+    return ballot64(page >= 0 && page < a.pages.pages && t * S::KEYS + (lane & (S::KEYS - 1)) >= see_first);
+  };
+  constexpr unsigned long long kAll = ~0ull;
+  const char* const kh = a.pages.K + hkv * a.pages.k_h;
+  const char* const vh = a.pages.V + hkv * a.pages.v_h;
+  auto stage = [&](char* sk, char* sv, int32_t t, int32_t page, unsigned long long there) {
+#pragma unroll
+    for (int x = 0; x < S::LOADS; ++x) {
+      const int r0 = (wave * S::LOADS + x) * S::AT_ONCE, r = r0 + lane / S::PIECES, piece = lane % S::PIECES;
+      const int64_t pg = __builtin_amdgcn_readlane(page, r0);  // (at most eight rows: one page)
+      const uint32_t in_page = static_cast<uint32_t>(t * S::KEYS + r0) & ((1u << a.pages.shift) - 1);
+      const char* k = kh + pg * a.pages.k_p + static_cast<uint64_t>(in_page) * a.pages.k_n;
+      const char* v = vh + pg * a.pages.v_p + static_cast<uint64_t>(in_page) * a.pages.v_n;
+      const uint32_t ko = (lane / S::PIECES) * a.pages.k_n + (piece ^ S::k_swizzle(r)) * 16;
+      const uint32_t vo = (lane / S::PIECES) * a.pages.v_n + (piece ^ S::v_swizzle(r)) * 16;
+      const char* kp = k + ko;
+      const char* vp = v + vo;
+      if (there != kAll && !(there >> r & 1)) {
+        kp = reinterpret_cast<const char*>(zero_row) + piece * 16;
+        vp = kp;
+      }
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)kp, (__attribute__((address_space(3))) void*)(sk + r0 * S::ROW), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)vp, (__attribute__((address_space(3))) void*)(sv + r0 * S::ROW), 16, 0, 0);
+    }
+  };
+
+  f32x16 o[DB];  // o[d] register r: column 32 d + 8 (r / 4) + 4 half + r % 4 of V, row `col`
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+  float m = -INFINITY, l = 0.f;  // (l: of this half's keys)
+
+  auto work = [&](const char* sk, const char* sv, int32_t t, unsigned long long there) {
+    const int32_t first = t * S::KEYS;
+    if (first > w_last || first + S::KEYS <= w_see || w_first > w_last) return;  // nothing that the wave's rows see
+    f32x16 x[KB];
+#pragma unroll
+    for (int k = 0; k < KB; ++k) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[k][r] = 0.f;
+#pragma unroll
+      for (int c = 0; c < S::PAIRS; ++c) {
+        const int r = k * 32 + col;
+        const u32x4 kk = *reinterpret_cast<const u32x4*>(sk + r * S::ROW + (((2 * c + half) ^ S::k_swizzle(r)) * 16));
+        if constexpr (S::F32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[k] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kk[e]), __uint_as_float(q[c][e]), x[k], 0, 0, 0);
+        } else {
+          x[k] = mfma32(kk, q[c], x[k]);
+        }
+      }
+    }
+    const bool masked = there != kAll || first + S::KEYS - 1 > w_first || (a.window && first <= w_last - a.window);
+    if (masked) {
+#pragma unroll
+      for (int k = 0; k < KB; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int kr = 32 * k + 8 * (r / 4) + 4 * half + r % 4;
+          const int32_t key = first + kr;
+          const bool seen = (key <= my_p) & (key > my_low) & ((there >> kr & 1) != 0);
+          x[k][r] = seen ? x[k][r] : -INFINITY;
+        }
+    }
+    float top = x[0][0];
+#pragma unroll
+    for (int k = 0; k < KB; ++k)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, x[k][r]);
+    top = fmaxf(top, other_half(top)) * a.scale_log2;  // (-inf times a scale of 0 does not come up: that is 1 then)
+    if (ballot64(top > m + kLazy)) {
+      // (nothing seen yet: sums are 0, or what the guard has put there)
+      const float m_new = fmaxf(m, top), alpha = m > -INFINITY ? exp2_safe(m - m_new) : 1.f;
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+      m = m_new;
+    }
+    const float m_ref = m > -INFINITY ? m : 0.f;  // nothing seen yet: all weights 0
+#pragma unroll
+    for (int k = 0; k < KB; ++k)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        x[k][r] = exp2_safe(fmaf(x[k][r], a.scale_log2, -m_ref));
+        l += x[k][r];
+      }
+    // output: keys 16 j .. + 15 (bf16), or one key a half (fp32), a step
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+      if constexpr (S::F32) {
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int kr = 32 * k + 8 * (r / 4) + 4 * half + r % 4;
+            const float v = *reinterpret_cast<const float*>(sv + kr * S::ROW + (((8 * d + col / 4) ^ S::v_swizzle(kr)) * 16) + (col & 3) * 4);
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, x[k][r], o[d], 0, 0, 0);
+          }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2 * KB; ++j) {
+          u32x4 v, p;
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const int kr = 16 * j + 8 * y + 4 * half + (lane & 15) / 4;
+            const int piece = 4 * d + 2 * (lane >> 4 & 1) + (lane & 3) / 2;
+            const char* at16 = sv + kr * S::ROW + ((piece ^ S::v_swizzle(kr)) * 16) + (lane & 1) * 8;
+            const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_char*)at16);
+            uint32_t w2[2];
+            __builtin_memcpy(w2, &w, 8);
+            v[2 * y] = w2[0];
+            v[2 * y + 1] = w2[1];
+          }
+#pragma unroll
+          for (int y = 0; y < 4; ++y) p[y] = bf16x2(x[j / 2][8 * (j & 1) + 2 * y], x[j / 2][8 * (j & 1) + 2 * y + 1]);
+          o[d] = mfma32(v, p, o[d]);
+        }
+      }
+    }
+  };
+  // A tile with rows that some of the workgroup's do not see: what is infinite or NaN there would be NaN times a weight of 0.  Such
+  // elements are added to the sums of those that see them, and are zeros for the products.  (All waves come here.)
+  auto guard = [&](char* sv, int32_t t, unsigned long long there) {
+    const int32_t first = t * S::KEYS;
+    if (there == kAll && first + S::KEYS - 1 <= p_first && !(a.window && first <= p_last - a.window)) return;
+    uint32_t most = 0;
+    for (int i = threadIdx.x * 16; i < S::TILE; i += kChunkThreads * 16) most = largest_exponent<T>(*reinterpret_cast<const u32x4*>(sv + i), most);
+    if (__builtin_expect(!__syncthreads_or(most == kExponent), 1)) return;
+    for (int kr = 0; kr < S::KEYS; ++kr) {
+      const int32_t key = first + kr;
+      const bool seen = mine & (key <= my_p) & (key > my_low) & ((there >> kr & 1) != 0);
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int c = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
+          const float v = to_float(*reinterpret_cast<const T*>(sv + kr * S::ROW + (((c * static_cast<int>(sizeof(T)) / 16) ^ S::v_swizzle(kr)) * 16) +
+                                                               c * sizeof(T) % 16));
+          o[d][r] += seen ? not_finite_or_zero(v) : 0.f;
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x * 16; i < S::TILE; i += kChunkThreads * 16)
+      *reinterpret_cast<u32x4*>(sv + i) = finite_or_zero<T>(*reinterpret_cast<const u32x4*>(sv + i));
+    __syncthreads();
+  };
+
+  int32_t page = -1;
+  unsigned long long there = 0;
+  if (tile < tile_end) {
+    page = pages_of_tile(tile);
+    there = rows_there(tile, page);
+    stage(s_k0, s_v0, tile, page, there);
+    page = pages_of_tile(tile + 1);
+  }
+  while (tile < tile_end) {
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    unsigned long long next = rows_there(tile + 1, page);
+    if (tile + 1 < tile_end) {
+      stage(s_k1, s_v1, tile + 1, page, next);
+      page = pages_of_tile(tile + 2);
+    }
+    guard(s_v0, tile, there);
+    work(s_k0, s_v0, tile, there);
+    if (++tile >= tile_end) break;
+    there = next;
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    next = rows_there(tile + 1, page);
+    if (tile + 1 < tile_end) {
+      stage(s_k0, s_v0, tile + 1, page, next);
+      page = pages_of_tile(tile + 2);
+    }
+    guard(s_v1, tile, there);
+    work(s_k1, s_v1, tile, there);
+    ++tile;
+    there = next;
+  }
+
+  l += other_half(l);
+  if (!mine) return;
+  const int64_t unit = static_cast<int64_t>(my_t) * a.Hq + my_h;
+  if (a.nsplit > 1) {
+    float* part = a.partials + (unit * a.nsplit + split) * D;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<float4*>(part + 32 * d + 2 * r + 4 * half) = make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+    if (half == 0) *reinterpret_cast<float2*>(a.partials + a.pairs_off + (unit * a.nsplit + split) * 2) = make_float2(m, l);
+    return;
+  }
+  const bool any = has_weight<true>(l);
+  const float inv = any ? 1.f / l : 0.f;
+  char* out = a.out + my_t * a.out_t + my_h * a.out_h;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      float f[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = any ? o[d][r + e] * inv : 0.f;
+      char* p = out + (32 * d + 2 * r + 4 * half) * sizeof(T);
+      if constexpr (S::F32)
+        *reinterpret_cast<uint4*>(p) = pack16(f);
+      else
+        *reinterpret_cast<uint2*>(p) = make_uint2(bf16x2(f[0], f[1]), bf16x2(f[2], f[3]));
+    }
+  if (a.lse && half == 0) a.lse[unit] = any ? m * kLn2 + logf(l) : -INFINITY;
+}
+
+// Adds up the splits of the chunk_kernel: a wave per row.
+constexpr int kJoinWaves = 4;
+template <typename T, int D>
+__global__ __launch_bounds__(kJoinWaves * kWave) void join_kernel(PagedAttnArgs a) {
+  constexpr int E = D / kWave;
+  const int lane = lane_id();
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kJoinWaves + wave_id();
+  if (unit >= static_cast<int64_t>(a.tok.T) * a.Hq) return;
+  const int32_t t = static_cast<int32_t>(unit / a.Hq), h = static_cast<int32_t>(unit - static_cast<int64_t>(t) * a.Hq);
+  const int32_t b = sequence_of(a.tok, t);
+  if (b >= a.tok.B) return;
+  const Sequence s = sequence(a.tok, b);
+  const int32_t i = t - s.first, p = s.row + i;
+  const int32_t n = min(s.n, a.max_new);
+  if (i < 0 || i >= n || n <= a.few >> a.gs || p < 0 || p >= a.tok.N) return;
+  const float* part = a.partials + unit * a.nsplit * D + lane * E;
+  const float* pairs = a.partials + a.pairs_off + unit * a.nsplit * 2;
+  float m = -INFINITY, l = 0.f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  for (int k = 0; k < a.nsplit; ++k) m = fmaxf(m, pairs[2 * k]);
+  for (int k = 0; k < a.nsplit; ++k) {
+    const float w = exp2_safe(pairs[2 * k] - (m > -INFINITY ? m : 0.f));
+    if (pairs[2 * k] == -INFINITY && pairs[2 * k + 1] == 0.f) continue;  // (saw nothing)
+    l += pairs[2 * k + 1] * w;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] += part[static_cast<int64_t>(k) * D + e] * w;
+  }
+  const bool any = has_weight<true>(l);
+  T* out = reinterpret_cast<T*>(a.out + t * a.out_t + h * a.out_h) + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) store_elt(out + e, any ? o[e] / l : 0.f);
+  if (a.lse && lane == 0) a.lse[unit] = any ? m * kLn2 + logf(l) : -INFINITY;
+}
+
+// ---- few tokens -----------------------------------------------------------------------------------
+// 16 rows (token, head of the group) as columns of v_mfma_f32_16x16x32_bf16 (16x16x4_f32).  Lane (i, kb) = (lane % 16, lane / 16) loads pieces
+// kb, kb + 4, .. of row i of 16 rows of K, and of the rows 4 kb + v of V the elements EV i .. + EV - 1; accumulator v of the scores
+// is then key 4 kb + v of column i, and element e of V's pieces the column EV i + e of the output, whose accumulator v is that of row 4 kb + v.
+// A wave has two steps' rows in flight.  Workgroups that share a sequence hand over by tb_attn_merge.h's protocol.
+constexpr int kTokenWaves = 8;
+constexpr int kTokenRows = 16;
+
+template <typename T, int D>
+struct TokenShape {
+  static constexpr bool F32 = std::is_same<T, float>::value;
+  static constexpr int ROW = D * sizeof(T);
+  static constexpr int GROUPS = ROW >= 512 ? 1 : 2;  // of 16 rows in a step
+  static constexpr int STEP = 16 * GROUPS;
+  static constexpr int KP = ROW / 64;                // pieces of a row of K for a lane
+  static constexpr int EV = D / 16;                  // elements of a row of V for a lane
+  static constexpr int VB = EV * sizeof(T);          // ... bytes: 8, 16 or 32
+  static constexpr int VP = (VB + 15) / 16;          // ... in pieces of up to 16
+  static_assert(F32 || GROUPS == 2, "32 keys fill a product");
+};
+
+template <typename T, int D, int GH>
+__global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttnArgs a) {
+  using S = TokenShape<T, D>;
+  __shared__ GroupLds<D, GH, kTokenWaves> gl;
+  const int tid = threadIdx.x, lane = lane_id(), wave = wave_id();
+  const int i16 = lane & 15, kb = lane >> 4;
+  const int split = blockIdx.x, hkv = blockIdx.y, b = blockIdx.z;
+  const Sequence s = sequence(a.tok, b);
+  const int32_t n = min(s.n, a.max_new);
+  if (n <= 0 || n > GH >> a.gs) return;
+  const int32_t p_first = max(s.row, 0), p_last = min(s.row + n - 1, a.tok.N - 1);
+  if (p_first > p_last) return;
+  const int32_t see_first = a.window ? max(p_first - a.window + 1, 0) : 0;
+  // whole steps for a workgroup: the splits that get any
+  const int32_t step_0 = see_first / S::STEP, steps = p_last / S::STEP + 1 - step_0;
+  const int32_t per = (steps + a.nsplit - 1) / a.nsplit, splits = (steps + per - 1) / per;
+  if (split >= splits) return;
+  const int32_t step_end = step_0 + min((split + 1) * per, steps);
+
+  const int32_t my_i = i16 >> a.gs, my_p = s.row + my_i;
+  const int32_t my_low = a.window ? my_p - a.window : -1;  // it sees the rows behind this one, up to its own
+  const bool mine = my_i < n && my_p >= 0 && my_p < a.tok.N;
+  u32x4 q[S::KP];
+  const char* qp = a.q + (s.first + (mine ? my_i : 0)) * a.q_t + ((hkv << a.gs) + (i16 & ((1 << a.gs) - 1))) * a.q_h + kb * 16;
+#pragma unroll
+  for (int c = 0; c < S::KP; ++c) {
+    q[c] = u32x4{0u, 0u, 0u, 0u};
+    if (mine) q[c] = with_sign(*reinterpret_cast<const u32x4*>(qp + c * 64), a);
+  }
+
+  // pages of the wave's next steps: lane (step, group of 16 rows)
+  const int32_t* table = a.pages.table + b * a.pages.table_stride;
+  constexpr int BATCH = kWave / S::GROUPS;
+  auto pages_from = [&](int32_t step) -> int32_t {
+    const int32_t r = (step + lane / S::GROUPS * kTokenWaves) * S::STEP + lane % S::GROUPS * 16;
+    const int32_t page = r <= p_last ? table[r >> a.pages.shift] : -1;
+    return page < a.pages.pages ? page : -1;
+  };
+  struct Rows {
+    u32x4 k[S::GROUPS][S::KP], v[S::GROUPS][4][S::VP];
+  };
+  const char* const kh = a.pages.K + hkv * a.pages.k_h + i16 * static_cast<uint64_t>(a.pages.k_n) + kb * 16;
+  const char* const vh = a.pages.V + hkv * a.pages.v_h + 4 * kb * static_cast<uint64_t>(a.pages.v_n) + i16 * S::VB;
+  auto fetch = [&](Rows& x, int32_t step, int32_t pages, int32_t nth) {
+#pragma unroll
+    for (int g = 0; g < S::GROUPS; ++g) {
+      const int64_t page = max(__builtin_amdgcn_readlane(pages, nth * S::GROUPS + g), 0);  // (a hole: rows that count for nothing below)
+      const uint32_t in_page = static_cast<uint32_t>(step * S::STEP + g * 16) & ((1u << a.pages.shift) - 1);
+      const char* k = kh + page * a.pages.k_p + static_cast<uint64_t>(in_page) * a.pages.k_n;
+      const char* v = vh + page * a.pages.v_p + static_cast<uint64_t>(in_page) * a.pages.v_n;
+#pragma unroll
+      for (int c = 0; c < S::KP; ++c) x.k[g][c] = *reinterpret_cast<const u32x4*>(k + c * 64);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < S::VP; ++c) {
+          if constexpr (S::VB == 8) {
+            const uint2 y = *reinterpret_cast<const uint2*>(v + r * static_cast<uint64_t>(a.pages.v_n));
+            x.v[g][r][c] = u32x4{y.x, y.y, 0u, 0u};
+          } else {
+            x.v[g][r][c] = *reinterpret_cast<const u32x4*>(v + r * static_cast<uint64_t>(a.pages.v_n) + c * 16);
+          }
+        }
+    }
+  };
+
+  f32x4 o[S::EV];
+#pragma unroll
+  for (int e = 0; e < S::EV; ++e) o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+
+  auto work = [&](Rows& x, int32_t step, int32_t pages, int32_t nth) {
+    const int32_t first = step * S::STEP;
+    uint32_t holes = 0;
+#pragma unroll
+    for (int g = 0; g < S::GROUPS; ++g) holes |= (__builtin_amdgcn_readlane(pages, nth * S::GROUPS + g) < 0 ? 1u : 0u) << g;
+    const bool masked = holes || first + S::STEP - 1 > p_first || (a.window && first <= p_last - a.window);
+    float p[S::GROUPS][4];
+#pragma unroll
+    for (int g = 0; g < S::GROUPS; ++g) {
+      f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < S::KP; ++c) {
+        if constexpr (S::F32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.k[g][c][e]), __uint_as_float(q[c][e]), sc, 0, 0, 0);
+        } else {
+          sc = mfma16(x.k[g][c], q[c], sc);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[g][r] = sc[r];
+    }
+    if (masked) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int g = 0; g < S::GROUPS; ++g)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int32_t key = first + 16 * g + 4 * kb + r;
+          // (selects: with branches here, hipcc of ROCm 7.2 lost the second half of this condition)
+          const bool hole = (holes >> g & 1) != 0;
+          p[g][r] = ((key <= my_p) & (key > my_low) & !hole) ? p[g][r] : -INFINITY;
+          const uint32_t kept = ((key > p_last) | (key < see_first) | hole) ? 0u : ~0u;  // a row that nobody sees counts as zeros
+#pragma unroll
+          for (int c = 0; c < S::VP; ++c) x.v[g][r][c] &= kept;
+#pragma unroll
+          for (int c = 0; c < S::VP; ++c) most = largest_exponent<T>(x.v[g][r][c], most);
+        }
+      // Rows that some tokens see and others do not: what is infinite or NaN there would be NaN times a weight of 0.  It is added to
+      // the sums of those that see it, and is zero for the products.
+      if (__builtin_expect(p_first < p_last && ballot64(most == kExponent) != 0, 0)) {
+#pragma clang loop unroll(disable)
+        for (int from = 0; from < 4; ++from)
+#pragma unroll
+          for (int g = 0; g < S::GROUPS; ++g)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int32_t key = first + 16 * g + 4 * from + r;
+#pragma unroll
+              for (int w = 0; w < S::VB / 4; ++w) {
+                __builtin_amdgcn_sched_barrier(0);  // (seldom run: few registers)
+                const uint32_t word = static_cast<uint32_t>(__shfl(static_cast<int>(x.v[g][r][w / 4][w % 4]), 16 * from + i16, kWave));
+#pragma unroll
+                for (int y = 0; y < S::EV * 4 / S::VB; ++y) {
+                  const float v = not_finite_or_zero(__uint_as_float(S::F32 ? word : (y ? word & 0xFFFF0000u : word << 16)));
+#pragma unroll
+                  for (int j = 0; j < 4; ++j) {
+                    const int32_t p_j = s.row + ((4 * kb + j) >> a.gs);
+                    o[w * (S::EV * 4 / S::VB) + y][j] += ((key <= p_j) & (key > (a.window ? p_j - a.window : -1))) ? v : 0.f;
+                  }
+                }
+              }
+            }
+#pragma unroll
+        for (int g = 0; g < S::GROUPS; ++g)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < S::VP; ++c) x.v[g][r][c] = finite_or_zero<T>(x.v[g][r][c]);
+      }
+    }
+    float top = p[0][0];
+#pragma unroll
+    for (int g = 0; g < S::GROUPS; ++g)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, p[g][r]);
+    top = fmaxf(top, __shfl_xor(top, 16, kWave));
+    top = fmaxf(top, __shfl_xor(top, 32, kWave)) * a.scale_log2;
+    if (ballot64(top > m + kLazy)) {
+      const float m_new = fmaxf(m, top), alpha = m > -INFINITY ? exp2_safe(m - m_new) : 1.f;
+      l *= alpha;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float al = __shfl(alpha, 4 * kb + r, kWave);  // (lane j < 16 holds row j)
+#pragma unroll
+        for (int e = 0; e < S::EV; ++e) o[e][r] *= al;
+      }
+      m = m_new;
+    }
+    const float m_ref = m > -INFINITY ? m : 0.f;
+#pragma unroll
+    for (int g = 0; g < S::GROUPS; ++g)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        p[g][r] = exp2_safe(fmaf(p[g][r], a.scale_log2, -m_ref));
+        l += p[g][r];
+      }
+    if constexpr (S::F32) {
+#pragma unroll
+      for (int e = 0; e < S::EV; ++e)
+#pragma unroll
+        for (int g = 0; g < S::GROUPS; ++g)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[g][r], __uint_as_float(x.v[g][r][e / 4][e % 4]), o[e], 0, 0, 0);
+    } else {
+      u32x4 w;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) w[y] = bf16x2(p[y / 2][2 * (y & 1)], p[y / 2][2 * (y & 1) + 1]);
+#pragma unroll
+      for (int e = 0; e < S::EV; ++e) {
+        const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;  // element e of two rows side by side
+        u32x4 v;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) v[y] = __builtin_amdgcn_perm(x.v[y / 2][2 * (y & 1) + 1][0][e / 2], x.v[y / 2][2 * (y & 1)][0][e / 2], sel);
+        o[e] = mfma16(w, v, o[e]);
+      }
+    }
+  };
+
+  // steps step_0 + split * per + wave, + kTokenWaves, ...; their pages in batches
+  int32_t step = step_0 + split * per + wave;
+  for (; step < step_end; step += BATCH * kTokenWaves) {
+    const int32_t pages = pages_from(step);
+    const int32_t count = min((step_end - step + kTokenWaves - 1) / kTokenWaves, BATCH);
+    Rows x, y;
+    fetch(x, step, pages, 0);
+    for (int32_t k = 0; k < count; k += 2) {
+      if (k + 1 < count) fetch(y, step + (k + 1) * kTokenWaves, pages, k + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      work(x, step + k * kTokenWaves, pages, k);
+      if (k + 1 >= count) break;
+      if (k + 2 < count) fetch(x, step + (k + 2) * kTokenWaves, pages, k + 2);
+      __builtin_amdgcn_sched_barrier(0);
+      work(y, step + (k + 1) * kTokenWaves, pages, k + 1);
+    }
+  }
+  l += __shfl_xor(l, 16, kWave);
+  l += __shfl_xor(l, 32, kWave);
+  if (lane < GH) {
+    gl.m[wave][lane] = m;
+    gl.l[wave][lane] = l;
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (4 * kb + r < GH) {
+#pragma unroll
+      for (int e = 0; e < S::EV; ++e) gl.acc[wave][4 * kb + r][S::EV * i16 + e] = o[e][r];
+    }
+  __syncthreads();
+
+  // merge the waves; a thread has outputs tid, tid + 512, ... of the GH x D
+  constexpr int kThreads = kTokenWaves * kWave, OUTS = (GH * D + kThreads - 1) / kThreads;
+  const int64_t group = static_cast<int64_t>(b) * a.Hkv + hkv;
+  auto store = [&](int row, int d, float M, float L, float v) {
+    const int32_t i = row >> a.gs, p = s.row + i;
+    if (i >= n || p < 0 || p >= a.tok.N) return;
+    const int64_t t = s.first + i;
+    const int h = (hkv << a.gs) + (row & ((1 << a.gs) - 1));
+    const bool any = has_weight<true>(L);
+    store_elt(reinterpret_cast<T*>(a.out + t * a.out_t + h * a.out_h) + d, any ? v / L : 0.f);
+    if (a.lse && d == 0) a.lse[t * a.Hq + h] = any ? M * kLn2 + logf(L) : -INFINITY;
+  };
+#pragma unroll
+  for (int x = 0; x < OUTS; ++x) {
+    const int e = tid + x * kThreads, row = e / D, d = e % D;
+    if (e >= GH * D) continue;
+    float M = -INFINITY, L = 0.f, v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kTokenWaves; ++w) M = fmaxf(M, gl.m[w][row]);
+    const float m_ref = M > -INFINITY ? M : 0.f;
+#pragma unroll
+    for (int w = 0; w < kTokenWaves; ++w) {
+      const float wgt = exp2_safe(gl.m[w][row] - m_ref);
+      L += gl.l[w][row] * wgt;
+      v += gl.acc[w][row][d] * wgt;
+    }
+    if (splits == 1) {
+      store(row, d, M, L, v);
+    } else {
+      const int64_t to = (group * GH + row) * a.nsplit + split;
+      __hip_atomic_store(&a.partials[to * D + d], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (d == 0) store_pair(a.partials + a.pairs_off + to * 2, M, L);
+    }
+  }
+  if (splits == 1) return;
+  publish_fence();
+  __syncthreads();
+  if (tid == 0) {
+    const uint32_t ticket = __hip_atomic_fetch_add(&a.counters[group * kCounterStrideWords], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    gl.last = ticket == static_cast<uint32_t>(splits - 1) ? 1u : 0u;
+  }
+  __syncthreads();
+  if (!gl.last) return;
+#pragma unroll
+  for (int x = 0; x < OUTS; ++x) {
+    const int e = tid + x * kThreads, row = e / D, d = e % D;
+    if (e >= GH * D) continue;
+    const int64_t from = (group * GH + row) * a.nsplit;
+    float M = -INFINITY, L = 0.f, v = 0.f;
+    for (int32_t k = 0; k < splits; ++k) {
+      const unsigned long long pair = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(a.partials + a.pairs_off + (from + k) * 2),
+                                                        __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const float o_k = __hip_atomic_load(&a.partials[(from + k) * D + d], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const float m_k = __uint_as_float(static_cast<uint32_t>(pair)), l_k = __uint_as_float(static_cast<uint32_t>(pair >> 32));
+      const float m_new = fmaxf(M, m_k);
+      const float m_ref = m_new > -INFINITY ? m_new : 0.f;
+      const float wa = exp2_safe(M - m_ref), wb = exp2_safe(m_k - m_ref);
+      L = L * wa + l_k * wb;
+      v = v * wa + o_k * wb;
+      M = m_new;
+    }
+    store(row, d, M, L, v);
+  }
+  if (tid == 0) __hip_atomic_store(&a.counters[group * kCounterStrideWords], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// ---- plans ----------------------------------------------------------------------------------------
+constexpr int64_t kCus = 256;
+constexpr int64_t kChunkTarget = 2 * kCus;  // workgroups of the chunk_kernel that the chip holds at once
+
+int chunk_keys(const tb_cache_desc& d) { return d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 32 : 64; }
+// Splits of a sequence's rows: as many workgroups as the chip holds, of at least four tiles each.
+int64_t chunk_splits(const tb_cache_desc& d, int64_t tiles) {
+  const int64_t wgs = std::max<int64_t>(tiles * d.Hkv, 1);
+  return std::max<int64_t>(1, std::min(kChunkTarget / wgs, d.N / (4 * chunk_keys(d))));
+}
+// ... of at least two steps a wave.
+int64_t token_splits(const tb_cache_desc& d) {
+  const int64_t groups = std::max<int64_t>(static_cast<int64_t>(d.B) * d.Hkv, 1), step = d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 16 : 32;
+  return std::max<int64_t>(1, std::min(kCus / groups, d.N / (2 * step * kTokenWaves)));
+}
+size_t token_counters(const tb_cache_desc& d) { return static_cast<size_t>(d.B) * d.Hkv * kCounterStrideWords * sizeof(uint32_t); }
+
+template <typename T, int D>
+tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
+  const tb_cache_desc& d = *L.desc;
+  constexpr int64_t elt = sizeof(T);
+  PagedAttnArgs a;
+  a.pages = pages_of(*L.cache, elt);
+  a.tok = tokens_of(d, L.T, L.cu, L.lens);
+  a.q = static_cast<const char*>(L.q->rows);
+  a.out = static_cast<char*>(L.out->rows);
+  a.q_t = L.q->stride_t * elt;
+  a.q_h = L.q->stride_h * elt;
+  a.out_t = L.out->stride_t * elt;
+  a.out_h = L.out->stride_h * elt;
+  a.lse = L.lse;
+  const uint32_t signs = elt == 4 ? 0x80000000u : 0x80008000u;
+  a.scale_log2 = L.sm_scale == 0.f ? 1.f : fabsf(L.sm_scale) * kLog2e;
+  a.q_and = L.sm_scale == 0.f ? 0u : ~0u;
+  a.q_xor = L.sm_scale < 0.f ? signs : 0u;
+  a.Hq = d.Hq;
+  a.Hkv = d.Hkv;
+  a.gs = __builtin_ctz(static_cast<unsigned>(d.Hq / d.Hkv));
+  a.max_new = static_cast<int32_t>(L.max_new);
+  a.window = static_cast<int32_t>(std::min<int64_t>(L.window, d.N));
+  a.counters = static_cast<uint32_t*>(L.ws);
+  a.partials = reinterpret_cast<float*>(static_cast<char*>(L.ws) + token_counters(d));
+  const int64_t most = L.cu ? L.max_new : a.tok.each;  // tokens of a sequence, at most
+  const bool chunks = most << a.gs > kTokenRows;
+  const bool tokens = !chunks || (L.cu && d.B > 1);  // sequences of few tokens may be among the others
+  if (chunks) {
+    const int tq_log = 7 - a.gs;
+    const int64_t tiles = L.cu ? (L.T >> tq_log) + std::min<int64_t>(d.B, L.T) : d.B * ((std::min<int64_t>(a.tok.each, L.max_new) + (1 << tq_log) - 1) >> tq_log);
+    a.few = tokens ? kTokenRows : 0;
+    a.tiles = static_cast<int32_t>(tiles);
+    // (ragged: at least as many tiles as full ones)
+    a.nsplit = static_cast<int32_t>(chunk_splits(d, L.cu ? std::max<int64_t>((L.T + (1 << tq_log) - 1) >> tq_log, 1) : tiles));
+    a.pairs_off = static_cast<int64_t>(a.tok.T) * a.Hq * a.nsplit * D;
+    tb_status rc = launch_one(chunk_kernel<T, D>, dim3(static_cast<unsigned>(d.Hkv * tiles), a.nsplit), kChunkThreads, st, a);
+    if (rc != TB_OK) return rc;
+    if (a.nsplit > 1) {
+      const int64_t units = static_cast<int64_t>(a.tok.T) * a.Hq;
+      rc = launch_one(join_kernel<T, D>, dim3(static_cast<unsigned>((units + kJoinWaves - 1) / kJoinWaves)), kJoinWaves * kWave, st, a);
+      if (rc != TB_OK) return rc;
+    }
+  }
+  if (tokens) {
+    a.nsplit = static_cast<int32_t>(token_splits(d));
+    const dim3 grid(a.nsplit, d.Hkv, d.B);
+    a.pairs_off = static_cast<int64_t>(d.B) * d.Hkv * kTokenRows * a.nsplit * D;
+    return launch_one(token_kernel<T, D, kTokenRows>, grid, kTokenWaves * kWave, st, a);
+  }
+  return TB_OK;
+}
+
+}  // namespace
+
+size_t paged_attn_ws_bytes(const tb_cache_desc* d, int64_t T) {
+  const int64_t row = (d->D + 2) * static_cast<int64_t>(sizeof(float));
+  const int64_t tokens = static_cast<int64_t>(d->B) * d->Hkv * kTokenRows * token_splits(*d);
+  // a call's rows times its splits: at most those of kChunkTarget workgroups, or of the rows in as many splits as there can be
+  const int64_t chunk = std::min(kChunkTarget * kChunkRows, T * d->Hq * chunk_splits(*d, 0));
+  return token_counters(*d) + static_cast<size_t>(std::max(tokens, chunk) * row);
+}
+
+tb_status launch_paged_attn(const PagedAttnLaunch& L, hipStream_t st) {
+  if (L.desc->dtype == TB_F32) return L.desc->D == 64 ? launch_td<float, 64>(L, st) : launch_td<float, 128>(L, st);
+  return L.desc->D == 64 ? launch_td<bf16_t, 64>(L, st) : launch_td<bf16_t, 128>(L, st);
+}
+
+}  // namespace tb

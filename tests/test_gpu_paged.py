@@ -1,0 +1,420 @@
+"""A cache in pages on the GPU: new rows with their rotation, attention of new tokens, attention over lists, against 64 bits."""
+import math
+
+import pytest
+import torch
+
+from oracle import paged as ref
+from paper_2503_07518_amd import binding as tb
+from paged_util import attn_bounds, close, half_step, make
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def on_gpu(c):
+    c.cache = tb.PagedCache(c.K.to(DEV), c.V.to(DEV), c.table.to(DEV))
+    c.desc = tb.make_paged_desc(c.N, c.Hq, c.cache)
+    return c
+
+
+def side_by_side(c):
+    """q, k and v as a projection leaves them: one row a token."""
+    qkv = torch.cat((c.q, c.k, c.v), 1).to(DEV)
+    return qkv[:, :c.Hq], qkv[:, c.Hq:c.Hq + c.Hkv], qkv[:, c.Hq + c.Hkv:]
+
+
+def same_bits(a, b):
+    return torch.equal(a.cpu().view(torch.uint8), b.cpu().view(torch.uint8))
+
+
+# ---- arrival ----------------------------------------------------------------------------------------
+def inv_freq(rot, base=10000.0):
+    return (base ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)).float() if rot else None
+
+
+def check_append(c, rot, interleaved, positions=None, with_q=True, in_place=False, k_out=True):
+    f = inv_freq(rot)
+    want = ref.append(c.q, c.k, c.v, c.K, c.V, c.table, c.cu, c.lens, c.N, f, interleaved, positions)
+    on_gpu(c)
+    q, k, v = side_by_side(c)
+    before = [x.clone() for x in (q, k, c.cache.K, c.cache.V)]
+    qo = q if in_place else torch.full((c.T, c.Hq, c.D), 7.0, dtype=c.dtype, device=DEV)
+    ko = k if in_place else (torch.full((c.T, c.Hkv, c.D), 7.0, dtype=c.dtype, device=DEV) if k_out else None)
+    tb.tb_append_paged_kv(c.desc, c.cache, q if with_q else None, k, v, c.cu.to(DEV), c.lens.to(DEV), None if f is None else f.to(DEV),
+                          qo if with_q else None, ko, positions=None if positions is None else positions.to(DEV), interleaved=interleaved)
+    torch.cuda.synchronize()
+    took = sorted(t for t, _, _ in ref.tokens(c.cu, c.lens, c.N))
+    out = [t for t in range(c.T) if t not in took]
+
+    def tolerance(x, y):
+        # cos and sin: the angle in half turns rounded to fp32 (pi 2^-25) and their own 2 steps; two products, a sum, the result's rounding
+        big = x.double().abs().amax(-1, keepdim=True) * 2
+        return big * 2.0 ** -21 + y.nan_to_num().abs() * half_step(c.dtype) * (1.01 if c.dtype != F32 else 2)
+
+    pairs = ([(qo, before[0], c.q, want[0])] if with_q else []) + ([(ko, before[1], c.k, want[1])] if ko is not None else [])
+    for got, was, x, y in pairs:
+        close(got[took], y[took], tolerance(x[took], y[took]), "rotated")
+        if rot < c.D:
+            assert same_bits(got[took][..., rot:].contiguous(), x[took][..., rot:].contiguous())
+        assert same_bits(got[out].contiguous(), (was if in_place else torch.full_like(got, 7.0))[out].contiguous())
+    # the rows that arrived, and all others as they were
+    arrived = torch.zeros(c.K.shape[0], c.page, dtype=torch.bool)
+    for t, b, row in ref.tokens(c.cu, c.lens, c.N):
+        at = ref.place(c.table, b, row, c.page, c.K.shape[0])
+        if at:
+            arrived[at] = True
+            close(c.cache.K[at[0], :, at[1]], want[1][t], tolerance(c.k[t], want[1][t]), "K")
+            assert same_bits(c.cache.V[at[0], :, at[1]].contiguous(), c.v[t].contiguous())
+    for now, was in ((c.cache.K, before[2]), (c.cache.V, before[3])):
+        assert same_bits(now.cpu().transpose(1, 2)[~arrived].contiguous(), was.cpu().transpose(1, 2)[~arrived].contiguous())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D,rot,interleaved", [(128, 128, False), (128, 128, True), (128, 64, False), (128, 16, True), (64, 64, False), (64, 32, True), (64, 0, False), (64, 48, False)])
+def test_append(dtype, D, rot, interleaved):
+    check_append(make(dtype, 8, 2, D, 16, [1, 0, 5, 17, 40], [0, 9, 30, 15, 3], seed=D + rot), rot, interleaved)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (8, 8), (2, 1), (64, 8)])
+def test_append_heads(Hq, Hkv):
+    check_append(make(BF, Hq, Hkv, 128, 32, [3, 1], [70, 0]), 128, False)
+
+
+def test_append_in_place_and_alone():
+    check_append(make(BF, 4, 2, 128, 16, [3, 1], [7, 0]), 128, False, in_place=True)
+    check_append(make(F32, 4, 2, 64, 16, [3, 1], [7, 0]), 64, True, with_q=False, k_out=False)
+
+
+def test_append_positions_far_apart():
+    c = make(F32, 4, 1, 128, 16, [4, 3], [1, 2])
+    check_append(c, 128, False, positions=torch.tensor([2 ** 31 - 1, 0, -5, 1 << 20, 131071, 999999937, 3], dtype=torch.int32))
+
+
+def test_append_leaves_out_what_has_no_place():
+    # a padded batch: lens below the tokens, tokens behind the last sequence, rows past N, holes
+    c = make(BF, 4, 2, 64, 16, [5, 4, 20], [0, 3, 30], pad=3, holes=[(2, 2), (1, 0)])
+    c.lens[0] = 2  # rows -3, -2, -1, 0, 1
+    c.N = 45       # of sequence 2, five rows are past it
+    check_append(c, 64, False)
+
+
+def test_append_many_sequences():
+    check_append(make(BF, 2, 1, 64, 16, [i % 3 for i in range(200)], [i % 7 for i in range(200)]), 64, False)
+
+
+# ---- attention of new tokens ------------------------------------------------------------------------
+def run_attn(c, sm_scale, window=0, max_new=None, cu=True, ws=None, lse=True):
+    q = c.q.to(DEV)
+    out = torch.full_like(q, 7.0)
+    l = torch.full((c.T, c.Hq), 7.0, device=DEV) if lse else None
+    if ws is None:
+        ws = tb.new_workspace(tb.TB_OP_PAGED_ATTN, c.desc, c.T)
+    tb.tb_paged_attn(c.desc, c.cache, q, c.cu.to(DEV) if cu else None, c.lens.to(DEV), c.most if max_new is None else max_new, sm_scale, out, l, ws, window=window)
+    torch.cuda.synchronize()
+    return out, l
+
+
+def check_attn(c, sm_scale=None, window=0, max_new=None, cu=True):
+    sm_scale = c.D ** -0.5 if sm_scale is None else sm_scale
+    want, lse, mag = ref.attn(c.q, c.K, c.V, c.table, c.cu, c.lens, c.N, sm_scale, window, max_new)
+    on_gpu(c)
+    out, l = run_attn(c, sm_scale, window, max_new, cu)
+    took = sorted(t for t, _, _ in ref.tokens(c.cu, c.lens, c.N, max_new))
+    rest = [t for t in range(c.T) if t not in took]
+    assert bool((out[rest] == 7).all()) and bool((l[rest] == 7).all())
+    tol, tol_lse = attn_bounds(c, c.q, c.K, c.V, c.N, sm_scale, mag[took].nan_to_num(), want[took].nan_to_num())
+    close(out[took], want[took], tol, "out")
+    close(l[took], lse[took], tol_lse + lse[took].abs().nan_to_num(posinf=0) * 2.0 ** -22, "lse")
+    return out, l
+
+
+SHAPES = [(8, 8), (8, 4), (8, 2), (8, 1)]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv", SHAPES)
+def test_tokens(dtype, D, Hq, Hkv):
+    check_attn(make(dtype, Hq, Hkv, D, 16, [1, 1, 1, 1, 1, 1], [0, 1, 15, 16, 700, 33], seed=Hkv))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv", SHAPES)
+def test_chunks(dtype, D, Hq, Hkv):
+    check_attn(make(dtype, Hq, Hkv, D, 16, [37, 0, 150, 1, 2, 65], [0, 5, 70, 130, 0, 31], seed=Hkv))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("window", [1, 2, 17, 64, 100])
+@pytest.mark.parametrize("page", [16, 64])
+def test_windows(dtype, window, page):
+    check_attn(make(dtype, 4, 2, 64, page, [90, 1, 3, 200], [0, 260, 100, 61], seed=window), window=window)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_split_rows(dtype, D):
+    # a short chunk over a long sequence: the rows are split over workgroups
+    check_attn(make(dtype, 4, 1, D, 64, [33], [2100]))
+    check_attn(make(dtype, 4, 1, D, 64, [4], [4000]))
+    check_attn(make(dtype, 4, 1, D, 32, [1], [4095]), window=1500)
+
+
+@pytest.mark.parametrize("page", [16, 32, 128, 1024])
+def test_pages(page):
+    check_attn(make(BF, 4, 2, 128, page, [70, 1, 5], [100, 1025, 15]))
+
+
+@pytest.mark.parametrize("n", [1, 2, 4, 5, 16, 17, 31])
+def test_numbers_of_tokens(n):
+    check_attn(make(BF, 4, 1, 64, 16, [n, n], [40, 0]))
+    check_attn(make(BF, 2, 2, 128, 16, [n, n], [3, 129]), cu=False)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1e-3, 4.0])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_scales(scale, dtype):
+    check_attn(make(dtype, 4, 2, 64, 16, [50, 1], [20, 90]), sm_scale=scale)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("new,kept", [([60, 1, 1], [70, 40, 15]), ([1, 2], [700, 30])])
+def test_holes(dtype, new, kept):
+    check_attn(make(dtype, 4, 2, 64, 16, new, kept, holes=[(0, 1), (0, 4), (1, 0), (len(new) - 1, 0)]))
+
+
+@pytest.mark.parametrize("new", [[5, 4, 60], [2, 3, 4]])
+def test_tokens_without_a_place(new):
+    c = make(BF, 4, 2, 64, 16, new, [0, 3, 30], pad=3)
+    c.lens[0] = 1
+    c.N = 32
+    check_attn(c)
+    c = make(BF, 4, 2, 64, 16, new, [0, 3, 30], pad=3)
+    c.lens[1] = 0
+    check_attn(c, max_new=3)
+
+
+def test_many_sequences():
+    check_attn(make(BF, 2, 1, 64, 16, [i % 3 + (40 if i == 77 else 0) for i in range(150)], [i % 37 for i in range(150)]))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,kept", [([90], [20]), ([3], [600]), ([4, 2], [0, 31]), ([200], [0])])
+@pytest.mark.parametrize("window", [0, 40])
+def test_infinite_rows(dtype, D, new, kept, window):
+    """Infinite and NaN elements of the newest rows: earlier tokens do not see them, later ones do."""
+    c = make(dtype, 4, 2, D, 16, new, kept, seed=3)
+    for b, n in enumerate((c.lens - 1).tolist()):
+        for back, (what, value) in enumerate([("V", math.inf), ("K", math.nan), ("V", -math.inf), ("V", math.nan)]):
+            row = n - back
+            if row < 0 or back >= new[b]:
+                continue
+            p, r = ref.place(c.table, b, row, c.page, c.K.shape[0])
+            getattr(c, what)[p, 1 if back % 2 else 0, r, 5 + 40 * (back % 2)] = value
+    if window:
+        p, r = ref.place(c.table, 0, int(c.lens[0]) - new[0], c.page, c.K.shape[0])
+        c.V[p, 0, r, 33] = math.inf
+    check_attn(c, window=window)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_scores_of_minus_infinity(dtype):
+    c = make(dtype, 2, 1, 64, 16, [40, 1], [0, 20])
+    c.q = c.q.abs()
+    for n in range(3):
+        c.K[ref.place(c.table, 0, n, 16, c.K.shape[0])[0], :, n, 0] = -math.inf
+    c.K[ref.place(c.table, 1, 0, 16, c.K.shape[0])[0], :, :, 0] = -math.inf
+    check_attn(c)
+
+
+def test_large_scores_move_the_reference():
+    c = make(BF, 4, 2, 128, 16, [130, 1], [10, 500])
+    c.q = c.q * 6
+    check_attn(c, sm_scale=0.5)
+
+
+def test_attn_strides_and_no_lse():
+    c = on_gpu(make(BF, 4, 2, 64, 16, [20, 1], [7, 44]))
+    out, l = run_attn(c, 0.125)
+    # the same from rows in other places: K and V of a page side by side, heads inside rows, queries among other things
+    P = c.K.shape[0]
+    both = torch.full((P, 16, 2, 2, 64), math.nan, dtype=BF, device=DEV)
+    both[:, :, 0], both[:, :, 1] = c.cache.K.transpose(1, 2), c.cache.V.transpose(1, 2)
+    c.cache = tb.PagedCache(both[:, :, 0].transpose(1, 2), both[:, :, 1].transpose(1, 2), torch.cat((c.cache.table, c.cache.table), 1)[:, :c.table.shape[1]])
+    c.desc = tb.make_paged_desc(c.N, c.Hq, c.cache)
+    wide = torch.zeros((c.T, 7, 64), dtype=BF, device=DEV)
+    wide[:, 2:6] = c.q.to(DEV)
+    o = torch.full((c.T, 4, 128), 7.0, dtype=BF, device=DEV)
+    tb.tb_paged_attn(c.desc, c.cache, wide[:, 2:6], c.cu.to(DEV), c.lens.to(DEV), 20, 0.125, o[:, :, :64], None, tb.new_workspace(tb.TB_OP_PAGED_ATTN, c.desc, c.T))
+    assert torch.equal(o[:, :, :64], out) and bool((o[:, :, 64:] == 7).all())
+
+
+# ---- attention over lists ---------------------------------------------------------------------------
+def lists(c, k, seed=0):
+    gen = torch.Generator().manual_seed(seed)
+    n = int(c.lens.min())
+    idx = torch.stack([torch.stack([torch.randperm(n, generator=gen)[:k].sort().values for _ in range(c.Hq)]) for _ in range(c.B)]).to(torch.int32)
+    count = torch.randint(0, k + 1, (c.B, c.Hq), generator=gen, dtype=torch.int32)
+    count[0, 0], count[-1, -1] = k, 0
+    return idx, count
+
+
+def run_sparse(c, q, idx, count, most, tail, scale):
+    out, lse = torch.full((c.B, c.Hq, c.D), 7.0, device=DEV), torch.full((c.B, c.Hq), 7.0, device=DEV)
+    ws = tb.new_workspace(tb.TB_OP_ATTN, c.desc, most + tail[1] - tail[0])
+    tb.tb_sparse_decode_attn_paged(c.desc, c.cache, q.to(DEV), idx.to(DEV), count.to(DEV), most, scale, out, lse, ws, *tail)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,Hq,Hkv,n,k,tail", [(1, 8, 8, 300, 40, 0), (3, 8, 2, 500, 77, 5), (2, 8, 1, 2500, 1500, 1), (2, 32, 8, 2000, 900, 7), (1, 4, 4, 20, 0, 9)])
+def test_sparse(dtype, D, B, Hq, Hkv, n, k, tail):
+    c = on_gpu(make(dtype, Hq, Hkv, D, 16, [0] * B, [n] * B, seed=n))
+    q = torch.randn((B, Hq, D), generator=c.gen).to(dtype)
+    idx, count = lists(c, max(k, 1))
+    count = torch.minimum(count, torch.tensor(k, dtype=torch.int32))
+    tails = (n - tail, n)
+    out, lse = run_sparse(c, q, idx, count, k, tails, D ** -0.5)
+    want, l, mag = ref.sparse(q, c.K, c.V, c.table, idx, count, tails, D ** -0.5)
+    tol, tol_lse = attn_bounds(c, q, c.K, c.V, k + tail, D ** -0.5, mag, want, exact_weights=True)
+    close(out, want, tol + mag * 16 * 2.0 ** -24, "out")
+    close(lse, l, tol_lse + l.abs().nan_to_num(neginf=0, posinf=0) * 2.0 ** -22, "lse")
+    # the same rows in a contiguous cache: the same bits
+    rows = torch.arange(n)
+    at = c.table[:, rows // 16].long()
+    K, V = (x[at, :, (rows % 16).expand_as(at)].transpose(1, 2).contiguous().to(DEV) for x in (c.K, c.V))
+    d = tb.make_desc(n, Hq, K=K, V=V)
+    o2, l2 = torch.zeros_like(out), torch.zeros_like(lse)
+    tb.tb_sparse_decode_attn(d, q.to(DEV), K, V, idx.to(DEV), count.to(DEV), k, D ** -0.5, o2, l2, tb.new_workspace(tb.TB_OP_ATTN, d, k + tail), *tails)
+    assert torch.equal(out, o2) and torch.equal(lse, l2)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_sparse_holes_and_wild_entries(dtype):
+    c = on_gpu(make(dtype, 4, 2, 64, 16, [0, 0], [100, 100], holes=[(0, 1), (1, 5), (1, 6)]))
+    q = torch.randn((2, 4, 64), generator=c.gen).to(dtype)
+    idx, count = lists(c, 60)
+    idx[0, 1, :16], count[0, 1] = torch.arange(16, 32), 16  # in the hole alone
+    want, l, mag = ref.sparse(q, c.K, c.V, c.table, idx, count, (0, 0), 0.125)
+    out, lse = run_sparse(c, q, idx, count, 60, (0, 0), 0.125)
+    tol, tol_lse = attn_bounds(c, q, c.K, c.V, 60, 0.125, mag, want, exact_weights=True)
+    close(out, want, tol + mag * 16 * 2.0 ** -24)
+    close(lse, l, tol_lse + l.abs().nan_to_num(neginf=0) * 2.0 ** -22)
+    # entries that are no rows: the nearest row, nothing outside the sequence's pages
+    idx[1, 0, 0], idx[1, 0, 59], count[1, 0] = -2 ** 31, 2 ** 31 - 1, 60
+    out, _ = run_sparse(c, q, idx, count, 60, (0, 0), 0.125)
+    assert bool(torch.isfinite(out).all())
+
+
+# ---- together -----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_prompt_then_selected_steps(dtype):
+    """A prompt in two chunks, its keys projected, then a step that scores, selects and attends, all over the pages."""
+    B, Hq, Hkv, D, n, k = 2, 8, 2, 64, 300, 50
+    c = on_gpu(make(dtype, Hq, Hkv, D, 16, [n] * B, [0] * B))
+    c.cache.K.fill_(math.nan), c.cache.V.fill_(math.nan)
+    f = inv_freq(D)
+    W = (torch.randn((1, D, 16), generator=c.gen) / 8).to(dtype).to(DEV)
+    Kimp = torch.zeros((B, Hkv, 304, 16), dtype=dtype, device=DEV)
+    ws = tb.new_workspace(tb.TB_OP_PAGED_ATTN, c.desc, c.T)
+    out, q_rot, k_rot = torch.zeros((B, n, Hq, D), dtype=dtype), torch.zeros((B, n, Hq, D), dtype=dtype), torch.zeros((B, n, Hkv, D), dtype=dtype)
+    q, kk, v = (x.view(B, n, -1, D) for x in (c.q, c.k, c.v))
+    for lo, hi in ((0, 177), (177, 299), (299, 300)):
+        part = [x[:, lo:hi].reshape(B * (hi - lo), -1, D).to(DEV) for x in (q, kk, v)]
+        lens = torch.full((B,), hi, dtype=torch.int32, device=DEV)
+        qo, ko, o = torch.empty_like(part[0]), torch.empty_like(part[1]), torch.empty_like(part[0])
+        tb.tb_append_paged_kv(c.desc, c.cache, *part, None, lens, f.to(DEV), qo, ko)
+        tb.tb_paged_attn(c.desc, c.cache, qo, None, lens, hi - lo, D ** -0.5, o, None, ws)
+        rows = ko.view(B, hi - lo, Hkv, D).transpose(1, 2)
+        tb.tb_project_keys(tb.make_desc(hi - lo, Hq, K=rows, Kimp=Kimp[:, :, lo:hi]), rows, W, Kimp[:, :, lo:hi], 0, hi - lo)
+        for all_of, x in ((out, o), (q_rot, qo), (k_rot, ko)):
+            all_of[:, lo:hi] = x.cpu().view(B, hi - lo, -1, D)
+    K, V = c.cache.K.cpu(), c.cache.V.cpu()
+    want_q, want_k, _, _ = ref.append(c.q, c.k, c.v, c.K, c.V, c.table, c.cu, c.lens, c.N, f, False)
+    tol = 2.0 ** -21 * 12 + half_step(dtype) * 1.01 * 2
+    close(q_rot.view(B * n, Hq, D), want_q, tol * want_q.abs().clamp(min=1))
+    close(k_rot.view(B * n, Hkv, D), want_k, tol * want_k.abs().clamp(min=1))
+    want, _, mag = ref.attn(q_rot.view(B * n, Hq, D), K, V, c.table, c.cu, c.lens, c.N, D ** -0.5)
+    bound, _ = attn_bounds(c, q_rot, K, V, n, D ** -0.5, mag, want)
+    close(out.view(B * n, Hq, D), want, bound)
+    # the step
+    d = tb.make_desc(n, Hq, Kimp=Kimp, D=D)
+    q1 = q_rot[:, -1].contiguous()
+    q_imp = torch.matmul(q1.float().to(DEV), W[0].float()).to(dtype)
+    scores, idx, cnt = torch.zeros((B, Hq, 304), device=DEV), torch.zeros((B, Hq, k), dtype=torch.int32, device=DEV), torch.zeros((B, Hq), dtype=torch.int32, device=DEV)
+    tb.tb_score(d, q_imp, Kimp, 1.0, scores)
+    tb.tb_select_topk(d, scores, k - 6, 2, 4, idx, cnt, tb.new_workspace(tb.TB_OP_SELECT, d, k))
+    o, l = run_sparse(c, q1, idx, cnt, k, (0, 0), D ** -0.5)
+    want, lse, mag = ref.sparse(q1, K, V, c.table, idx.cpu(), cnt.cpu(), (0, 0), D ** -0.5)
+    tol, tol_lse = attn_bounds(c, q1, K, V, k, D ** -0.5, mag, want, exact_weights=True)
+    close(o, want, tol + mag * 16 * 2.0 ** -24)
+
+
+def test_captured_step_replays():
+    """A decode step (append, dense attention, attention over lists) in a graph, with other lengths and values at every replay."""
+    c = on_gpu(make(BF, 8, 2, 128, 16, [1, 1, 1], [600, 599, 20]))
+    f = inv_freq(128).to(DEV)
+    q, k, v = (x.to(DEV) for x in (c.q, c.k, c.v))
+    lens, idx, cnt = c.lens.to(DEV), torch.arange(20, dtype=torch.int32, device=DEV).expand(3, 8, 20).contiguous(), torch.full((3, 8), 20, dtype=torch.int32, device=DEV)
+    qo, out, lse = torch.zeros_like(q), torch.zeros_like(q), torch.zeros((3, 8), device=DEV)
+    so, sl = torch.zeros((3, 8, 128), device=DEV), torch.zeros((3, 8), device=DEV)
+    ws, ws2 = tb.new_workspace(tb.TB_OP_PAGED_ATTN, c.desc, 3), tb.new_workspace(tb.TB_OP_ATTN, c.desc, 20)
+
+    def step():
+        tb.tb_append_paged_kv(c.desc, c.cache, q, k, v, None, lens, f, qo)
+        tb.tb_paged_attn(c.desc, c.cache, qo, None, lens, 1, 0.09, out, lse, ws)
+        tb.tb_sparse_decode_attn_paged(c.desc, c.cache, qo, idx, cnt, 20, 0.09, so, sl, ws2)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(5):
+        lens.copy_(torch.tensor([601 - 90 * i, 600 - i, 21 - 5 * i], dtype=torch.int32))
+        q.copy_(torch.randn(c.q.shape, generator=c.gen))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (qo, out, lse, so, sl)]
+        for x in (qo, out, lse, so, sl):
+            x.zero_()
+        step()
+        torch.cuda.synchronize()
+        for x, y in zip(got, (qo, out, lse, so, sl)):
+            assert torch.equal(x, y)
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    a, b = (on_gpu(make(BF, 8, 2, 128, 16, [1, 30], [n, 200], seed=n)) for n in (900, 333))
+    want = [run_attn(x, 0.09) for x in (a, b)]
+    wss = [tb.new_workspace(tb.TB_OP_PAGED_ATTN, x.desc, x.T) for x in (a, b)]
+    ins = [(x.q.to(DEV), x.cu.to(DEV), x.lens.to(DEV), torch.zeros((x.T, 8, 128), dtype=BF, device=DEV), torch.zeros((x.T, 8), device=DEV)) for x in (a, b)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, ws, (q, cu, lens, o, l), st in zip((a, b), wss, ins, streams):
+            tb.tb_paged_attn(x.desc, x.cache, q, cu, lens, 30, 0.09, o, l, ws, stream=st)
+    torch.cuda.synchronize()
+    for (o, l), (_, _, _, o2, l2) in zip(want, ins):
+        assert torch.equal(o, o2) and torch.equal(l, l2)
+
+
+def test_one_workspace_for_calls_of_all_kinds():
+    """A workspace made for the most tokens serves every smaller call, one after the other, and is left as it was found."""
+    c = on_gpu(make(BF, 8, 2, 128, 16, [70, 1, 9], [300, 2000, 40]))
+    ws = tb.new_workspace(tb.TB_OP_PAGED_ATTN, c.desc, 500)
+    first = run_attn(c, 0.09, ws=ws)
+    for _ in range(3):
+        again = run_attn(c, 0.09, ws=ws)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+        x = on_gpu(make(BF, 8, 2, 128, 16, [1, 1, 1], [2000, 0, 500]))
+        alone, mixed = run_attn(x, 0.09), run_attn(x, 0.09, ws=ws)
+        assert torch.equal(alone[0], mixed[0]) and torch.equal(alone[1], mixed[1])
