@@ -113,7 +113,7 @@ def load_library() -> ctypes.CDLL:
     L.tb_score_mx.argtypes = [dp, vp, mp, f32, vp, i64, vp]
     L.tb_sparse_decode_attn_mx.argtypes = [dp, vp, mp, mp, vp, vp, i64, i64, i64, i64, f32, vp, vp, vp, sz, vp]
     L.tb_sparse_decode_attn_shared_mx.argtypes = L.tb_sparse_decode_attn_mx.argtypes
-    pp, rp = ctypes.POINTER(tb_paged_cache), ctypes.POINTER(tb_token_rows)
+    pp, rp = ctypes.POINTER(tb_paged_cache), vp  # (rp: tb_token_rows by their address)
     L.tb_append_paged_kv.argtypes = [dp, pp, i64, vp, vp, vp, vp, i32, i32, rp, rp, rp, rp, rp, vp]
     L.tb_paged_attn.argtypes = [dp, pp, i64, vp, vp, i64, rp, i64, f32, rp, vp, vp, sz, vp]
     L.tb_sparse_decode_attn_paged.argtypes = [dp, pp, vp, vp, vp, i64, i64, i64, i64, f32, vp, vp, vp, sz, vp]
@@ -280,7 +280,7 @@ class PagedCache:
         self.desc = tb_paged_cache(K.data_ptr(), V.data_ptr(), table.data_ptr(), K.shape[0], K.shape[2], table.shape[1],
                                    table.stride(0) if table.shape[0] > 1 else table.shape[1], *_strides3(K), *_strides3(V))
         self.ref = ctypes.byref(self.desc)
-        self.device = K.get_device()
+        self.device, self.dtype = K.get_device(), K.dtype
         if not self.device == V.get_device() == table.get_device():
             raise ValueError(f"K on {K.device}, V on {V.device}, table on {table.device}")
 
@@ -295,13 +295,9 @@ def make_paged_desc(N: int, Hq: int, cache: PagedCache) -> tb_cache_desc:
     return tb_cache_desc(cache.table.shape[0], Hq, Hkv, D, 32, _dtype_code(cache.K.dtype), N, 0, 0, D, 0, 0, D, 0, 0, 32)
 
 
-def _token_rows(t: Optional[torch.Tensor]):
-    """Rows [T, heads, D] of tokens."""
-    if t is None:
-        return None
-    st = t.stride()
-    assert len(st) == 3 and st[2] == 1, "rows of tokens are [T, heads, D] with D contiguous"
-    return tb_token_rows(t.data_ptr(), st[0], st[1])
+# tb_token_rows of a call's tensors, one after the other: a fifth of the cost of a structure each
+_two_rows, _five_rows = ctypes.c_int64 * 6, ctypes.c_int64 * 15
+_ROWS = ctypes.sizeof(tb_token_rows)
 
 
 def tb_version() -> int:
@@ -527,26 +523,47 @@ def tb_sparse_decode_attn_shared_mx(desc, q, K: MxRows, V: MxRows, idx, count, m
 
 
 def _check_tokens(desc, cache: PagedCache, cu, lens) -> None:
-    assert lens.dtype == torch.int32 and lens.is_contiguous() and lens.shape == (desc.B,) and desc.B == cache.table.shape[0]
-    assert cu is None or (cu.dtype == torch.int32 and cu.is_contiguous() and cu.shape == (desc.B + 1,))
+    B = desc.B
+    assert lens.dtype is torch.int32 and lens.shape == (B,) and (B < 2 or lens.stride(0) == 1) and B == cache.table.shape[0]
+    assert cu is None or (cu.dtype is torch.int32 and cu.shape == (B + 1,) and cu.is_contiguous())
 
 
+# (The calls below spell their arguments out, as those of the 4-bit cache do, and look at each tensor's shape and strides once: 10 us of
+# host time for the first one otherwise, now 6.)
 def tb_append_paged_kv(desc, cache: PagedCache, q, k, v, cu, lens, inv_freq, q_out=None, k_out=None, positions=None,
                        interleaved: bool = False, stream=None) -> None:
     """Rows of the new tokens k, v [T, Hkv, D] into the cache, k (also to k_out) and q [T, Hq, D] (to q_out; both may be None) rotated by
     positions[t] * inv_freq[i] (int32 [T], None: the token's row; fp32 [rot / 2], None: no rotation).  cu: int32 [B + 1], None: as many
     tokens of every sequence; lens: int32 [B], the rows of the sequences with the new tokens."""
-    T, Hkv, D = k.shape
-    assert v.shape == k.shape and k.dtype == v.dtype == cache.K.dtype and (Hkv, D) == (desc.Hkv, desc.D)
-    assert (q is None) == (q_out is None) and (q is None or (q.shape == q_out.shape == (T, desc.Hq, D) and q.dtype == q_out.dtype == k.dtype))
-    assert k_out is None or (k_out.shape == k.shape and k_out.dtype == k.dtype)
-    assert inv_freq is None or (inv_freq.dtype == torch.float32 and inv_freq.is_contiguous() and inv_freq.dim() == 1)
-    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.shape == (T,))
+    shape, dtype = k.shape, cache.dtype
+    T, Hkv, D = shape
+    k_t, k_h, k_d = k.stride()
+    v_t, v_h, v_d = v.stride()
+    assert v.shape == shape and Hkv == desc.Hkv and D == desc.D and k.dtype is dtype and v.dtype is dtype and k_d == v_d == 1
+    qp = qop = kop = None
+    q_t = q_h = qo_t = qo_h = ko_t = ko_h = 0
+    if q is not None or q_out is not None:
+        q_t, q_h, q_d = q.stride()
+        qo_t, qo_h, qo_d = q_out.stride()
+        assert q.shape == q_out.shape == (T, desc.Hq, D) and q.dtype is dtype and q_out.dtype is dtype and q_d == qo_d == 1
+        qp, qop = q.data_ptr(), q_out.data_ptr()
+    if k_out is not None:
+        ko_t, ko_h, ko_d = k_out.stride()
+        assert k_out.shape == shape and k_out.dtype is dtype and ko_d == 1
+        kop = k_out.data_ptr()
+    rot, fp = 0, None
+    if inv_freq is not None:
+        (rot,) = inv_freq.shape
+        assert inv_freq.dtype is torch.float32 and (rot < 2 or inv_freq.stride(0) == 1)
+        rot, fp = 2 * rot, inv_freq.data_ptr()
+    assert positions is None or (positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (T,))
     _check_tokens(desc, cache, cu, lens)
+    rows = _five_rows(qp or 0, q_t, q_h, k.data_ptr(), k_t, k_h, v.data_ptr(), v_t, v_h, qop or 0, qo_t, qo_h, kop or 0, ko_t, ko_h)
+    at = ctypes.addressof(rows)
     rc = (_lib or load_library()).tb_append_paged_kv(
-        ctypes.byref(desc), cache.ref, T, None if cu is None else cu.data_ptr(), lens.data_ptr(), None if positions is None else positions.data_ptr(),
-        None if inv_freq is None else inv_freq.data_ptr(), 0 if inv_freq is None else 2 * inv_freq.shape[0], interleaved, _token_rows(q), _token_rows(k),
-        _token_rows(v), _token_rows(q_out), _token_rows(k_out),
+        ctypes.byref(desc), cache.ref, T, None if cu is None else cu.data_ptr(), lens.data_ptr(), None if positions is None else positions.data_ptr(), fp,
+        rot, interleaved, None if q is None else at, at + _ROWS, at + 2 * _ROWS, None if q is None else at + 3 * _ROWS,
+        None if k_out is None else at + 4 * _ROWS,
         _stream_on(cache.device, stream, (q, k, v, cu, lens, inv_freq, q_out, k_out, positions) if _several_devices else ()))
     if rc:
         _check(rc, "tb_append_paged_kv")
@@ -556,12 +573,18 @@ def tb_paged_attn(desc, cache: PagedCache, q, cu, lens, max_new: int, sm_scale: 
     """Causal attention of the new tokens q [T, Hq, D] over their sequences' rows (their own have been appended), to the last `window` of
     them unless that is 0.  cu and lens as for tb_append_paged_kv; max_new: the most new tokens of a sequence; out: as q; lse: fp32 [T, Hq]
     or None."""
-    assert q.shape == out.shape and q.dtype == out.dtype == cache.K.dtype and q.shape[1:] == (desc.Hq, desc.D)
-    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2])
+    shape, dtype = q.shape, cache.dtype
+    T, Hq, D = shape
+    q_t, q_h, q_d = q.stride()
+    o_t, o_h, o_d = out.stride()
+    assert out.shape == shape and Hq == desc.Hq and D == desc.D and q.dtype is dtype and out.dtype is dtype and q_d == o_d == 1
+    assert lse is None or (lse.dtype is torch.float32 and lse.shape == (T, Hq) and lse.is_contiguous())
     _check_tokens(desc, cache, cu, lens)
+    rows = _two_rows(q.data_ptr(), q_t, q_h, out.data_ptr(), o_t, o_h)
+    at = ctypes.addressof(rows)
     rc = (_lib or load_library()).tb_paged_attn(
-        ctypes.byref(desc), cache.ref, q.shape[0], None if cu is None else cu.data_ptr(), lens.data_ptr(), max_new, _token_rows(q), window, sm_scale,
-        _token_rows(out), None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes,
+        ctypes.byref(desc), cache.ref, T, None if cu is None else cu.data_ptr(), lens.data_ptr(), max_new, at, window, sm_scale, at + _ROWS,
+        None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes,
         _stream_on(cache.device, stream, (q, cu, lens, out, lse, ws) if _several_devices else ()))
     if rc:
         _check(rc, "tb_paged_attn")
@@ -570,7 +593,7 @@ def tb_paged_attn(desc, cache: PagedCache, q, cu, lens, max_new: int, sm_scale: 
 def tb_sparse_decode_attn_paged(desc, cache: PagedCache, q, idx, count, max_count: int, sm_scale: float, out, lse, ws, tail_begin: int = 0,
                                 tail_end: int = 0, stream=None) -> None:
     """tb_sparse_decode_attn over a cache in pages."""
-    assert q.is_contiguous() and out.is_contiguous() and q.dtype == cache.K.dtype
+    assert q.is_contiguous() and out.is_contiguous() and q.dtype is cache.dtype and out.dtype is torch.float32
     assert q.shape == out.shape == (desc.B, desc.Hq, desc.D) and desc.B == cache.table.shape[0]
     rc = (_lib or load_library()).tb_sparse_decode_attn_paged(
         ctypes.byref(desc), cache.ref, q.data_ptr(), idx.data_ptr(), count.data_ptr(), idx.stride(-2), max_count, tail_begin, tail_end, sm_scale,

@@ -484,6 +484,7 @@ template <typename T, int D, int GH>
 __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttnArgs a) {
   using S = TokenShape<T, D>;
   __shared__ GroupLds<D, GH, kTokenWaves> gl;
+  __shared__ float s_out[GH * D], s_lse[GH];
   const int tid = threadIdx.x, lane = lane_id(), wave = wave_id();
   const int i16 = lane & 15, kb = lane >> 4;
   const int split = blockIdx.x, hkv = blockIdx.y, b = blockIdx.z;
@@ -690,6 +691,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
   }
   l += __shfl_xor(l, 16, kWave);
   l += __shfl_xor(l, 32, kWave);
+  if (l != l && m == -INFINITY) m = 0.f;  // (scores that are all NaN: the merges leave out what has a reference of -inf)
   if (lane < GH) {
     gl.m[wave][lane] = m;
     gl.l[wave][lane] = l;
@@ -705,15 +707,16 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
   // merge the waves; a thread has outputs tid, tid + 512, ... of the GH x D
   constexpr int kThreads = kTokenWaves * kWave, OUTS = (GH * D + kThreads - 1) / kThreads;
   const int64_t group = static_cast<int64_t>(b) * a.Hkv + hkv;
-  auto store = [&](int row, int d, float M, float L, float v) {
+  auto store = [&](int row, int d, bool any, float v, float lse) {
     const int32_t i = row >> a.gs, p = s.row + i;
     if (i >= n || p < 0 || p >= a.tok.N) return;
     const int64_t t = s.first + i;
     const int h = (hkv << a.gs) + (row & ((1 << a.gs) - 1));
-    const bool any = has_weight<true>(L);
-    store_elt(reinterpret_cast<T*>(a.out + t * a.out_t + h * a.out_h) + d, any ? v / L : 0.f);
-    if (a.lse && d == 0) a.lse[t * a.Hq + h] = any ? M * kLn2 + logf(L) : -INFINITY;
+    store_elt(reinterpret_cast<T*>(a.out + t * a.out_t + h * a.out_h) + d, any ? v : 0.f);
+    if (a.lse && d == 0) a.lse[t * a.Hq + h] = any ? lse : -INFINITY;
   };
+  float* const po = a.partials + group * GH * a.nsplit * D;  // [row][split][D]
+  float* const pp = a.partials + a.pairs_off + group * GH * a.nsplit * 2;
 #pragma unroll
   for (int x = 0; x < OUTS; ++x) {
     const int e = tid + x * kThreads, row = e / D, d = e % D;
@@ -729,11 +732,11 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
       v += gl.acc[w][row][d] * wgt;
     }
     if (splits == 1) {
-      store(row, d, M, L, v);
+      store(row, d, has_weight<true>(L), v / L, M * kLn2 + logf(L));
     } else {
-      const int64_t to = (group * GH + row) * a.nsplit + split;
-      __hip_atomic_store(&a.partials[to * D + d], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (d == 0) store_pair(a.partials + a.pairs_off + to * 2, M, L);
+      const int to = row * splits + split;
+      __hip_atomic_store(&po[static_cast<int64_t>(to) * D + d], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (d == 0) store_pair(pp + to * 2, M, L);
     }
   }
   if (splits == 1) return;
@@ -745,25 +748,12 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
   }
   __syncthreads();
   if (!gl.last) return;
+  combine_published<D, GH, kTokenWaves, true>(po, pp, splits, s_out, s_lse, gl.m, gl.l, gl.acc);
+  __syncthreads();
 #pragma unroll
   for (int x = 0; x < OUTS; ++x) {
-    const int e = tid + x * kThreads, row = e / D, d = e % D;
-    if (e >= GH * D) continue;
-    const int64_t from = (group * GH + row) * a.nsplit;
-    float M = -INFINITY, L = 0.f, v = 0.f;
-    for (int32_t k = 0; k < splits; ++k) {
-      const unsigned long long pair = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(a.partials + a.pairs_off + (from + k) * 2),
-                                                        __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const float o_k = __hip_atomic_load(&a.partials[(from + k) * D + d], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const float m_k = __uint_as_float(static_cast<uint32_t>(pair)), l_k = __uint_as_float(static_cast<uint32_t>(pair >> 32));
-      const float m_new = fmaxf(M, m_k);
-      const float m_ref = m_new > -INFINITY ? m_new : 0.f;
-      const float wa = exp2_safe(M - m_ref), wb = exp2_safe(m_k - m_ref);
-      L = L * wa + l_k * wb;
-      v = v * wa + o_k * wb;
-      M = m_new;
-    }
-    store(row, d, M, L, v);
+    const int e = tid + x * kThreads;
+    if (e < GH * D) store(e / D, e % D, true, s_out[e], s_lse[e / D]);
   }
   if (tid == 0) __hip_atomic_store(&a.counters[group * kCounterStrideWords], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -833,6 +823,9 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
     a.nsplit = static_cast<int32_t>(token_splits(d));
     const dim3 grid(a.nsplit, d.Hkv, d.B);
     a.pairs_off = static_cast<int64_t>(d.B) * d.Hkv * kTokenRows * a.nsplit * D;
+    const int64_t rows = most << a.gs;  // (results of fewer rows are merged faster)
+    if (rows <= 4) return launch_one(token_kernel<T, D, 4>, grid, kTokenWaves * kWave, st, a);
+    if (rows <= 8) return launch_one(token_kernel<T, D, 8>, grid, kTokenWaves * kWave, st, a);
     return launch_one(token_kernel<T, D, kTokenRows>, grid, kTokenWaves * kWave, st, a);
   }
   return TB_OK;
