@@ -192,7 +192,6 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
   const int my_h = (hkv << a.gs) + (row & ((1 << a.gs) - 1));
   // and the rows that the wave's see
   const int32_t w_first = max(s.row + i0 + (wave * 32 >> a.gs), p_first), w_last = min(s.row + i0 + ((wave * 32 + 31) >> a.gs), p_last);
-  const int32_t w_see = a.window ? max(w_first - a.window + 1, 0) : 0;
   u32x4 q[S::PAIRS];
 #pragma unroll
   for (int c = 0; c < S::PAIRS; ++c) {
@@ -214,24 +213,42 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
   constexpr unsigned long long kAll = ~0ull;
   const char* const kh = a.pages.K + hkv * a.pages.k_h;
   const char* const vh = a.pages.V + hkv * a.pages.v_h;
+  // A wave loads a quarter of the tile's rows: 8 or 16, which lie in one page.
+  constexpr int MY_ROWS = S::LOADS * S::AT_ONCE;
+  static_assert(16 % MY_ROWS == 0, "rows of a wave lie in one page");
+  const int lane_row = lane / S::PIECES, piece = lane % S::PIECES;
+  const uint32_t k_lane = lane_row * a.pages.k_n, v_lane = lane_row * a.pages.v_n;
   auto stage = [&](char* sk, char* sv, int32_t t, int32_t page, unsigned long long there) {
+    const int32_t pg = max(__builtin_amdgcn_readlane(page, wave * MY_ROWS), 0);
+    const uint32_t in_page = static_cast<uint32_t>(t * S::KEYS + wave * MY_ROWS) & ((1u << a.pages.shift) - 1);
+    const char* k = kh + pg * a.pages.k_p + static_cast<uint64_t>(in_page) * a.pages.k_n;
+    const char* v = vh + pg * a.pages.v_p + static_cast<uint64_t>(in_page) * a.pages.v_n;
+    sk += wave * MY_ROWS * S::ROW;
+    sv += wave * MY_ROWS * S::ROW;
+    auto load = [](const char* from, char* to) {
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+    };
+    if (there == kAll) {
 #pragma unroll
-    for (int x = 0; x < S::LOADS; ++x) {
-      const int r0 = (wave * S::LOADS + x) * S::AT_ONCE, r = r0 + lane / S::PIECES, piece = lane % S::PIECES;
-      const int64_t pg = __builtin_amdgcn_readlane(page, r0);  // (at most eight rows: one page)
-      const uint32_t in_page = static_cast<uint32_t>(t * S::KEYS + r0) & ((1u << a.pages.shift) - 1);
-      const char* k = kh + pg * a.pages.k_p + static_cast<uint64_t>(in_page) * a.pages.k_n;
-      const char* v = vh + pg * a.pages.v_p + static_cast<uint64_t>(in_page) * a.pages.v_n;
-      const uint32_t ko = (lane / S::PIECES) * a.pages.k_n + (piece ^ S::k_swizzle(r)) * 16;
-      const uint32_t vo = (lane / S::PIECES) * a.pages.v_n + (piece ^ S::v_swizzle(r)) * 16;
-      const char* kp = k + ko;
-      const char* vp = v + vo;
-      if (there != kAll && !(there >> r & 1)) {
-        kp = reinterpret_cast<const char*>(zero_row) + piece * 16;
-        vp = kp;
+      for (int x = 0; x < S::LOADS; ++x) {
+        const int r = wave * MY_ROWS + x * S::AT_ONCE + lane_row;
+        load(k + (k_lane + (piece ^ S::k_swizzle(r)) * 16), sk + x * 1024);
+        load(v + (v_lane + (piece ^ S::v_swizzle(r)) * 16), sv + x * 1024);
+        k += S::AT_ONCE * static_cast<uint64_t>(a.pages.k_n);
+        v += S::AT_ONCE * static_cast<uint64_t>(a.pages.v_n);
       }
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)kp, (__attribute__((address_space(3))) void*)(sk + r0 * S::ROW), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)vp, (__attribute__((address_space(3))) void*)(sv + r0 * S::ROW), 16, 0, 0);
+    } else {
+#pragma clang loop unroll(disable)
+      for (int x = 0; x < S::LOADS; ++x) {
+        const int r = wave * MY_ROWS + x * S::AT_ONCE + lane_row;
+        const char* kp = k + (k_lane + (piece ^ S::k_swizzle(r)) * 16);
+        const char* vp = v + (v_lane + (piece ^ S::v_swizzle(r)) * 16);
+        const bool is = (there >> r & 1) != 0;
+        load(is ? kp : reinterpret_cast<const char*>(zero_row), sk + x * 1024);
+        load(is ? vp : reinterpret_cast<const char*>(zero_row), sv + x * 1024);
+        k += S::AT_ONCE * static_cast<uint64_t>(a.pages.k_n);
+        v += S::AT_ONCE * static_cast<uint64_t>(a.pages.v_n);
+      }
     }
   };
 
@@ -242,37 +259,90 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
   float m = -INFINITY, l = 0.f;  // (l: of this half's keys)
 
-  auto work = [&](const char* sk, const char* sv, int32_t t, unsigned long long there) {
+  // Where a lane reads: of K piece `half` of its row (pieces 2 c + half: the address with 32 c flipped), of V for columns 0 .. 31 (32 d ..: with
+  // 32 d elements flipped); rows that are multiples of 8 further differ by a constant.
+  const int k_at = col * S::ROW + ((half ^ S::k_swizzle(col)) * 16);
+  const int v_row = S::F32 ? 4 * half : 4 * half + (lane & 15) / 4;
+  const int v_piece = S::F32 ? col / 4 : 2 * (lane >> 4 & 1) + (lane & 3) / 2;
+  const int v_at = v_row * S::ROW + ((v_piece ^ S::v_swizzle(v_row)) * 16) + (S::F32 ? (col & 3) * 4 : (lane & 1) * 8);
+  // (hidden from the compiler, which would keep all that follows from them in registers)
+  auto hidden = [](int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+  };
+  // Pieces of K for the first product: number f is the piece pair f % PAIRS of the block f / PAIRS of 32 keys.
+  constexpr int PIECE_PAIRS = KB * S::PAIRS;
+  constexpr int AHEAD = S::F32 && D == 128 ? 0 : PIECE_PAIRS / 2;  // of them are read while the tile before is finished: as many as registers allow
+  u32x4 kf[PIECE_PAIRS];
+  auto read_k = [&](const char* sk, auto ahead_tag) {
+    constexpr bool FIRST = decltype(ahead_tag)::value;
+    const int at = hidden(k_at);
+#pragma unroll
+    for (int f = FIRST ? 0 : AHEAD; f < (FIRST ? AHEAD : PIECE_PAIRS); ++f)
+      kf[f] = *reinterpret_cast<const u32x4*>(sk + (at ^ (f % S::PAIRS * 32)) + f / S::PAIRS * 32 * S::ROW);
+  };
+  // The tile t from sk, sv; then `between`, which makes the next one there; then it begins to read that from sk_next.
+  auto work = [&](const char* sk, const char* sv, const char* sk_next, int32_t t, unsigned long long there, auto&& between) {
     const int32_t first = t * S::KEYS;
-    if (first > w_last || first + S::KEYS <= w_see || w_first > w_last) return;  // nothing that the wave's rows see
     f32x16 x[KB];
+    read_k(sk, std::false_type{});
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < KB; ++k) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[k][r] = 0.f;
 #pragma unroll
       for (int c = 0; c < S::PAIRS; ++c) {
-        const int r = k * 32 + col;
-        const u32x4 kk = *reinterpret_cast<const u32x4*>(sk + r * S::ROW + (((2 * c + half) ^ S::k_swizzle(r)) * 16));
         if constexpr (S::F32) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[k] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kk[e]), __uint_as_float(q[c][e]), x[k], 0, 0, 0);
+          for (int e = 0; e < 4; ++e)
+            x[k] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[k * S::PAIRS + c][e]), __uint_as_float(q[c][e]), x[k], 0, 0, 0);
         } else {
-          x[k] = mfma32(kk, q[c], x[k]);
+          x[k] = mfma32(kf[k * S::PAIRS + c], q[c], x[k]);
         }
       }
     }
-    const bool masked = there != kAll || first + S::KEYS - 1 > w_first || (a.window && first <= w_last - a.window);
-    if (masked) {
+    __builtin_amdgcn_sched_barrier(0);
+    // V's operands, of bf16 a column of four rows a lane, transposed on the way: one half of its columns while the weights are computed, the
+    // other under the products with the first
+    constexpr int VF = S::F32 ? 4 * KB : 2 * KB;  // steps of 16 keys (bf16), four of one key a half (fp32)
+    const int at_v = hidden(v_at);
+    auto read_v = [&](u32x4(&vf)[DB / 2][VF], int d0) {
 #pragma unroll
-      for (int k = 0; k < KB; ++k)
+      for (int j = 0; j < VF; ++j)
+#pragma unroll
+        for (int d = 0; d < DB / 2; ++d) {
+          const char* from = sv + (at_v ^ ((d0 + d) * 32 * static_cast<int>(sizeof(T)))) + j * (S::F32 ? 8 : 16) * S::ROW;
+          if constexpr (S::F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vf[d][j][e] = *reinterpret_cast<const uint32_t*>(from + e * S::ROW);
+          } else {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_char*)(from + 8 * y * S::ROW));
+              uint32_t w2[2];
+              __builtin_memcpy(w2, &w, 8);
+              vf[d][j][2 * y] = w2[0];
+              vf[d][j][2 * y + 1] = w2[1];
+            }
+          }
+        }
+    };
+    u32x4 v0[DB / 2][VF], v1[DB / 2][VF];
+    read_v(v0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    if (there != kAll || first + S::KEYS - 1 > w_first || (a.window && first <= w_last - a.window)) {
+      // keys behind `low` up to `high`, by the number that a register has in both halves
+      const int high = my_p - first - 4 * half, low = max(my_low - first - 4 * half, -1);
+#pragma unroll
+      for (int k = 0; k < KB; ++k) {
+        const uint32_t is = static_cast<uint32_t>(there >> 32 * k) >> 4 * half;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int kr = 32 * k + 8 * (r / 4) + 4 * half + r % 4;
-          const int32_t key = first + kr;
-          const bool seen = (key <= my_p) & (key > my_low) & ((there >> kr & 1) != 0);
-          x[k][r] = seen ? x[k][r] : -INFINITY;
+          const int kr = 8 * (r / 4) + r % 4;
+          x[k][r] = ((32 * k + kr <= high) & (32 * k + kr > low) & ((is & 1u << kr) != 0)) ? x[k][r] : -INFINITY;
         }
+      }
     }
     float top = x[0][0];
 #pragma unroll
@@ -281,7 +351,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
       for (int r = 0; r < 16; ++r) top = fmaxf(top, x[k][r]);
     top = fmaxf(top, other_half(top)) * a.scale_log2;  // (-inf times a scale of 0 does not come up: that is 1 then)
     if (ballot64(top > m + kLazy)) {
-      // (nothing seen yet: sums are 0, or what the guard has put there)
+      // (nothing seen yet: the sums are 0)
       const float m_new = fmaxf(m, top), alpha = m > -INFINITY ? exp2_safe(m - m_new) : 1.f;
       l *= alpha;
 #pragma unroll
@@ -298,100 +368,107 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
         x[k][r] = exp2_safe(fmaf(x[k][r], a.scale_log2, -m_ref));
         l += x[k][r];
       }
-    // output: keys 16 j .. + 15 (bf16), or one key a half (fp32), a step
+    u32x4 p[S::F32 ? 1 : 2 * KB];
+    if constexpr (!S::F32) {
 #pragma unroll
-    for (int d = 0; d < DB; ++d) {
-      if constexpr (S::F32) {
+      for (int j = 0; j < 2 * KB; ++j)
 #pragma unroll
-        for (int k = 0; k < KB; ++k)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int kr = 32 * k + 8 * (r / 4) + 4 * half + r % 4;
-            const float v = *reinterpret_cast<const float*>(sv + kr * S::ROW + (((8 * d + col / 4) ^ S::v_swizzle(kr)) * 16) + (col & 3) * 4);
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, x[k][r], o[d], 0, 0, 0);
-          }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 2 * KB; ++j) {
-          u32x4 v, p;
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const int kr = 16 * j + 8 * y + 4 * half + (lane & 15) / 4;
-            const int piece = 4 * d + 2 * (lane >> 4 & 1) + (lane & 3) / 2;
-            const char* at16 = sv + kr * S::ROW + ((piece ^ S::v_swizzle(kr)) * 16) + (lane & 1) * 8;
-            const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_char*)at16);
-            uint32_t w2[2];
-            __builtin_memcpy(w2, &w, 8);
-            v[2 * y] = w2[0];
-            v[2 * y + 1] = w2[1];
-          }
-#pragma unroll
-          for (int y = 0; y < 4; ++y) p[y] = bf16x2(x[j / 2][8 * (j & 1) + 2 * y], x[j / 2][8 * (j & 1) + 2 * y + 1]);
-          o[d] = mfma32(v, p, o[d]);
+        for (int y = 0; y < 4; ++y) {
+          uint32_t w = bf16x2(x[j / 2][8 * (j & 1) + 2 * y], x[j / 2][8 * (j & 1) + 2 * y + 1]);
+          asm volatile("" : "+v"(w));  // (now, not behind the barrier: the scores' registers are wanted)
+          p[j][y] = w;
         }
-      }
     }
+    auto products = [&](const u32x4(&vf)[DB / 2][VF], int d0) {
+#pragma unroll
+      for (int j = 0; j < VF; ++j)
+#pragma unroll
+        for (int d = 0; d < DB / 2; ++d) {
+          if constexpr (S::F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              o[d0 + d] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(vf[d][j][e]), x[j / 4][4 * (j % 4) + e], o[d0 + d], 0, 0, 0);
+          } else {
+            o[d0 + d] = mfma32(vf[d][j], p[j], o[d0 + d]);
+          }
+        }
+    };
+    __builtin_amdgcn_sched_barrier(0);
+    read_v(v1, DB / 2);
+    __builtin_amdgcn_sched_barrier(0);
+    products(v0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    between();
+    __builtin_amdgcn_sched_barrier(0);
+    read_k(sk_next, std::true_type{});
+    __builtin_amdgcn_sched_barrier(0);
+    products(v1, DB / 2);
   };
   // A tile with rows that some of the workgroup's do not see: what is infinite or NaN there would be NaN times a weight of 0.  Such
-  // elements are added to the sums of those that see them, and are zeros for the products.  (All waves come here.)
-  auto guard = [&](char* sv, int32_t t, unsigned long long there) {
-    const int32_t first = t * S::KEYS;
-    if (there == kAll && first + S::KEYS - 1 <= p_first && !(a.window && first <= p_last - a.window)) return;
+  // elements are zeros for the products, and are added in the end to the sums of those that see them.  (All waves come here.)
+  bool specials = false;
+  auto partly_seen = [&](int32_t first) { return first + S::KEYS - 1 > p_first || (a.window && first <= p_last - a.window); };
+  auto guard = [&](char* sv, int32_t t) {
+    if (!partly_seen(t * S::KEYS)) return;
     uint32_t most = 0;
-    for (int i = threadIdx.x * 16; i < S::TILE; i += kChunkThreads * 16) most = largest_exponent<T>(*reinterpret_cast<const u32x4*>(sv + i), most);
+    const int at = hidden(threadIdx.x * 16);
+    for (int i = at; i < S::TILE; i += kChunkThreads * 16) most = largest_exponent<T>(*reinterpret_cast<const u32x4*>(sv + i), most);
     if (__builtin_expect(!__syncthreads_or(most == kExponent), 1)) return;
-    for (int kr = 0; kr < S::KEYS; ++kr) {
-      const int32_t key = first + kr;
-      const bool seen = mine & (key <= my_p) & (key > my_low) & ((there >> kr & 1) != 0);
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int c = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
-          const float v = to_float(*reinterpret_cast<const T*>(sv + kr * S::ROW + (((c * static_cast<int>(sizeof(T)) / 16) ^ S::v_swizzle(kr)) * 16) +
-                                                               c * sizeof(T) % 16));
-          o[d][r] += seen ? not_finite_or_zero(v) : 0.f;
-        }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x * 16; i < S::TILE; i += kChunkThreads * 16)
+    specials = true;
+    for (int i = at; i < S::TILE; i += kChunkThreads * 16)
       *reinterpret_cast<u32x4*>(sv + i) = finite_or_zero<T>(*reinterpret_cast<const u32x4*>(sv + i));
     __syncthreads();
   };
 
-  int32_t page = -1;
-  unsigned long long there = 0;
+  // Two tiles are in LDS, or on their way there; when all waves have read one, the next but one takes its place.  (Past the end the same bytes
+  // are read once more, for nothing.)
+  const int32_t tile_first = tile;
   if (tile < tile_end) {
-    page = pages_of_tile(tile);
-    there = rows_there(tile, page);
+    int32_t page = pages_of_tile(tile), page_next = pages_of_tile(tile + 1);
+    unsigned long long there = rows_there(tile, page), next = rows_there(tile + 1, page_next);
     stage(s_k0, s_v0, tile, page, there);
-    page = pages_of_tile(tile + 1);
-  }
-  while (tile < tile_end) {
-    __builtin_amdgcn_s_waitcnt(0);
+    if (tile + 1 < tile_end) stage(s_k1, s_v1, tile + 1, page_next, next);
+    page = pages_of_tile(tile + 2);
+    auto step = [&](char* sk, char* sv, char* sk_next) {
+      guard(sv, tile);
+      work(sk, sv, sk_next, tile, there, [&]() {
+        __syncthreads();  // all have read the tile, and the next one has arrived
+        there = next;
+        next = rows_there(tile + 2, page);
+        if (tile + 2 < tile_end) {
+          stage(sk, sv, tile + 2, page, next);
+          page = pages_of_tile(tile + 3);
+        }
+      });
+    };
     __syncthreads();
-    unsigned long long next = rows_there(tile + 1, page);
-    if (tile + 1 < tile_end) {
-      stage(s_k1, s_v1, tile + 1, page, next);
-      page = pages_of_tile(tile + 2);
+    read_k(s_k0, std::true_type{});
+    while (true) {
+      step(s_k0, s_v0, s_k1);
+      if (++tile >= tile_end) break;
+      step(s_k1, s_v1, s_k0);
+      if (++tile >= tile_end) break;
     }
-    guard(s_v0, tile, there);
-    work(s_k0, s_v0, tile, there);
-    if (++tile >= tile_end) break;
-    there = next;
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    next = rows_there(tile + 1, page);
-    if (tile + 1 < tile_end) {
-      stage(s_k0, s_v0, tile + 1, page, next);
-      page = pages_of_tile(tile + 2);
-    }
-    guard(s_v1, tile, there);
-    work(s_k1, s_v1, tile, there);
-    ++tile;
-    there = next;
   }
 
+  if (__builtin_expect(specials, 0)) {
+    for (int32_t t = tile_first; t < tile_end; ++t) {
+      if (!partly_seen(t * S::KEYS)) continue;
+      for (int32_t key = max(t * S::KEYS, see_first); key <= min(t * S::KEYS + S::KEYS - 1, p_last); ++key) {
+        const int32_t pg = table[key >> a.pages.shift];
+        if (pg < 0 || pg >= a.pages.pages) continue;
+        const char* from = vh + pg * a.pages.v_p + static_cast<uint64_t>(key & ((1 << a.pages.shift) - 1)) * a.pages.v_n + 4 * half * sizeof(T);
+        const bool seen = mine & (key <= my_p) & (key > my_low);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float v = to_float(reinterpret_cast<const T*>(from)[32 * d + 8 * (r / 4) + r % 4]);
+            o[d][r] += seen ? not_finite_or_zero(v) : 0.f;
+          }
+      }
+    }
+  }
   l += other_half(l);
   if (!mine) return;
   const int64_t unit = static_cast<int64_t>(my_t) * a.Hq + my_h;
