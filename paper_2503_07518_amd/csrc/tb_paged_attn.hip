@@ -88,8 +88,13 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 x, u32x4 y, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, q, c, 0, 0, 0);
 }
 
-// What the other half of the wave holds.
+// What the other half of the wave holds; the larger of what both do.
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, kWave); }
+__device__ __forceinline__ float over_halves(float x) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
 
 // ---- many tokens ----------------------------------------------------------------------------------
 // A wave holds 32 rows as columns of v_mfma_f32_32x32x16_bf16 (or 32x32x2_f32, which keeps fp32 as it is): their queries (32 or 64 registers), their
@@ -217,37 +222,38 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
   constexpr int MY_ROWS = S::LOADS * S::AT_ONCE;
   static_assert(16 % MY_ROWS == 0, "rows of a wave lie in one page");
   const int lane_row = lane / S::PIECES, piece = lane % S::PIECES;
-  const uint32_t k_lane = lane_row * a.pages.k_n, v_lane = lane_row * a.pages.v_n;
-  auto stage = [&](char* sk, char* sv, int32_t t, int32_t page, unsigned long long there) {
+  const int k_lane = lane_row * a.pages.k_n, v_lane = lane_row * a.pages.v_n;
+  // (numbers hidden from the compiler, which would keep all that follows from them in registers)
+  auto hidden = [](int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+  };
+  auto load = [](const char* from, char* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+  };
+  auto stage = [&](auto v_tag, char* to, int32_t t, int32_t page, unsigned long long there) {
+    constexpr bool IS_V = decltype(v_tag)::value;
     const int32_t pg = max(__builtin_amdgcn_readlane(page, wave * MY_ROWS), 0);
     const uint32_t in_page = static_cast<uint32_t>(t * S::KEYS + wave * MY_ROWS) & ((1u << a.pages.shift) - 1);
-    const char* k = kh + pg * a.pages.k_p + static_cast<uint64_t>(in_page) * a.pages.k_n;
-    const char* v = vh + pg * a.pages.v_p + static_cast<uint64_t>(in_page) * a.pages.v_n;
-    sk += wave * MY_ROWS * S::ROW;
-    sv += wave * MY_ROWS * S::ROW;
-    auto load = [](const char* from, char* to) {
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-    };
+    const uint32_t row_bytes = IS_V ? a.pages.v_n : a.pages.k_n;
+    const char* from = (IS_V ? vh : kh) + pg * (IS_V ? a.pages.v_p : a.pages.k_p) + static_cast<uint64_t>(in_page) * row_bytes;
+    to += wave * MY_ROWS * S::ROW;
+    // (the swizzle of a sum of numbers without common bits is that of one and that of the other)
+    const int r_wave = wave * MY_ROWS + lane_row, in_row = hidden((piece ^ (IS_V ? S::v_swizzle(r_wave) : S::k_swizzle(r_wave))) * 16);
+    const uint32_t row_at = static_cast<uint32_t>(hidden(IS_V ? v_lane : k_lane));
+    auto place = [&](int x) -> uint32_t { return row_at + (in_row ^ (IS_V ? S::v_swizzle(x * S::AT_ONCE) : S::k_swizzle(x * S::AT_ONCE)) * 16); };
     if (there == kAll) {
 #pragma unroll
       for (int x = 0; x < S::LOADS; ++x) {
-        const int r = wave * MY_ROWS + x * S::AT_ONCE + lane_row;
-        load(k + (k_lane + (piece ^ S::k_swizzle(r)) * 16), sk + x * 1024);
-        load(v + (v_lane + (piece ^ S::v_swizzle(r)) * 16), sv + x * 1024);
-        k += S::AT_ONCE * static_cast<uint64_t>(a.pages.k_n);
-        v += S::AT_ONCE * static_cast<uint64_t>(a.pages.v_n);
+        load(from + place(x), to + x * 1024);
+        from += S::AT_ONCE * static_cast<uint64_t>(row_bytes);
       }
     } else {
 #pragma clang loop unroll(disable)
       for (int x = 0; x < S::LOADS; ++x) {
-        const int r = wave * MY_ROWS + x * S::AT_ONCE + lane_row;
-        const char* kp = k + (k_lane + (piece ^ S::k_swizzle(r)) * 16);
-        const char* vp = v + (v_lane + (piece ^ S::v_swizzle(r)) * 16);
-        const bool is = (there >> r & 1) != 0;
-        load(is ? kp : reinterpret_cast<const char*>(zero_row), sk + x * 1024);
-        load(is ? vp : reinterpret_cast<const char*>(zero_row), sv + x * 1024);
-        k += S::AT_ONCE * static_cast<uint64_t>(a.pages.k_n);
-        v += S::AT_ONCE * static_cast<uint64_t>(a.pages.v_n);
+        const bool is = (there >> (wave * MY_ROWS + x * S::AT_ONCE + lane_row) & 1) != 0;
+        load(is ? from + place(x) : reinterpret_cast<const char*>(zero_row), to + x * 1024);
+        from += S::AT_ONCE * static_cast<uint64_t>(row_bytes);
       }
     }
   };
@@ -265,72 +271,39 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
   const int v_row = S::F32 ? 4 * half : 4 * half + (lane & 15) / 4;
   const int v_piece = S::F32 ? col / 4 : 2 * (lane >> 4 & 1) + (lane & 3) / 2;
   const int v_at = v_row * S::ROW + ((v_piece ^ S::v_swizzle(v_row)) * 16) + (S::F32 ? (col & 3) * 4 : (lane & 1) * 8);
-  // (hidden from the compiler, which would keep all that follows from them in registers)
-  auto hidden = [](int x) {
-    asm volatile("" : "+v"(x));
-    return x;
-  };
-  // Pieces of K for the first product: number f is the piece pair f % PAIRS of the block f / PAIRS of 32 keys.
+  // Scores of a tile (column `col` of it: register r of block k is key 32 k + 8 (r / 4) + 4 half + r % 4).  The products go round the blocks, so
+  // that none waits for the one before it; `meanwhile(i)` is work that does not wait for them either.
   constexpr int PIECE_PAIRS = KB * S::PAIRS;
-  constexpr int AHEAD = S::F32 && D == 128 ? 0 : PIECE_PAIRS / 2;  // of them are read while the tile before is finished: as many as registers allow
-  u32x4 kf[PIECE_PAIRS];
-  auto read_k = [&](const char* sk, auto ahead_tag) {
-    constexpr bool FIRST = decltype(ahead_tag)::value;
+  auto scores = [&](const char* sk, f32x16(&x)[KB], auto&& meanwhile) {
     const int at = hidden(k_at);
+    constexpr int HELD = PIECE_PAIRS < 6 ? PIECE_PAIRS : 6;  // operands that are on their way or waiting
+    u32x4 kf[HELD];
+    auto read = [&](int f) { kf[f % HELD] = *reinterpret_cast<const u32x4*>(sk + (at ^ (f / KB * 32)) + f % KB * 32 * S::ROW); };
 #pragma unroll
-    for (int f = FIRST ? 0 : AHEAD; f < (FIRST ? AHEAD : PIECE_PAIRS); ++f)
-      kf[f] = *reinterpret_cast<const u32x4*>(sk + (at ^ (f % S::PAIRS * 32)) + f / S::PAIRS * 32 * S::ROW);
-  };
-  // The tile t from sk, sv; then `between`, which makes the next one there; then it begins to read that from sk_next.
-  auto work = [&](const char* sk, const char* sv, const char* sk_next, int32_t t, unsigned long long there, auto&& between) {
-    const int32_t first = t * S::KEYS;
-    f32x16 x[KB];
-    read_k(sk, std::false_type{});
-    __builtin_amdgcn_sched_barrier(0);
+    for (int f = 0; f < HELD; ++f) read(f);
 #pragma unroll
-    for (int k = 0; k < KB; ++k) {
+    for (int k = 0; k < KB; ++k)
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[k][r] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int c = 0; c < S::PAIRS; ++c) {
-        if constexpr (S::F32) {
+    for (int f = 0; f < PIECE_PAIRS; ++f) {
+      const int c = f / KB, k = f % KB;
+      const u32x4 kk = kf[f % HELD];
+      if constexpr (S::F32) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            x[k] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[k * S::PAIRS + c][e]), __uint_as_float(q[c][e]), x[k], 0, 0, 0);
-        } else {
-          x[k] = mfma32(kf[k * S::PAIRS + c], q[c], x[k]);
-        }
+        for (int e = 0; e < 4; ++e) x[k] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kk[e]), __uint_as_float(q[c][e]), x[k], 0, 0, 0);
+      } else {
+        x[k] = mfma32(kk, q[c], x[k]);
       }
+      if (f + HELD < PIECE_PAIRS) read(f + HELD);
+      meanwhile(f);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    // V's operands, of bf16 a column of four rows a lane, transposed on the way: one half of its columns while the weights are computed, the
-    // other under the products with the first
-    constexpr int VF = S::F32 ? 4 * KB : 2 * KB;  // steps of 16 keys (bf16), four of one key a half (fp32)
-    const int at_v = hidden(v_at);
-    auto read_v = [&](u32x4(&vf)[DB / 2][VF], int d0) {
-#pragma unroll
-      for (int j = 0; j < VF; ++j)
-#pragma unroll
-        for (int d = 0; d < DB / 2; ++d) {
-          const char* from = sv + (at_v ^ ((d0 + d) * 32 * static_cast<int>(sizeof(T)))) + j * (S::F32 ? 8 : 16) * S::ROW;
-          if constexpr (S::F32) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) vf[d][j][e] = *reinterpret_cast<const uint32_t*>(from + e * S::ROW);
-          } else {
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_char*)(from + 8 * y * S::ROW));
-              uint32_t w2[2];
-              __builtin_memcpy(w2, &w, 8);
-              vf[d][j][2 * y] = w2[0];
-              vf[d][j][2 * y + 1] = w2[1];
-            }
-          }
-        }
-    };
-    u32x4 v0[DB / 2][VF], v1[DB / 2][VF];
-    read_v(v0, 0);
-    __builtin_amdgcn_sched_barrier(0);
+  };
+  // What the rows see of a tile's keys, and its part in the running reference: `x` becomes -inf elsewhere.
+  auto see = [&](f32x16(&x)[KB], int32_t t, unsigned long long there) {
+    const int32_t first = t * S::KEYS;
     if (there != kAll || first + S::KEYS - 1 > w_first || (a.window && first <= w_last - a.window)) {
       // keys behind `low` up to `high`, by the number that a register has in both halves
       const int high = my_p - first - 4 * half, low = max(my_low - first - 4 * half, -1);
@@ -344,15 +317,18 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
         }
       }
     }
+  };
+  auto largest = [&](const f32x16(&x)[KB]) -> float {
     float top = x[0][0];
 #pragma unroll
     for (int k = 0; k < KB; ++k)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, x[k][r]);
-    top = fmaxf(top, other_half(top)) * a.scale_log2;  // (-inf times a scale of 0 does not come up: that is 1 then)
+    return over_halves(top) * a.scale_log2;  // (-inf times a scale of 0 does not come up: that is 1 then)
+  };
+  auto follow = [&](float top) {
     if (ballot64(top > m + kLazy)) {
-      // (nothing seen yet: the sums are 0)
-      const float m_new = fmaxf(m, top), alpha = m > -INFINITY ? exp2_safe(m - m_new) : 1.f;
+      const float m_new = fmaxf(m, top), alpha = m > -INFINITY ? exp2_safe(m - m_new) : 1.f;  // (nothing seen yet: the sums are 0)
       l *= alpha;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
@@ -360,49 +336,75 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
         for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
       m = m_new;
     }
+  };
+  // A tile t whose scores x are there: its weights are computed under the products of the next tile's scores (from sk), its part in
+  // the output, from sv, under the search for their maximum.
+  auto work = [&](f32x16(&x)[KB], f32x16(&x_next)[KB], const char* sk, const char* sv, int32_t t, unsigned long long there_next) {
     const float m_ref = m > -INFINITY ? m : 0.f;  // nothing seen yet: all weights 0
-#pragma unroll
-    for (int k = 0; k < KB; ++k)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        x[k][r] = exp2_safe(fmaf(x[k][r], a.scale_log2, -m_ref));
-        l += x[k][r];
-      }
+    constexpr int STEPS = KB * S::PAIRS, EACH = KB * 16 / STEPS;  // weights a product
     u32x4 p[S::F32 ? 1 : 2 * KB];
-    if constexpr (!S::F32) {
+    scores(sk, x_next, [&](int i) {
 #pragma unroll
-      for (int j = 0; j < 2 * KB; ++j)
+      for (int y = i * EACH; y < (i + 1) * EACH; ++y) {
+        const float w = exp2_safe(fmaf(x[y / 16][y % 16], a.scale_log2, -m_ref));
+        x[y / 16][y % 16] = w;
+        l += w;
+        if constexpr (!S::F32)
+          if (y & 1) {
+            uint32_t u = bf16x2(x[y / 16][y % 16 - 1], w);
+            p[y / 8][y % 8 / 2] = u;
+          }
+      }
+    });
+    // V's operands, of bf16 a column of four rows a lane, transposed on the way
+    constexpr int VF = S::F32 ? 4 * KB : 2 * KB;  // steps of 16 keys (bf16), four of one key a half (fp32)
+    const int at_v = hidden(v_at);
+    constexpr int HELD = VF < 3 ? VF : 3;  // steps whose operands are on their way or waiting
+    u32x4 vf[HELD][DB];
+    auto read_v = [&](int j) {
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          uint32_t w = bf16x2(x[j / 2][8 * (j & 1) + 2 * y], x[j / 2][8 * (j & 1) + 2 * y + 1]);
-          asm volatile("" : "+v"(w));  // (now, not behind the barrier: the scores' registers are wanted)
-          p[j][y] = w;
-        }
-    }
-    auto products = [&](const u32x4(&vf)[DB / 2][VF], int d0) {
+      for (int d = 0; d < DB; ++d) {
+        const char* from = sv + (at_v ^ (d * 32 * static_cast<int>(sizeof(T)))) + j * (S::F32 ? 8 : 16) * S::ROW;
+        u32x4& v = vf[j % HELD][d];
+        if constexpr (S::F32) {
 #pragma unroll
-      for (int j = 0; j < VF; ++j)
+          for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const uint32_t*>(from + e * S::ROW);
+        } else {
 #pragma unroll
-        for (int d = 0; d < DB / 2; ++d) {
-          if constexpr (S::F32) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              o[d0 + d] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(vf[d][j][e]), x[j / 4][4 * (j % 4) + e], o[d0 + d], 0, 0, 0);
-          } else {
-            o[d0 + d] = mfma32(vf[d][j], p[j], o[d0 + d]);
+          for (int y = 0; y < 2; ++y) {
+            const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_char*)(from + 8 * y * S::ROW));
+            uint32_t w2[2];
+            __builtin_memcpy(w2, &w, 8);
+            v[2 * y] = w2[0];
+            v[2 * y + 1] = w2[1];
           }
         }
+      }
     };
+    const bool more = t + 1 < tile_end;
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) read_v(j);
+    if (more) see(x_next, t + 1, there_next);
     __builtin_amdgcn_sched_barrier(0);
-    read_v(v1, DB / 2);
-    __builtin_amdgcn_sched_barrier(0);
-    products(v0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    between();
-    __builtin_amdgcn_sched_barrier(0);
-    read_k(sk_next, std::true_type{});
-    __builtin_amdgcn_sched_barrier(0);
-    products(v1, DB / 2);
+    float top = x_next[0][0];
+#pragma unroll
+    for (int j = 0; j < VF; ++j) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        if constexpr (S::F32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(vf[j % HELD][d][e]), x[j / 4][4 * (j % 4) + e], o[d], 0, 0, 0);
+        } else {
+          o[d] = mfma32(vf[j % HELD][d], p[j], o[d]);
+        }
+      }
+      if (j + HELD < VF) read_v(j + HELD);
+#pragma unroll
+      for (int y = j * KB * 16 / VF; y < (j + 1) * KB * 16 / VF; ++y) top = fmaxf(top, x_next[y / 16][y % 16]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (more) follow(over_halves(top) * a.scale_log2);
   };
   // A tile with rows that some of the workgroup's do not see: what is infinite or NaN there would be NaN times a weight of 0.  Such
   // elements are zeros for the products, and are added in the end to the sums of those that see them.  (All waves come here.)
@@ -420,33 +422,38 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
     __syncthreads();
   };
 
-  // Two tiles are in LDS, or on their way there; when all waves have read one, the next but one takes its place.  (Past the end the same bytes
-  // are read once more, for nothing.)
+  // In LDS are the tile's V and the next one's K, or on their way there; the next V and the K behind that are asked for when all waves
+  // have read what they replace.
   const int32_t tile_first = tile;
   if (tile < tile_end) {
-    int32_t page = pages_of_tile(tile), page_next = pages_of_tile(tile + 1);
-    unsigned long long there = rows_there(tile, page), next = rows_there(tile + 1, page_next);
-    stage(s_k0, s_v0, tile, page, there);
-    if (tile + 1 < tile_end) stage(s_k1, s_v1, tile + 1, page_next, next);
-    page = pages_of_tile(tile + 2);
-    auto step = [&](char* sk, char* sv, char* sk_next) {
+    int32_t page = pages_of_tile(tile), page_next = pages_of_tile(tile + 1), page_2 = pages_of_tile(tile + 2);
+    unsigned long long next = rows_there(tile + 1, page_next);
+    f32x16 x0[KB], x1[KB];
+    {
+      const unsigned long long there = rows_there(tile, page);
+      stage(std::false_type{}, s_k0, tile, page, there);
+      stage(std::true_type{}, s_v0, tile, page, there);
+      if (tile + 1 < tile_end) stage(std::false_type{}, s_k1, tile + 1, page_next, next);
+      __syncthreads();
+      scores(s_k0, x0, [](int) {});
+      see(x0, tile, there);
+      follow(largest(x0));
+    }
+    auto step = [&](f32x16(&x)[KB], f32x16(&x_next)[KB], char* sk, char* sk_next, char* sv, char* sv_next) {
+      __syncthreads();
       guard(sv, tile);
-      work(sk, sv, sk_next, tile, there, [&]() {
-        __syncthreads();  // all have read the tile, and the next one has arrived
-        there = next;
-        next = rows_there(tile + 2, page);
-        if (tile + 2 < tile_end) {
-          stage(sk, sv, tile + 2, page, next);
-          page = pages_of_tile(tile + 3);
-        }
-      });
+      const unsigned long long next_2 = rows_there(tile + 2, page_2);
+      if (tile + 1 < tile_end) stage(std::true_type{}, sv_next, tile + 1, page_next, next);
+      if (tile + 2 < tile_end) stage(std::false_type{}, sk, tile + 2, page_2, next_2);
+      page_next = page_2;
+      page_2 = pages_of_tile(tile + 3);
+      work(x, x_next, sk_next, sv, tile, next);
+      next = next_2;
     };
-    __syncthreads();
-    read_k(s_k0, std::true_type{});
     while (true) {
-      step(s_k0, s_v0, s_k1);
+      step(x0, x1, s_k0, s_k1, s_v0, s_v1);
       if (++tile >= tile_end) break;
-      step(s_k1, s_v1, s_k0);
+      step(x1, x0, s_k1, s_k0, s_v1, s_v0);
       if (++tile >= tile_end) break;
     }
   }
