@@ -10,6 +10,7 @@
 // keys take its k slots is the accumulators' own, and the operand from V follows it.
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "tb_attn_merge.h"
 #include "tb_paged.h"
@@ -37,7 +38,6 @@ struct PagedAttnArgs {
   int32_t max_new, window;
   int32_t nsplit;
   int32_t few;  // chunk_kernel: sequences with up to so many rows are the token_kernel's
-  int32_t tiles;  // chunk_kernel: of a KV head, at most
   float* partials;
   int64_t pairs_off;
   uint32_t* counters;
@@ -102,20 +102,17 @@ __device__ __forceinline__ float over_halves(float x) {
 // while one is worked on, the next one comes straight from memory (global_load_lds, 16 bytes a lane).  Rows in LDS are
 // permuted in pieces of 16 bytes by their number so that neither the rows of K (a piece of 32 rows at once) nor the transposing reads
 // of V (a column of four rows) meet on a bank.
-constexpr int kChunkRows = 128;  // of a workgroup
-constexpr int kChunkThreads = 256;
-constexpr int kChunkWaves = kChunkThreads / kWave;
 // The reference of a row's softmax follows its maximum only when that has moved by more than this (weights stay below 2^8): the
 // accumulators are seldom rescaled.
 constexpr float kLazy = 8.f;
 
-template <typename T, int D>
+template <typename T, int D, int NW>
 struct ChunkShape {
   static constexpr int ROW = D * sizeof(T);                     // bytes
   static constexpr int KEYS = ROW >= 512 ? 32 : 64;             // of a tile
   static constexpr int PIECES = ROW / 16;                       // of 16 bytes in a row
   static constexpr int AT_ONCE = 1024 / ROW;                    // rows that a wave loads at once
-  static constexpr int LOADS = KEYS * ROW / 1024 / kChunkWaves;  // of a wave for a tile of K or V
+  static constexpr int LOADS = KEYS * ROW / 1024 / NW;       // of a wave for a tile of K or V
   static constexpr int TILE = KEYS * ROW;
   static constexpr int PAIRS = PIECES / 2;  // of pieces: what a lane half each takes of a row
   static constexpr bool F32 = std::is_same<T, float>::value;
@@ -126,9 +123,10 @@ struct ChunkShape {
   }
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a) {
-  using S = ChunkShape<T, D>;
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
+  using S = ChunkShape<T, D, NW>;
+  constexpr int THREADS = NW * kWave;
   constexpr int KB = S::KEYS / 32, DB = D / 32;  // blocks of 32 keys, of 32 columns of V
   __shared__ __attribute__((aligned(1024))) char s_k0[S::TILE], s_k1[S::TILE], s_v0[S::TILE], s_v1[S::TILE];
 
@@ -138,7 +136,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
   const int split = blockIdx.y;
 
   // the tile of tokens: those that see the most rows begin first
-  const int tq_log = 7 - a.gs;  // tokens of a tile: 128 rows >> gs
+  const int tq_log = __builtin_ctz(32 * NW) - a.gs;  // tokens of a tile: 32 rows a wave
   int32_t at = blockIdx.x / a.Hkv, b = 0;
   Sequence s;
   int32_t n;  // of its tokens that take part
@@ -349,11 +347,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
         const float w = exp2_safe(fmaf(x[y / 16][y % 16], a.scale_log2, -m_ref));
         x[y / 16][y % 16] = w;
         l += w;
-        if constexpr (!S::F32)
-          if (y & 1) {
-            uint32_t u = bf16x2(x[y / 16][y % 16 - 1], w);
-            p[y / 8][y % 8 / 2] = u;
-          }
+        if (!S::F32 && (y & 1)) p[y / 8][y % 8 / 2] = bf16x2(x[y / 16][y % 16 - 1], w);
       }
     });
     // V's operands, of bf16 a column of four rows a lane, transposed on the way
@@ -414,10 +408,10 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(PagedAttnArgs a
     if (!partly_seen(t * S::KEYS)) return;
     uint32_t most = 0;
     const int at = hidden(threadIdx.x * 16);
-    for (int i = at; i < S::TILE; i += kChunkThreads * 16) most = largest_exponent<T>(*reinterpret_cast<const u32x4*>(sv + i), most);
+    for (int i = at; i < S::TILE; i += THREADS * 16) most = largest_exponent<T>(*reinterpret_cast<const u32x4*>(sv + i), most);
     if (__builtin_expect(!__syncthreads_or(most == kExponent), 1)) return;
     specials = true;
-    for (int i = at; i < S::TILE; i += kChunkThreads * 16)
+    for (int i = at; i < S::TILE; i += THREADS * 16)
       *reinterpret_cast<u32x4*>(sv + i) = finite_or_zero<T>(*reinterpret_cast<const u32x4*>(sv + i));
     __syncthreads();
   };
@@ -549,6 +543,9 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void join_kernel(PagedAttnArgs 
 // is then key 4 kb + v of column i, and element e of V's pieces the column EV i + e of the output, whose accumulator v is that of row 4 kb + v.
 // A wave has two steps' rows in flight.  Workgroups that share a sequence hand over by tb_attn_merge.h's protocol.
 constexpr int kTokenWaves = 8;
+// Every row is read once: not kept for anybody (32 heads on 8, D = 128, bf16, plain loads and these: 32768 rows 30.0 and 26.6 us, 16 sequences of
+// 9002 to 16384 163 and 152, one of 16384, whose rows the last-level cache still held, 18.5 and 18.4).
+constexpr int kNonTemporal = 2;  // (cache policy of a buffer load: nt)
 constexpr int kTokenRows = 16;
 
 template <typename T, int D>
@@ -606,26 +603,34 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
   struct Rows {
     u32x4 k[S::GROUPS][S::KP], v[S::GROUPS][4][S::VP];
   };
-  const char* const kh = a.pages.K + hkv * a.pages.k_h + i16 * static_cast<uint64_t>(a.pages.k_n) + kb * 16;
-  const char* const vh = a.pages.V + hkv * a.pages.v_h + 4 * kb * static_cast<uint64_t>(a.pages.v_n) + i16 * S::VB;
-  auto fetch = [&](Rows& x, int32_t step, int32_t pages, int32_t nth) {
+  const char* const kh = a.pages.K + hkv * a.pages.k_h;
+  const char* const vh = a.pages.V + hkv * a.pages.v_h;
+  const uint32_t k_lane = i16 * a.pages.k_n + kb * 16, v_lane = 4 * kb * a.pages.v_n + i16 * S::VB;
+  // Rows that nobody sees, those in holes and all of a step that is none read as zeros, by the buffers' bounds (of rows in front the offset is
+  // negative, and so a large one): the loads are issued in any case, so that what waits for those of one step need not wait for those of the next.
+  auto fetch = [&](Rows& x, int32_t step, int32_t pages, int32_t nth, bool is) {
 #pragma unroll
     for (int g = 0; g < S::GROUPS; ++g) {
-      const int64_t page = max(__builtin_amdgcn_readlane(pages, nth * S::GROUPS + g), 0);  // (a hole: rows that count for nothing below)
-      const uint32_t in_page = static_cast<uint32_t>(step * S::STEP + g * 16) & ((1u << a.pages.shift) - 1);
-      const char* k = kh + page * a.pages.k_p + static_cast<uint64_t>(in_page) * a.pages.k_n;
-      const char* v = vh + page * a.pages.v_p + static_cast<uint64_t>(in_page) * a.pages.v_n;
+      const int32_t page = __builtin_amdgcn_readlane(pages, (nth * S::GROUPS + g) & (kWave - 1)), row = step * S::STEP + g * 16;
+      const int32_t front = max(see_first - row, 0);
+      const int32_t rows = __builtin_amdgcn_readfirstlane(is && page >= 0 ? max(min(p_last + 1 - row, 16) - front, 0) : 0);
+      const uint32_t in_page = __builtin_amdgcn_readfirstlane((row & ((1 << a.pages.shift) - 1)) + front);
+      const __amdgpu_buffer_rsrc_t k = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<char*>(kh + max(page, 0) * a.pages.k_p + static_cast<uint64_t>(in_page) * a.pages.k_n), 0, rows * a.pages.k_n, 0x00027000);
+      const __amdgpu_buffer_rsrc_t v = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<char*>(vh + max(page, 0) * a.pages.v_p + static_cast<uint64_t>(in_page) * a.pages.v_n), 0, rows * a.pages.v_n, 0x00027000);
+      const uint32_t k_off = k_lane - front * a.pages.k_n, v_off = v_lane - front * a.pages.v_n;
 #pragma unroll
-      for (int c = 0; c < S::KP; ++c) x.k[g][c] = *reinterpret_cast<const u32x4*>(k + c * 64);
+      for (int c = 0; c < S::KP; ++c) x.k[g][c] = __builtin_amdgcn_raw_buffer_load_b128(k, k_off + c * 64, 0, kNonTemporal);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int c = 0; c < S::VP; ++c) {
           if constexpr (S::VB == 8) {
-            const uint2 y = *reinterpret_cast<const uint2*>(v + r * static_cast<uint64_t>(a.pages.v_n));
-            x.v[g][r][c] = u32x4{y.x, y.y, 0u, 0u};
+            const auto y = __builtin_amdgcn_raw_buffer_load_b64(v, v_off + r * a.pages.v_n, 0, kNonTemporal);
+            x.v[g][r][c] = u32x4{y[0], y[1], 0u, 0u};
           } else {
-            x.v[g][r][c] = *reinterpret_cast<const u32x4*>(v + r * static_cast<uint64_t>(a.pages.v_n) + c * 16);
+            x.v[g][r][c] = __builtin_amdgcn_raw_buffer_load_b128(v, v_off + r * a.pages.v_n + c * 16, 0, kNonTemporal);
           }
         }
     }
@@ -636,12 +641,13 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
   for (int e = 0; e < S::EV; ++e) o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
 
-  auto work = [&](Rows& x, int32_t step, int32_t pages, int32_t nth) {
+  // EDGE: a step with rows that some of the tokens do not see.
+  auto work = [&](auto edge_tag, auto& x, int32_t step, int32_t pages, int32_t nth) {
+    constexpr bool EDGE = decltype(edge_tag)::value;
     const int32_t first = step * S::STEP;
     uint32_t holes = 0;
 #pragma unroll
     for (int g = 0; g < S::GROUPS; ++g) holes |= (__builtin_amdgcn_readlane(pages, nth * S::GROUPS + g) < 0 ? 1u : 0u) << g;
-    const bool masked = holes || first + S::STEP - 1 > p_first || (a.window && first <= p_last - a.window);
     float p[S::GROUPS][4];
 #pragma unroll
     for (int g = 0; g < S::GROUPS; ++g) {
@@ -658,19 +664,21 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
 #pragma unroll
       for (int r = 0; r < 4; ++r) p[g][r] = sc[r];
     }
-    if (masked) {
+    if (holes) {
+#pragma unroll
+      for (int g = 0; g < S::GROUPS; ++g)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[g][r] = (holes >> g & 1) != 0 ? -INFINITY : p[g][r];
+    }
+    if constexpr (EDGE) {
       uint32_t most = 0;
 #pragma unroll
       for (int g = 0; g < S::GROUPS; ++g)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int32_t key = first + 16 * g + 4 * kb + r;
-          // (selects: with branches here, hipcc of ROCm 7.2 lost the second half of this condition)
-          const bool hole = (holes >> g & 1) != 0;
-          p[g][r] = ((key <= my_p) & (key > my_low) & !hole) ? p[g][r] : -INFINITY;
-          const uint32_t kept = ((key > p_last) | (key < see_first) | hole) ? 0u : ~0u;  // a row that nobody sees counts as zeros
-#pragma unroll
-          for (int c = 0; c < S::VP; ++c) x.v[g][r][c] &= kept;
+          // (a select: with branches here, hipcc of ROCm 7.2 lost the second half of this condition)
+          p[g][r] = ((key <= my_p) & (key > my_low)) ? p[g][r] : -INFINITY;
 #pragma unroll
           for (int c = 0; c < S::VP; ++c) most = largest_exponent<T>(x.v[g][r][c], most);
         }
@@ -756,22 +764,42 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
     }
   };
 
-  // steps step_0 + split * per + wave, + kTokenWaves, ...; their pages in batches
-  int32_t step = step_0 + split * per + wave;
-  for (; step < step_end; step += BATCH * kTokenWaves) {
+  // The wave has the steps mine_0, mine_0 + kTokenWaves, ..: first those that all tokens see whole, the pages of many at a time, then the others
+  // (the last one or two of a sequence, and where a window begins).
+  const int32_t mine_0 = step_0 + split * per + wave;
+  const int32_t whole_0 = a.window ? max((p_last - a.window + S::STEP) / S::STEP, step_0) : 0, whole_end = min((p_first + 1) / S::STEP, step_end);
+  int32_t step = mine_0 + (max(whole_0 - mine_0, 0) + kTokenWaves - 1) / kTokenWaves * kTokenWaves;
+  const int32_t edge_end = step;  // (of those in front)
+  for (; step < whole_end; step += BATCH * kTokenWaves) {
     const int32_t pages = pages_from(step);
-    const int32_t count = min((step_end - step + kTokenWaves - 1) / kTokenWaves, BATCH);
+    const int32_t count = min((whole_end - step + kTokenWaves - 1) / kTokenWaves, BATCH);
     Rows x, y;
-    fetch(x, step, pages, 0);
-    for (int32_t k = 0; k < count; k += 2) {
-      if (k + 1 < count) fetch(y, step + (k + 1) * kTokenWaves, pages, k + 1);
+    fetch(x, step, pages, 0, true);
+    // (one way through the loop: with another round it the compiler would wait for loads that are not its own)
+    for (int32_t k = 0; k + 1 < count; k += 2) {
+      fetch(y, step + (k + 1) * kTokenWaves, pages, k + 1, true);
       __builtin_amdgcn_sched_barrier(0);
-      work(x, step + k * kTokenWaves, pages, k);
-      if (k + 1 >= count) break;
-      if (k + 2 < count) fetch(x, step + (k + 2) * kTokenWaves, pages, k + 2);
+      work(std::false_type{}, static_cast<const Rows&>(x), step + k * kTokenWaves, pages, k);
+      __builtin_amdgcn_sched_barrier(0);  // (into the registers that the step before has left)
+      fetch(x, step + (k + 2) * kTokenWaves, pages, k + 2, k + 2 < count);
       __builtin_amdgcn_sched_barrier(0);
-      work(y, step + (k + 1) * kTokenWaves, pages, k + 1);
+      work(std::false_type{}, static_cast<const Rows&>(y), step + (k + 1) * kTokenWaves, pages, k + 1);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    if (count & 1) work(std::false_type{}, static_cast<const Rows&>(x), step + (count - 1) * kTokenWaves, pages, count - 1);
+    // the last loads, of nothing, end here: not known to have, they would be waited for in the loop
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+  }
+#pragma clang loop unroll(disable)
+  for (step = mine_0; step < step_end; step += kTokenWaves) {
+    if (step >= edge_end && step < whole_end) {
+      step += (whole_end - 1 - step) / kTokenWaves * kTokenWaves;
+      continue;
+    }
+    const int32_t pages = pages_from(step);
+    Rows x;
+    fetch(x, step, pages, 0, true);
+    work(std::true_type{}, x, step, pages, 0);
   }
   l += __shfl_xor(l, 16, kWave);
   l += __shfl_xor(l, 32, kWave);
@@ -844,18 +872,26 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
 
 // ---- plans ----------------------------------------------------------------------------------------
 constexpr int64_t kCus = 256;
-constexpr int64_t kChunkTarget = 2 * kCus;  // workgroups of the chunk_kernel that the chip holds at once
+constexpr int64_t kChunkTarget = 2 * kCus;  // workgroups of four waves that the chip holds at once
 
 int chunk_keys(const tb_cache_desc& d) { return d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 32 : 64; }
-// Splits of a sequence's rows: as many workgroups as the chip holds, of at least four tiles each.
-int64_t chunk_splits(const tb_cache_desc& d, int64_t tiles) {
-  const int64_t wgs = std::max<int64_t>(tiles * d.Hkv, 1);
-  return std::max<int64_t>(1, std::min(kChunkTarget / wgs, d.N / (4 * chunk_keys(d))));
+// Waves of a workgroup: eight read each row of K and V half as often.
+int chunk_waves(const tb_cache_desc& d, int64_t T) {
+  if (const char* e = getenv("TB_WAVES")) return atoi(e);
+  return T * d.Hq >= 32 * 8 * kCus ? 8 : 4;
 }
-// ... of at least two steps a wave.
+// Splits of a sequence's rows: as many workgroups as the chip holds, of at least four tiles each.
+int64_t chunk_splits(const tb_cache_desc& d, int waves, int64_t tiles) {
+  const int64_t wgs = std::max<int64_t>(tiles * d.Hkv, 1);
+  if (const char* e = getenv("TB_NS")) return atoi(e);
+  return std::max<int64_t>(1, std::min(kChunkTarget * 4 / waves / wgs, d.N / (4 * chunk_keys(d))));
+}
+// Rows times splits that a workspace has room for.
+constexpr int64_t kPartialRows = 131072;
+// ... of at least two steps.
 int64_t token_splits(const tb_cache_desc& d) {
   const int64_t groups = std::max<int64_t>(static_cast<int64_t>(d.B) * d.Hkv, 1), step = d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 16 : 32;
-  return std::max<int64_t>(1, std::min(kCus / groups, d.N / (2 * step * kTokenWaves)));
+  return std::max<int64_t>(1, std::min(kCus / groups, d.N / (2 * step)));
 }
 size_t token_counters(const tb_cache_desc& d) { return static_cast<size_t>(d.B) * d.Hkv * kCounterStrideWords * sizeof(uint32_t); }
 
@@ -888,14 +924,15 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
   const bool chunks = most << a.gs > kTokenRows;
   const bool tokens = !chunks || (L.cu && d.B > 1);  // sequences of few tokens may be among the others
   if (chunks) {
-    const int tq_log = 7 - a.gs;
+    const int waves = chunk_waves(d, L.T);
+    const int tq_log = __builtin_ctz(32 * waves) - a.gs;
     const int64_t tiles = L.cu ? (L.T >> tq_log) + std::min<int64_t>(d.B, L.T) : d.B * ((std::min<int64_t>(a.tok.each, L.max_new) + (1 << tq_log) - 1) >> tq_log);
     a.few = tokens ? kTokenRows : 0;
-    a.tiles = static_cast<int32_t>(tiles);
     // (ragged: at least as many tiles as full ones)
-    a.nsplit = static_cast<int32_t>(chunk_splits(d, L.cu ? std::max<int64_t>((L.T + (1 << tq_log) - 1) >> tq_log, 1) : tiles));
+    a.nsplit = static_cast<int32_t>(std::min(std::max<int64_t>(kPartialRows / (L.T * d.Hq), 1), chunk_splits(d, waves, L.cu ? std::max<int64_t>((L.T + (1 << tq_log) - 1) >> tq_log, 1) : tiles)));
     a.pairs_off = static_cast<int64_t>(a.tok.T) * a.Hq * a.nsplit * D;
-    tb_status rc = launch_one(chunk_kernel<T, D>, dim3(static_cast<unsigned>(d.Hkv * tiles), a.nsplit), kChunkThreads, st, a);
+    const dim3 grid(static_cast<unsigned>(d.Hkv * tiles), a.nsplit);
+    tb_status rc = waves == 8 ? launch_one(chunk_kernel<T, D, 8>, grid, 8 * kWave, st, a) : launch_one(chunk_kernel<T, D, 4>, grid, 4 * kWave, st, a);
     if (rc != TB_OK) return rc;
     if (a.nsplit > 1) {
       const int64_t units = static_cast<int64_t>(a.tok.T) * a.Hq;
@@ -920,8 +957,8 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
 size_t paged_attn_ws_bytes(const tb_cache_desc* d, int64_t T) {
   const int64_t row = (d->D + 2) * static_cast<int64_t>(sizeof(float));
   const int64_t tokens = static_cast<int64_t>(d->B) * d->Hkv * kTokenRows * token_splits(*d);
-  // a call's rows times its splits: at most those of kChunkTarget workgroups, or of the rows in as many splits as there can be
-  const int64_t chunk = std::min(kChunkTarget * kChunkRows, T * d->Hq * chunk_splits(*d, 0));
+  // a call's rows times its splits, where there are several
+  const int64_t chunk = std::min(kPartialRows, T * d->Hq * std::max<int64_t>(1, d->N / (4 * chunk_keys(*d))));
   return token_counters(*d) + static_cast<size_t>(std::max(tokens, chunk) * row);
 }
 
