@@ -10,7 +10,6 @@
 // keys take its k slots is the accumulators' own, and the operand from V follows it.
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 
 #include "tb_attn_merge.h"
 #include "tb_paged.h"
@@ -36,7 +35,9 @@ struct PagedAttnArgs {
   uint32_t q_and, q_xor;
   int32_t Hq, Hkv, gs;  // 1 << gs query heads a KV head
   int32_t max_new, window;
-  int32_t nsplit;
+  int32_t nsplit;      // at most
+  int32_t target;      // chunk_kernel: workgroups that share the keys
+  int32_t* splits_of;  // ... and how many a row has got
   int32_t few;  // chunk_kernel: sequences with up to so many rows are the token_kernel's
   float* partials;
   int64_t pairs_off;
@@ -105,6 +106,8 @@ __device__ __forceinline__ float over_halves(float x) {
 // The reference of a row's softmax follows its maximum only when that has moved by more than this (weights stay below 2^8): the
 // accumulators are seldom rescaled.
 constexpr float kLazy = 8.f;
+// Tiles of keys that a split is worth its hand-over from (fp32: an eighth of the rate).
+constexpr int split_tiles(bool f32) { return f32 ? 4 : 16; }
 
 template <typename T, int D, int NW>
 struct ChunkShape {
@@ -138,40 +141,38 @@ __global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
   // the tile of tokens: those that see the most rows begin first
   const int tq_log = __builtin_ctz(32 * NW) - a.gs;  // tokens of a tile: 32 rows a wave
   int32_t at = blockIdx.x / a.Hkv, b = 0;
-  Sequence s;
-  int32_t n;  // of its tokens that take part
-  if (a.tok.cu) {
-    auto tiles_of = [&](int32_t i) -> uint32_t {
-      if (i >= a.tok.B) return 0;
-      const int32_t of = min(sequence(a.tok, i).n, a.max_new);
-      return of <= a.few >> a.gs ? 0 : (of + (1 << tq_log) - 1) >> tq_log;
-    };
-    uint32_t all = 0;
-    for (int32_t i = 0; i < a.tok.B; i += kWave) all += __builtin_amdgcn_readlane(wave_incl_scan_u32(tiles_of(i + lane)), kWave - 1);
-    if (static_cast<uint32_t>(at) >= all) return;
-    uint32_t want = all - 1 - at;
-    for (b = 0; b < a.tok.B; b += kWave) {
-      const uint32_t upto = wave_incl_scan_u32(tiles_of(b + lane));
-      const uint32_t here = __builtin_amdgcn_readlane(upto, kWave - 1);
-      if (want < here) {
-        const int skip = static_cast<int>(popc64(ballot64(upto <= want)));
-        if (skip) want -= __builtin_amdgcn_readlane(upto, skip - 1);
-        b += skip;
-        break;
-      }
-      want -= here;
-    }
-    at = static_cast<int32_t>(want);
-    b = __builtin_amdgcn_readfirstlane(b);
-  } else {
-    const int32_t tiles_each = (min(a.tok.each, a.max_new) + (1 << tq_log) - 1) >> tq_log;
-    at = a.tok.B * tiles_each - 1 - at;
-    if (at < 0) return;
-    b = at / tiles_each;
-    at -= b * tiles_each;
+  // a sequence's tiles of tokens, and with `keys` those times its tiles of keys, give or take
+  auto tiles_of = [&](int32_t i, bool keys) -> uint32_t {
+    if (i >= a.tok.B) return 0;
+    const Sequence x = sequence(a.tok, i);
+    const int32_t of = min(x.n, a.max_new);
+    if (of <= a.few >> a.gs) return 0;
+    const uint32_t tiles = (of + (1 << tq_log) - 1) >> tq_log;
+    const int32_t half_way = max(x.row + of / 2, 0);
+    return keys ? tiles * ((a.window ? min(half_way, a.window) : half_way) / S::KEYS + 2) : tiles;
+  };
+  uint32_t all = 0, work_all = 0;
+  for (int32_t i = 0; i < a.tok.B; i += kWave) {
+    all += __builtin_amdgcn_readlane(wave_incl_scan_u32(tiles_of(i + lane, false)), kWave - 1);
+    if (a.nsplit > 1) work_all += __builtin_amdgcn_readlane(wave_incl_scan_u32(tiles_of(i + lane, true)), kWave - 1);
   }
-  s = sequence(a.tok, b);
-  n = min(s.n, a.max_new);
+  if (static_cast<uint32_t>(at) >= all) return;
+  uint32_t want = all - 1 - at;
+  for (b = 0; b < a.tok.B; b += kWave) {
+    const uint32_t upto = wave_incl_scan_u32(tiles_of(b + lane, false));
+    const uint32_t here = __builtin_amdgcn_readlane(upto, kWave - 1);
+    if (want < here) {
+      const int skip = static_cast<int>(popc64(ballot64(upto <= want)));
+      if (skip) want -= __builtin_amdgcn_readlane(upto, skip - 1);
+      b += skip;
+      break;
+    }
+    want -= here;
+  }
+  at = static_cast<int32_t>(want);
+  b = __builtin_amdgcn_readfirstlane(b);
+  const Sequence s = sequence(a.tok, b);
+  const int32_t n = min(s.n, a.max_new);  // of its tokens that take part
 
   // rows of the sequence that its tokens see
   const int32_t i0 = at << tq_log;
@@ -179,9 +180,16 @@ __global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
   if (p_first > p_last) return;
   const int32_t see_first = a.window ? max(p_first - a.window + 1, 0) : 0;
   int32_t tile = see_first / S::KEYS, tile_end = p_last / S::KEYS + 1;
+  int32_t splits = 1;
   if (a.nsplit > 1) {
-    const int32_t per = (tile_end - tile + a.nsplit - 1) / a.nsplit;
-    tile = min(tile + split * per, tile_end);
+    // as many tiles of keys for a workgroup as make a.target of them in all, as far as there is room for partial results
+    const int32_t share = static_cast<int32_t>((static_cast<uint64_t>(work_all) * a.Hkv + a.target - 1) / a.target);
+    const int32_t tiles = tile_end - tile;
+    splits = max(min(tiles / max(share, split_tiles(S::F32)), a.nsplit), 1);
+    const int32_t per = (tiles + splits - 1) / splits;
+    splits = (tiles + per - 1) / per;
+    if (split >= splits) return;
+    tile += split * per;
     tile_end = min(tile + per, tile_end);
   }
 
@@ -473,7 +481,8 @@ __global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
   l += other_half(l);
   if (!mine) return;
   const int64_t unit = static_cast<int64_t>(my_t) * a.Hq + my_h;
-  if (a.nsplit > 1) {
+  if (a.nsplit > 1 && split == 0 && half == 0) a.splits_of[unit] = splits;
+  if (splits > 1) {
     float* part = a.partials + (unit * a.nsplit + split) * D;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -517,13 +526,15 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void join_kernel(PagedAttnArgs 
   const int32_t i = t - s.first, p = s.row + i;
   const int32_t n = min(s.n, a.max_new);
   if (i < 0 || i >= n || n <= a.few >> a.gs || p < 0 || p >= a.tok.N) return;
+  const int32_t splits = __builtin_amdgcn_readfirstlane(a.splits_of[unit]);
+  if (splits < 2) return;  // (its output is there)
   const float* part = a.partials + unit * a.nsplit * D + lane * E;
   const float* pairs = a.partials + a.pairs_off + unit * a.nsplit * 2;
   float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int k = 0; k < a.nsplit; ++k) m = fmaxf(m, pairs[2 * k]);
-  for (int k = 0; k < a.nsplit; ++k) {
+  for (int k = 0; k < splits; ++k) m = fmaxf(m, pairs[2 * k]);
+  for (int k = 0; k < splits; ++k) {
     const float w = exp2_safe(pairs[2 * k] - (m > -INFINITY ? m : 0.f));
     if (pairs[2 * k] == -INFINITY && pairs[2 * k + 1] == 0.f) continue;  // (saw nothing)
     l += pairs[2 * k + 1] * w;
@@ -872,22 +883,19 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
 
 // ---- plans ----------------------------------------------------------------------------------------
 constexpr int64_t kCus = 256;
-constexpr int64_t kChunkTarget = 2 * kCus;  // workgroups of four waves that the chip holds at once
 
 int chunk_keys(const tb_cache_desc& d) { return d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 32 : 64; }
-// Waves of a workgroup: eight read each row of K and V half as often.
+// Waves of a workgroup: eight read each row of K and V half as often, four leave less idle where they see different numbers of rows.
 int chunk_waves(const tb_cache_desc& d, int64_t T) {
-  if (const char* e = getenv("TB_WAVES")) return atoi(e);
-  return T * d.Hq >= 32 * 8 * kCus ? 8 : 4;
+  const int64_t rows = T * d.Hq;
+  return d.dtype == TB_BF16 && d.D == 128 && rows >= 256 * kCus && (rows >= 512 * kCus || d.N >= 4 * T) ? 8 : 4;
 }
-// Splits of a sequence's rows: as many workgroups as the chip holds, of at least four tiles each.
-int64_t chunk_splits(const tb_cache_desc& d, int waves, int64_t tiles) {
-  const int64_t wgs = std::max<int64_t>(tiles * d.Hkv, 1);
-  if (const char* e = getenv("TB_NS")) return atoi(e);
-  return std::max<int64_t>(1, std::min(kChunkTarget * 4 / waves / wgs, d.N / (4 * chunk_keys(d))));
+// Workgroups share the rows of a sequence where those of whole tiles of tokens do not fill the chip: in up to so many splits, which a
+// workspace has room for.
+constexpr int64_t kPartialRows = 262144;
+int64_t chunk_splits(const tb_cache_desc& d, int64_t T) {
+  return std::max<int64_t>(1, std::min(kPartialRows / std::max<int64_t>(T * d.Hq, 1), d.N / (split_tiles(d.dtype == TB_F32) * chunk_keys(d))));
 }
-// Rows times splits that a workspace has room for.
-constexpr int64_t kPartialRows = 131072;
 // ... of at least two steps.
 int64_t token_splits(const tb_cache_desc& d) {
   const int64_t groups = std::max<int64_t>(static_cast<int64_t>(d.B) * d.Hkv, 1), step = d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 16 : 32;
@@ -928,9 +936,11 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
     const int tq_log = __builtin_ctz(32 * waves) - a.gs;
     const int64_t tiles = L.cu ? (L.T >> tq_log) + std::min<int64_t>(d.B, L.T) : d.B * ((std::min<int64_t>(a.tok.each, L.max_new) + (1 << tq_log) - 1) >> tq_log);
     a.few = tokens ? kTokenRows : 0;
-    // (ragged: at least as many tiles as full ones)
-    a.nsplit = static_cast<int32_t>(std::min(std::max<int64_t>(kPartialRows / (L.T * d.Hq), 1), chunk_splits(d, waves, L.cu ? std::max<int64_t>((L.T + (1 << tq_log) - 1) >> tq_log, 1) : tiles)));
+    // what the chip holds at once; a quarter more in fp32, whose products one wave a SIMD keeps busy
+    a.target = static_cast<int32_t>(d.dtype == TB_F32 ? 5 * kCus / 2 : 2 * kCus * 4 / waves);
+    a.nsplit = static_cast<int32_t>(L.T * d.Hq >= 32 * waves * a.target ? 1 : chunk_splits(d, L.T));
     a.pairs_off = static_cast<int64_t>(a.tok.T) * a.Hq * a.nsplit * D;
+    a.splits_of = reinterpret_cast<int32_t*>(a.partials + a.pairs_off + static_cast<int64_t>(a.tok.T) * a.Hq * a.nsplit * 2);
     const dim3 grid(static_cast<unsigned>(d.Hkv * tiles), a.nsplit);
     tb_status rc = waves == 8 ? launch_one(chunk_kernel<T, D, 8>, grid, 8 * kWave, st, a) : launch_one(chunk_kernel<T, D, 4>, grid, 4 * kWave, st, a);
     if (rc != TB_OK) return rc;
@@ -957,9 +967,9 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
 size_t paged_attn_ws_bytes(const tb_cache_desc* d, int64_t T) {
   const int64_t row = (d->D + 2) * static_cast<int64_t>(sizeof(float));
   const int64_t tokens = static_cast<int64_t>(d->B) * d->Hkv * kTokenRows * token_splits(*d);
-  // a call's rows times its splits, where there are several
-  const int64_t chunk = std::min(kPartialRows, T * d->Hq * std::max<int64_t>(1, d->N / (4 * chunk_keys(*d))));
-  return token_counters(*d) + static_cast<size_t>(std::max(tokens, chunk) * row);
+  // a call's rows times its splits, where there are several (of fewer tokens: more splits, but no more rows), and the number of each row's
+  const int64_t rows = std::min(kPartialRows, T * d->Hq), chunk = std::min(kPartialRows, T * d->Hq * std::max<int64_t>(1, d->N / (split_tiles(d->dtype == TB_F32) * chunk_keys(*d))));
+  return token_counters(*d) + static_cast<size_t>(std::max(tokens * row, chunk * row + rows * static_cast<int64_t>(sizeof(int32_t))));
 }
 
 tb_status launch_paged_attn(const PagedAttnLaunch& L, hipStream_t st) {
