@@ -511,41 +511,53 @@ __global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
   if (a.lse && half == 0) a.lse[unit] = any ? m * kLn2 + logf(l) : -INFINITY;
 }
 
-// Adds up the splits of the chunk_kernel: a wave per row.
-constexpr int kJoinWaves = 4;
+// Adds up the splits of the chunk_kernel: a wave for 16 heads of a token, D / 4 lanes a row.
+constexpr int kJoinWaves = 4, kJoinHeads = 16;
 template <typename T, int D>
 __global__ __launch_bounds__(kJoinWaves * kWave) void join_kernel(PagedAttnArgs a) {
-  constexpr int E = D / kWave;
-  const int lane = lane_id();
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kJoinWaves + wave_id();
-  if (unit >= static_cast<int64_t>(a.tok.T) * a.Hq) return;
-  const int32_t t = static_cast<int32_t>(unit / a.Hq), h = static_cast<int32_t>(unit - static_cast<int64_t>(t) * a.Hq);
+  constexpr int LANES = D / 4, ROWS = kWave / LANES;
+  const int lane = lane_id(), d = lane % LANES * 4;
+  const int32_t t = blockIdx.x * kJoinWaves + wave_id();
+  if (t >= a.tok.T) return;
   const int32_t b = sequence_of(a.tok, t);
   if (b >= a.tok.B) return;
   const Sequence s = sequence(a.tok, b);
   const int32_t i = t - s.first, p = s.row + i;
   const int32_t n = min(s.n, a.max_new);
   if (i < 0 || i >= n || n <= a.few >> a.gs || p < 0 || p >= a.tok.N) return;
-  const int32_t splits = __builtin_amdgcn_readfirstlane(a.splits_of[unit]);
-  if (splits < 2) return;  // (its output is there)
-  const float* part = a.partials + unit * a.nsplit * D + lane * E;
-  const float* pairs = a.partials + a.pairs_off + unit * a.nsplit * 2;
-  float m = -INFINITY, l = 0.f, o[E];
+  for (int h0 = 0; h0 < kJoinHeads; h0 += ROWS) {
+    const int h = blockIdx.y * kJoinHeads + h0 + lane / LANES;
+    if (h >= a.Hq) return;
+    const int64_t unit = static_cast<int64_t>(t) * a.Hq + h;
+    const int32_t splits = a.splits_of[unit];
+    if (splits < 2) continue;  // (its output is there)
+    const float* part = a.partials + unit * a.nsplit * D + d;
+    const float* pairs = a.partials + a.pairs_off + unit * a.nsplit * 2;
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < splits; ++k) m = fmaxf(m, pairs[2 * k]);
+    const float m_ref = m > -INFINITY ? m : 0.f;
+    for (int k = 0; k < splits; ++k) {
+      const float2 ml = *reinterpret_cast<const float2*>(pairs + 2 * k);
+      const float4 x = *reinterpret_cast<const float4*>(part + static_cast<int64_t>(k) * D);
+      if (ml.x == -INFINITY && ml.y == 0.f) continue;  // (saw nothing)
+      const float w = exp2_safe(ml.x - m_ref);
+      l += ml.y * w;
+      o[0] += x.x * w;
+      o[1] += x.y * w;
+      o[2] += x.z * w;
+      o[3] += x.w * w;
+    }
+    const bool any = has_weight<true>(l);
+    float f[4];
 #pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int k = 0; k < splits; ++k) m = fmaxf(m, pairs[2 * k]);
-  for (int k = 0; k < splits; ++k) {
-    const float w = exp2_safe(pairs[2 * k] - (m > -INFINITY ? m : 0.f));
-    if (pairs[2 * k] == -INFINITY && pairs[2 * k + 1] == 0.f) continue;  // (saw nothing)
-    l += pairs[2 * k + 1] * w;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += part[static_cast<int64_t>(k) * D + e] * w;
+    for (int e = 0; e < 4; ++e) f[e] = any ? o[e] / l : 0.f;
+    char* out = a.out + t * a.out_t + h * a.out_h + d * sizeof(T);
+    if constexpr (std::is_same<T, float>::value)
+      *reinterpret_cast<uint4*>(out) = pack16(f);
+    else
+      *reinterpret_cast<uint2*>(out) = make_uint2(bf16x2(f[0], f[1]), bf16x2(f[2], f[3]));
+    if (a.lse && d == 0) a.lse[unit] = any ? m * kLn2 + logf(l) : -INFINITY;
   }
-  const bool any = has_weight<true>(l);
-  T* out = reinterpret_cast<T*>(a.out + t * a.out_t + h * a.out_h) + lane * E;
-#pragma unroll
-  for (int e = 0; e < E; ++e) store_elt(out + e, any ? o[e] / l : 0.f);
-  if (a.lse && lane == 0) a.lse[unit] = any ? m * kLn2 + logf(l) : -INFINITY;
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------
@@ -945,8 +957,8 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
     tb_status rc = waves == 8 ? launch_one(chunk_kernel<T, D, 8>, grid, 8 * kWave, st, a) : launch_one(chunk_kernel<T, D, 4>, grid, 4 * kWave, st, a);
     if (rc != TB_OK) return rc;
     if (a.nsplit > 1) {
-      const int64_t units = static_cast<int64_t>(a.tok.T) * a.Hq;
-      rc = launch_one(join_kernel<T, D>, dim3(static_cast<unsigned>((units + kJoinWaves - 1) / kJoinWaves)), kJoinWaves * kWave, st, a);
+      const dim3 rows(static_cast<unsigned>((L.T + kJoinWaves - 1) / kJoinWaves), (d.Hq + kJoinHeads - 1) / kJoinHeads);
+      rc = launch_one(join_kernel<T, D>, rows, kJoinWaves * kWave, st, a);
       if (rc != TB_OK) return rc;
     }
   }
