@@ -355,6 +355,9 @@ __global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
         const float w = exp2_safe(fmaf(x[y / 16][y % 16], a.scale_log2, -m_ref));
         x[y / 16][y % 16] = w;
         l += w;
+        // (kept from being moved behind the products, which pays where four waves a workgroup run out of step: 2048 tokens 64.2 and 60.0 us,
+        // 8192 of D = 64 376 and 361; eight, in step: 1024 over 64000 rows 1985 and 2022)
+        if (!S::F32 && NW == 4 && (y & 1)) asm volatile("" : "+v"(l));
         if (!S::F32 && (y & 1)) p[y / 8][y % 8 / 2] = bf16x2(x[y / 16][y % 16 - 1], w);
       }
     });

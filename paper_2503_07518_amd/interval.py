@@ -213,6 +213,109 @@ class MxIntervalDecoder:
         return self.out, self.lse
 
 
+class PagedIntervalDecoder:
+    """The interval loop over a cache in pages (``binding.PagedCache``), from the prompt on: rows are appended with their rotation, the
+    prompt attends densely, single steps to selected rows.
+
+    ``prompt`` takes the next tokens of every sequence as a model projects them -- queries, keys, values ``[B, n, heads, D]``, any number
+    of times -- puts keys and values into the pages, the keys rotated, and returns the causal attention over all rows so far.  ``step`` takes one token
+    of every sequence and attends as ``IntervalDecoder.step`` does: selected rows on prediction steps, then the widened list and the rows
+    since.  Projected keys (of rotated ones) are kept in a cache of their own, contiguous, a tenth of the pages' size; those of single steps are
+    projected together on the next prediction step.  All sequences have the same number of rows; pages are the caller's to
+    hand out, by writing into the table, before their first row arrives.
+    """
+
+    def __init__(self, cache: tb.PagedCache, W, Hq: int, k: int, P: int, radius: int, sink: int = 0, window: int = 0, sm_scale: float = 1.0,
+                 score_scale: float = 1.0, mode: int = 0, expand_on_predict: bool = False, inv_freq=None, interleaved: bool = False):
+        self.cache, self.W, self.Hq, self.k, self.P, self.radius = cache, W, Hq, k, P, radius
+        self.sink, self.window, self.sm_scale, self.score_scale = sink, window, sm_scale, score_scale
+        self.mode, self.expand_on_predict, self.inv_freq, self.interleaved = mode, expand_on_predict, inv_freq, interleaved
+        _, self.Hkv, page, self.D = cache.K.shape
+        self.B, self.Ncap, dev = cache.table.shape[0], cache.table.shape[1] * page, cache.K.device
+        B = self.B
+        assert W.dtype == cache.dtype and W.dim() == 3 and W.shape[1] == self.D
+        self.sel_cap = sink + k + window
+        self.exp_cap = min(self.Ncap, ((2 * radius + 1) if mode == 0 else 2) * self.sel_cap)
+        self.Kimp = torch.zeros((B, self.Hkv, self.Ncap, W.shape[2]), dtype=cache.dtype, device=dev)
+        self.waiting = torch.empty((B, P, self.Hkv, self.D), dtype=cache.dtype, device=dev)  # rotated keys not projected yet
+        self.scores = torch.empty((B, Hq, (self.Ncap + 3) // 4 * 4), dtype=torch.float32, device=dev)
+        self.idx = torch.zeros((B, Hq, self.sel_cap), dtype=torch.int32, device=dev)
+        self.cnt = torch.zeros((B, Hq), dtype=torch.int32, device=dev)
+        self.exp_idx = torch.zeros((B, Hq, self.exp_cap), dtype=torch.int32, device=dev)
+        self.exp_cnt = torch.zeros((B, Hq), dtype=torch.int32, device=dev)
+        self.out = torch.empty((B, Hq, self.D), dtype=torch.float32, device=dev)
+        self.lse = torch.empty((B, Hq), dtype=torch.float32, device=dev)
+        self.lens = torch.zeros((B,), dtype=torch.int32, device=dev)
+        # (any number of rows may be appended between two predictions)
+        self.ws = tb.new_workspace(tb.TB_OP_ATTN, tb.make_paged_desc(self.Ncap, Hq, cache), self.exp_cap + self.Ncap)
+        self.sel_ws = tb.new_workspace(tb.TB_OP_SELECT, tb.make_desc(self.Ncap, Hq, Kimp=self.Kimp, D=self.D), self.sel_cap)
+        self.N = 0          # rows of every sequence
+        self.n_waiting = 0  # the last ones of them, whose keys wait
+        self.N_pred = None
+
+    def _append(self, q, k, v):
+        """Rows of n more tokens; returns rotated queries and keys [B n, heads, D]."""
+        B, n = q.shape[:2]
+        assert q.shape == (self.B, n, self.Hq, self.D) and k.shape == v.shape == (B, n, self.Hkv, self.D)
+        if self.N + n > self.Ncap:
+            raise ValueError(f"{self.N} + {n} rows in a cache for {self.Ncap}")
+        q, k, v = (x.reshape(B * n, x.shape[2], self.D) for x in (q, k, v))
+        self.N += n
+        self.lens.fill_(self.N)
+        q_rot, k_rot = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        tb.tb_append_paged_kv(tb.make_paged_desc(self.N, self.Hq, self.cache), self.cache, q, k, v, None, self.lens, self.inv_freq, q_rot, k_rot,
+                              interleaved=self.interleaved)
+        return q_rot, k_rot
+
+    def _project(self, keys, first: int) -> None:
+        """Projected keys of rows [first, first + n) from rotated keys [B, n, Hkv, D]."""
+        keys, rows = keys.transpose(1, 2), self.Kimp[:, :, first:first + keys.shape[1]]
+        n = keys.shape[2]
+        tb.tb_project_keys(tb.make_desc(n, self.Hq, K=keys, Kimp=rows), keys, self.W, rows, 0, n)
+
+    def _project_waiting(self, upto: int) -> None:
+        if self.n_waiting:
+            self._project(self.waiting[:, :self.n_waiting], upto - self.n_waiting)
+            self.n_waiting = 0
+
+    def prompt(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> torch.Tensor:
+        """The next n tokens of every sequence; their attention over all rows so far, [B, n, Hq, D]."""
+        B, n = q.shape[:2]
+        if n == 0:
+            return torch.empty_like(q)
+        self._project_waiting(self.N)
+        q_rot, k_rot = self._append(q, k, v)
+        desc = tb.make_paged_desc(self.N, self.Hq, self.cache)
+        out = torch.empty_like(q_rot)
+        tb.tb_paged_attn(desc, self.cache, q_rot, None, self.lens, n, self.sm_scale, out, None, tb.new_workspace(tb.TB_OP_PAGED_ATTN, desc, B * n))
+        self._project(k_rot.view(B, n, self.Hkv, self.D), self.N - n)
+        return out.view(B, n, self.Hq, self.D)
+
+    def step(self, t: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_imp: torch.Tensor):
+        """Step t: one token of every sequence, q [B, Hq, D], k, v [B, Hkv, D], importance queries [B, Hq, d'].  Returns (out, lse) views
+        valid until the next call."""
+        q_rot, k_rot = self._append(q.unsqueeze(1), k.unsqueeze(1), v.unsqueeze(1))
+        N, B = self.N, self.B
+        if self.n_waiting == self.P:
+            self._project_waiting(N - 1)
+        self.waiting[:, self.n_waiting].copy_(k_rot)
+        self.n_waiting += 1
+        desc = tb.make_paged_desc(N, self.Hq, self.cache)
+        if t % self.P == 0:
+            self._project_waiting(N)
+            lists = tb.make_desc(N, self.Hq, Kimp=self.Kimp, D=self.D)
+            tb.tb_score(lists, q_imp, self.Kimp, self.score_scale, self.scores)
+            tb.tb_select_topk(lists, self.scores, self.k, self.sink, self.window, self.idx, self.cnt, self.sel_ws)
+            tb.tb_expand_neighbors(B, self.Hq, N, self.radius, self.mode, self.idx, self.cnt, self.exp_idx, self.exp_cnt)
+            self.N_pred = N
+        if t % self.P == 0 and not self.expand_on_predict:
+            tb.tb_sparse_decode_attn_paged(desc, self.cache, q_rot, self.idx, self.cnt, self.sel_cap, self.sm_scale, self.out, self.lse, self.ws)
+        else:
+            tb.tb_sparse_decode_attn_paged(desc, self.cache, q_rot, self.exp_idx, self.exp_cnt, self.exp_cap, self.sm_scale, self.out, self.lse,
+                                           self.ws, tail_begin=self.N_pred, tail_end=N)
+        return self.out, self.lse
+
+
 class RingLayoutDecoder:
     """The three physical buffers of Sec. 3.3 "Inference Setup", driven through the C-ABI calls.
 
