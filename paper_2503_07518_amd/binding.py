@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -280,7 +281,7 @@ class PagedCache:
         self.desc = tb_paged_cache(K.data_ptr(), V.data_ptr(), table.data_ptr(), K.shape[0], K.shape[2], table.shape[1],
                                    table.stride(0) if table.shape[0] > 1 else table.shape[1], *_strides3(K), *_strides3(V))
         self.ref = ctypes.byref(self.desc)
-        self.device, self.dtype = K.get_device(), K.dtype
+        self.device, self.dtype, self.B = K.get_device(), K.dtype, table.shape[0]
         if not self.device == V.get_device() == table.get_device():
             raise ValueError(f"K on {K.device}, V on {V.device}, table on {table.device}")
 
@@ -297,6 +298,7 @@ def make_paged_desc(N: int, Hq: int, cache: PagedCache) -> tb_cache_desc:
 
 # tb_token_rows of a call's tensors, one after the other: a fifth of the cost of a structure each
 _two_rows, _five_rows = ctypes.c_int64 * 6, ctypes.c_int64 * 15
+_pack_two, _pack_five = struct.Struct("6q").pack, struct.Struct("15q").pack
 _ROWS = ctypes.sizeof(tb_token_rows)
 
 
@@ -523,8 +525,8 @@ def tb_sparse_decode_attn_shared_mx(desc, q, K: MxRows, V: MxRows, idx, count, m
 
 
 def _check_tokens(desc, cache: PagedCache, cu, lens) -> None:
-    B = desc.B
-    assert lens.dtype is torch.int32 and lens.shape == (B,) and (B < 2 or lens.stride(0) == 1) and B == cache.table.shape[0]
+    B = cache.B
+    assert desc.B == B and lens.dtype is torch.int32 and lens.shape == (B,) and lens.is_contiguous()
     assert cu is None or (cu.dtype is torch.int32 and cu.shape == (B + 1,) and cu.is_contiguous())
 
 
@@ -540,7 +542,7 @@ def tb_append_paged_kv(desc, cache: PagedCache, q, k, v, cu, lens, inv_freq, q_o
     k_t, k_h, k_d = k.stride()
     v_t, v_h, v_d = v.stride()
     assert v.shape == shape and Hkv == desc.Hkv and D == desc.D and k.dtype is dtype and v.dtype is dtype and k_d == v_d == 1
-    qp = qop = kop = None
+    qp = qop = kop = 0
     q_t = q_h = qo_t = qo_h = ko_t = ko_h = 0
     if q is not None or q_out is not None:
         q_t, q_h, q_d = q.stride()
@@ -558,7 +560,7 @@ def tb_append_paged_kv(desc, cache: PagedCache, q, k, v, cu, lens, inv_freq, q_o
         rot, fp = 2 * rot, inv_freq.data_ptr()
     assert positions is None or (positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (T,))
     _check_tokens(desc, cache, cu, lens)
-    rows = _five_rows(qp or 0, q_t, q_h, k.data_ptr(), k_t, k_h, v.data_ptr(), v_t, v_h, qop or 0, qo_t, qo_h, kop or 0, ko_t, ko_h)
+    rows = _five_rows.from_buffer_copy(_pack_five(qp, q_t, q_h, k.data_ptr(), k_t, k_h, v.data_ptr(), v_t, v_h, qop, qo_t, qo_h, kop, ko_t, ko_h))
     at = ctypes.addressof(rows)
     rc = (_lib or load_library()).tb_append_paged_kv(
         ctypes.byref(desc), cache.ref, T, None if cu is None else cu.data_ptr(), lens.data_ptr(), None if positions is None else positions.data_ptr(), fp,
@@ -580,7 +582,7 @@ def tb_paged_attn(desc, cache: PagedCache, q, cu, lens, max_new: int, sm_scale: 
     assert out.shape == shape and Hq == desc.Hq and D == desc.D and q.dtype is dtype and out.dtype is dtype and q_d == o_d == 1
     assert lse is None or (lse.dtype is torch.float32 and lse.shape == (T, Hq) and lse.is_contiguous())
     _check_tokens(desc, cache, cu, lens)
-    rows = _two_rows(q.data_ptr(), q_t, q_h, out.data_ptr(), o_t, o_h)
+    rows = _two_rows.from_buffer_copy(_pack_two(q.data_ptr(), q_t, q_h, out.data_ptr(), o_t, o_h))
     at = ctypes.addressof(rows)
     rc = (_lib or load_library()).tb_paged_attn(
         ctypes.byref(desc), cache.ref, T, None if cu is None else cu.data_ptr(), lens.data_ptr(), max_new, at, window, sm_scale, at + _ROWS,
