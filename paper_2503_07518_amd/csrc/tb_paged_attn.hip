@@ -430,6 +430,11 @@ __global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
   // In LDS are the tile's V and the next one's K, or on their way there; the next V and the K behind that are asked for when all waves
   // have read what they replace.
   const int32_t tile_first = tile;
+  // A wave's loads into LDS have arrived, then those of all.  (The barrier alone does not wait for them: they count as loads from memory.)
+  auto arrive = []() {
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+  };
   if (tile < tile_end) {
     int32_t page = pages_of_tile(tile), page_next = pages_of_tile(tile + 1), page_2 = pages_of_tile(tile + 2);
     unsigned long long next = rows_there(tile + 1, page_next);
@@ -439,13 +444,13 @@ __global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
       stage(std::false_type{}, s_k0, tile, page, there);
       stage(std::true_type{}, s_v0, tile, page, there);
       if (tile + 1 < tile_end) stage(std::false_type{}, s_k1, tile + 1, page_next, next);
-      __syncthreads();
+      arrive();
       scores(s_k0, x0, [](int) {});
       see(x0, tile, there);
       follow(largest(x0));
     }
     auto step = [&](f32x16(&x)[KB], f32x16(&x_next)[KB], char* sk, char* sk_next, char* sv, char* sv_next) {
-      __syncthreads();
+      arrive();
       guard(sv, tile);
       const unsigned long long next_2 = rows_there(tile + 2, page_2);
       if (tile + 1 < tile_end) stage(std::true_type{}, sv_next, tile + 1, page_next, next);

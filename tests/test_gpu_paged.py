@@ -253,6 +253,42 @@ def test_attn_strides_and_no_lse():
     assert torch.equal(o[:, :, :64], out) and bool((o[:, :, 64:] == 7).all())
 
 
+@pytest.mark.parametrize("dtype,Hq,D,new,kept", [(BF, 64, 128, 1024, 40000), (BF, 32, 128, 4099, 0), (BF, 32, 128, 300, 30011), (BF, 32, 64, 2048, 9000),
+                                                 (F32, 16, 128, 500, 6000), (F32, 16, 64, 2049, 77)])
+def test_long_calls(dtype, Hq, D, new, kept):
+    """Calls that fill the GPU, in all of its workgroup shapes, against 64 bits on the GPU, and every time the same bits."""
+    Hkv, page, n = 8, 64, new + kept
+    gen = torch.Generator(device=DEV).manual_seed(n)
+    entries = -(-n // page)
+    table = torch.randperm(entries + 3, generator=gen, device=DEV)[:entries].view(1, entries).to(torch.int32)
+    K, V = (torch.randn((entries + 3, Hkv, page, D), generator=gen, device=DEV).to(dtype) for _ in range(2))
+    q = (1.5 * torch.randn((new, Hq, D), generator=gen, device=DEV)).to(dtype)
+    cache, scale = tb.PagedCache(K, V, table), D ** -0.5
+    desc = tb.make_paged_desc(n, Hq, cache)
+    ws = tb.new_workspace(tb.TB_OP_PAGED_ATTN, desc, new)
+    lens, cu = torch.tensor([n], dtype=torch.int32, device=DEV), torch.tensor([0, new], dtype=torch.int32, device=DEV)
+    runs = []
+    for i in range(6):
+        out, lse = torch.empty_like(q), torch.empty((new, Hq), device=DEV)
+        tb.tb_paged_attn(desc, cache, q, cu if i % 2 else None, lens, new, scale, out, lse, ws)
+        runs.append((out, lse))
+    torch.cuda.synchronize()
+    for out, lse in runs[1:]:
+        assert torch.equal(out, runs[0][0]) and torch.equal(lse, runs[0][1])
+    rows, p = torch.arange(n, device=DEV), torch.arange(kept, n, device=DEV)[:, None]
+    at = table[0, rows // page].long()
+    c = type("c", (), dict(D=D, dtype=dtype))
+    for h in range(0, Hq, 5):
+        Kh, Vh = (x[at, h * Hkv // Hq, rows % page].double() for x in (K, V))
+        x = (q[:, h].double() @ Kh.T * scale).masked_fill_(rows > p, -math.inf)
+        lse = torch.logsumexp(x, 1)
+        w = torch.exp(x - lse[:, None])
+        want, mag = w @ Vh, w @ Vh.abs()
+        tol, tol_lse = attn_bounds(c, q[:, h].cpu(), Kh.cpu(), Vh.cpu(), n, scale, mag.cpu(), want.cpu())
+        close(runs[0][0][:, h], want.cpu(), tol, f"out, head {h}")
+        close(runs[0][1][:, h], lse.cpu(), tol_lse + lse.abs().cpu() * 2.0 ** -22, f"lse, head {h}")
+
+
 # ---- attention over lists ---------------------------------------------------------------------------
 def lists(c, k, seed=0):
     gen = torch.Generator().manual_seed(seed)
