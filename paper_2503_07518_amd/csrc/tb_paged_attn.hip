@@ -349,18 +349,20 @@ __global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
     const float m_ref = m > -INFINITY ? m : 0.f;  // nothing seen yet: all weights 0
     constexpr int STEPS = KB * S::PAIRS, EACH = KB * 16 / STEPS;  // weights a product
     u32x4 p[S::F32 ? 1 : 2 * KB];
+    float sum = 0.f;  // (the tile's weights on their own: their roundings are of its size)
     scores(sk, x_next, [&](int i) {
 #pragma unroll
       for (int y = i * EACH; y < (i + 1) * EACH; ++y) {
         const float w = exp2_safe(fmaf(x[y / 16][y % 16], a.scale_log2, -m_ref));
         x[y / 16][y % 16] = w;
-        l += w;
+        sum += w;
         // (kept from being moved behind the products, which pays where four waves a workgroup run out of step: 2048 tokens 64.2 and 60.0 us,
         // 8192 of D = 64 376 and 361; eight, in step: 1024 over 64000 rows 1985 and 2022)
-        if (!S::F32 && NW == 4 && (y & 1)) asm volatile("" : "+v"(l));
+        if (!S::F32 && NW == 4 && (y & 1)) asm volatile("" : "+v"(sum));
         if (!S::F32 && (y & 1)) p[y / 8][y % 8 / 2] = bf16x2(x[y / 16][y % 16 - 1], w);
       }
     });
+    l += sum;
     // V's operands, of bf16 a column of four rows a lane, transposed on the way
     constexpr int VF = S::F32 ? 4 * KB : 2 * KB;  // steps of 16 keys (bf16), four of one key a half (fp32)
     const int at_v = hidden(v_at);
