@@ -321,7 +321,7 @@ typedef struct tb_token_rows {
 /* New tokens of the sequences reach the cache, their queries and keys rotated by their positions on the way.
  * The T tokens of a call are those of sequence 0, then of sequence 1, ...: sequence b has the tokens cu[b] .. cu[b+1]-1 (cu: int32 [B+1],
  * cu[0] = 0; NULL: T / B tokens each), which are the last of its lens[b] rows (int32 [B], on the device as cu is): token number i of n
- * is row lens[b] - n + i.  Tokens whose row is not in [0, N), and those from cu[B] on, take no part: nothing of theirs is read or written.
+ * is row lens[b] - n + i.  T <= 2^22 (else TB_ERR_UNSUPPORTED).  Tokens whose row is not in [0, N), and those from cu[B] on, take no part: nothing of theirs is read or written.
  *   angle(t, i) = positions[t] * inv_freq[i]   0 <= i < rot / 2; positions: int32 [T], NULL: the token's row; inv_freq: fp32 [rot / 2]
  *   (x[j], x[k]) -> (x[j] cos - x[k] sin, x[k] cos + x[j] sin)   of q and k, (j, k) = (i, i + rot / 2), or (2i, 2i + 1) if interleaved
  * with one rounding at the end, angles in 64 bits; elements from rot on stay as they are.  rot: 0 (no rotation) to D, a multiple of 16.
@@ -340,7 +340,7 @@ tb_status tb_append_paged_kv(const tb_cache_desc* desc, const tb_paged_cache* ca
  * out has the element type of q (one rounding; weights are rounded to that type, too, before they meet V); lse: fp32 [T][Hq] or NULL.  A
  * token that attends to nothing, or with scores of minus infinity alone, has out = 0 and lse = -inf.  Rows that a token does not attend to
  * add nothing to its result, whatever they hold.
- * ws: tb_workspace_bytes(TB_OP_PAGED_ATTN, desc, T). */
+ * ws: tb_workspace_bytes(TB_OP_PAGED_ATTN, desc, T); calls that share it have the same Hkv, too. */
 tb_status tb_paged_attn(const tb_cache_desc* desc, const tb_paged_cache* cache, int64_t T, const int32_t* cu, const int32_t* lens,
                         int64_t max_new, const tb_token_rows* q, int64_t window, float sm_scale, const tb_token_rows* out, float* lse,
                         void* ws, size_t ws_bytes, void* stream);

@@ -511,14 +511,14 @@ tb_status check_paged(const tb_cache_desc* d, const tb_paged_cache* c) {
 
 // (rows that are read may be the same ones for several heads or tokens, those that are written may not)
 tb_status check_token_rows(const tb_cache_desc* d, const tb_token_rows* r, int64_t T, int32_t heads, bool written) {
-  if (!r || !r->rows) return TB_ERR_INVALID_ARG;
+  if (!r || (!r->rows && T > 0)) return TB_ERR_INVALID_ARG;
   if (written && ((heads > 1 && r->stride_h < d->D) || (T > 1 && r->stride_t < d->D))) return TB_ERR_INVALID_ARG;
   return aligned16(r->rows) ? check_strides(d, r->stride_t, r->stride_h, d->D, d->D) : TB_ERR_UNSUPPORTED;
 }
 
 tb_status check_tokens(const tb_cache_desc* d, int64_t T, const int32_t* cu, const int32_t* lens) {
-  if (T < 0 || !lens || (!cu && (d->B == 0 ? T != 0 : T % d->B != 0))) return TB_ERR_INVALID_ARG;
-  return T <= (int64_t{1} << 24) ? TB_OK : TB_ERR_UNSUPPORTED;  // (of a grid's numbers)
+  if (T < 0 || (!lens && d->B > 0) || (!cu && (d->B == 0 ? T != 0 : T % d->B != 0))) return TB_ERR_INVALID_ARG;
+  return T <= (int64_t{1} << 22) ? TB_OK : TB_ERR_UNSUPPORTED;  // (of a launch's threads, which are numbered with 32 bits)
 }
 
 }  // namespace

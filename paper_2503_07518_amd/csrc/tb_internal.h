@@ -287,7 +287,7 @@ struct PagedAttnLaunch {
   void* ws;
 };
 tb_status launch_paged_attn(const PagedAttnLaunch& a, hipStream_t st);
-// Bytes of workspace that calls of up to T tokens take: counters [B * Hkv], 256 B apart, then partial results.
+// Bytes of workspace that calls of up to T tokens take: the counters as in WsLayout, then partial results.
 size_t paged_attn_ws_bytes(const tb_cache_desc* d, int64_t T);
 
 // Query predictor of a producer layer (LN + two-layer MLP), see tb_predict.hip.

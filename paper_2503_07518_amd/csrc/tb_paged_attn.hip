@@ -923,7 +923,10 @@ int64_t token_splits(const tb_cache_desc& d) {
   const int64_t groups = std::max<int64_t>(static_cast<int64_t>(d.B) * d.Hkv, 1), step = d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 16 : 32;
   return std::max<int64_t>(1, std::min(kCus / groups, d.N / (2 * step)));
 }
-size_t token_counters(const tb_cache_desc& d) { return static_cast<size_t>(d.B) * d.Hkv * kCounterStrideWords * sizeof(uint32_t); }
+// Partial results lie behind the counters of B * Hq units, as in the workspaces of the other operations, so that one may serve several.
+size_t partials_at(const tb_cache_desc& d) { return ws_layout(static_cast<int64_t>(d.B) * d.Hq, d.D, 1).part_off; }
+// (of a launch's threads, which are numbered with 32 bits)
+constexpr int64_t kMostTiles = 1 << 22;
 
 template <typename T, int D>
 tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
@@ -949,7 +952,7 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
   a.max_new = static_cast<int32_t>(L.max_new);
   a.window = static_cast<int32_t>(std::min<int64_t>(L.window, d.N));
   a.counters = static_cast<uint32_t*>(L.ws);
-  a.partials = reinterpret_cast<float*>(static_cast<char*>(L.ws) + token_counters(d));
+  a.partials = reinterpret_cast<float*>(static_cast<char*>(L.ws) + partials_at(d));
   const int64_t most = L.cu ? L.max_new : a.tok.each;  // tokens of a sequence, at most
   const bool chunks = most << a.gs > kTokenRows;
   const bool tokens = !chunks || (L.cu && d.B > 1);  // sequences of few tokens may be among the others
@@ -957,6 +960,7 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
     const int waves = chunk_waves(d, L.T);
     const int tq_log = __builtin_ctz(32 * waves) - a.gs;
     const int64_t tiles = L.cu ? (L.T >> tq_log) + std::min<int64_t>(d.B, L.T) : d.B * ((std::min<int64_t>(a.tok.each, L.max_new) + (1 << tq_log) - 1) >> tq_log);
+    if (d.Hkv * tiles > kMostTiles) return TB_ERR_UNSUPPORTED;
     a.few = tokens ? kTokenRows : 0;
     // what the chip holds at once; a quarter more in fp32, whose products one wave a SIMD keeps busy
     a.target = static_cast<int32_t>(d.dtype == TB_F32 ? 5 * kCus / 2 : 2 * kCus * 4 / waves);
@@ -991,7 +995,7 @@ size_t paged_attn_ws_bytes(const tb_cache_desc* d, int64_t T) {
   const int64_t tokens = static_cast<int64_t>(d->B) * d->Hkv * kTokenRows * token_splits(*d);
   // a call's rows times its splits, where there are several (of fewer tokens: more splits, but no more rows), and the number of each row's
   const int64_t rows = std::min(kPartialRows, T * d->Hq), chunk = std::min(kPartialRows, T * d->Hq * std::max<int64_t>(1, d->N / (split_tiles(d->dtype == TB_F32) * chunk_keys(*d))));
-  return token_counters(*d) + static_cast<size_t>(std::max(tokens * row, chunk * row + rows * static_cast<int64_t>(sizeof(int32_t))));
+  return partials_at(*d) + static_cast<size_t>(std::max(tokens * row, chunk * row + rows * static_cast<int64_t>(sizeof(int32_t))));
 }
 
 tb_status launch_paged_attn(const PagedAttnLaunch& L, hipStream_t st) {

@@ -443,6 +443,39 @@ def test_two_streams_with_workspaces_of_their_own():
         assert torch.equal(o, o2) and torch.equal(l, l2)
 
 
+def test_no_tokens():
+    c = on_gpu(make(BF, 4, 2, 64, 16, [0, 0], [9, 40]))
+    lens = c.lens.to(DEV)
+    none, kv = torch.empty((0, 4, 64), dtype=BF, device=DEV), torch.empty((0, 2, 64), dtype=BF, device=DEV)
+    for cu in (None, c.cu.to(DEV)):
+        tb.tb_append_paged_kv(c.desc, c.cache, none, kv, kv, cu, lens, inv_freq(64).to(DEV), none, kv)
+        tb.tb_paged_attn(c.desc, c.cache, none, cu, lens, 5, 0.1, none, None, tb.new_workspace(tb.TB_OP_PAGED_ATTN, c.desc, 0))
+    torch.cuda.synchronize()
+
+
+def test_one_workspace_for_both_attentions():
+    """Each leaves the other's counters as they were: lists that are split, then sequences that are, and so on."""
+    c = on_gpu(make(BF, 8, 2, 128, 16, [1, 1, 1], [2000, 1500, 900]))
+    idx = torch.arange(800, dtype=torch.int32).expand(3, 8, 800).contiguous().to(DEV)
+    count = torch.full((3, 8), 800, dtype=torch.int32, device=DEV)
+    q = c.q.to(DEV)
+    size = max(tb.tb_workspace_bytes(tb.TB_OP_PAGED_ATTN, c.desc, 3), tb.tb_workspace_bytes(tb.TB_OP_ATTN, c.desc, 800))
+    ws = torch.zeros(size, dtype=torch.uint8, device=DEV)
+    first = None
+    for _ in range(4):
+        a = run_attn(c, 0.09, ws=ws)
+        out, lse = torch.zeros((3, 8, 128), device=DEV), torch.zeros((3, 8), device=DEV)
+        tb.tb_sparse_decode_attn_paged(c.desc, c.cache, q, idx, count, 800, 0.09, out, lse, ws)
+        torch.cuda.synchronize()
+        got = (*a, out, lse)
+        if first is None:
+            first = got
+            want, l = run_sparse(c, c.q, idx.cpu(), count.cpu(), 800, (0, 0), 0.09)
+            assert torch.equal(out, want) and torch.equal(lse, l)
+        for x, y in zip(got, first):
+            assert torch.equal(x, y)
+
+
 def test_one_workspace_for_calls_of_all_kinds():
     """A workspace made for the most tokens serves every smaller call, one after the other, and is left as it was found."""
     c = on_gpu(make(BF, 8, 2, 128, 16, [70, 1, 9], [300, 2000, 40]))

@@ -74,11 +74,11 @@ def test_caches_refused(lib, call, want, kw):
 
 
 @pytest.mark.parametrize("want,kw", [
-    (INV, dict(T=-1)), (INV, dict(lens=None)), (INV, dict(cu=None, T=5)), (UNS, dict(T=(1 << 24) + 1)), (INV, dict(k=None)), (INV, dict(v=None)),
+    (INV, dict(T=-1)), (INV, dict(lens=None)), (INV, dict(cu=None, T=5)), (UNS, dict(T=(1 << 22) + 1)), (INV, dict(k=None)), (INV, dict(v=None)),
     (INV, dict(q=None)), (INV, dict(qo=None)), (INV, dict(rot=-16)), (INV, dict(rot=144)), (UNS, dict(rot=24)), (INV, dict(f=None)),
     (INV, dict(k=rows(2, rows=None))), (UNS, dict(k=rows(2, rows=P + 8))), (UNS, dict(v=rows(2, stride_t=260))), (INV, dict(ko=rows(2, stride_h=64))), (INV, dict(qo=rows(stride_t=64))),
     (INV, dict(ko=rows(2, stride_t=-256))), (UNS, dict(qo=rows(rows=P + 4))),
-    (OK, dict(T=0)), (OK, dict(T=0, q=None, qo=None, ko=None, rot=0, f=None)), (OK, dict(d=desc(B=0), T=0, cu=None)),
+    (OK, dict(T=0)), (OK, dict(T=0, k=rows(2, rows=None), v=rows(2, rows=None), ko=None)), (OK, dict(T=0, q=None, qo=None, ko=None, rot=0, f=None)), (OK, dict(d=desc(B=0), T=0, cu=None)),
 ])
 def test_append_refusals(lib, want, kw):
     assert append(lib, **kw) == want
@@ -87,7 +87,8 @@ def test_append_refusals(lib, want, kw):
 @pytest.mark.parametrize("want,kw", [
     (INV, dict(T=-1)), (INV, dict(lens=None)), (INV, dict(cu=None, T=5)), (INV, dict(most=-1)), (INV, dict(window=-1)), (INV, dict(q=None)),
     (INV, dict(out=None)), (INV, dict(out=rows(stride_h=120))), (INV, dict(out=rows(stride_t=64))), (UNS, dict(q=rows(rows=P + 8))), (UNS, dict(out=rows(stride_t=1028))),
-    (WS, dict(ws=None)), (WS, dict(ws=P + 8)), (WS, dict(ws_bytes=100)), (OK, dict(T=0)), (OK, dict(most=0)), (OK, dict(d=desc(B=0), T=0)),
+    (WS, dict(ws=None)), (WS, dict(ws=P + 8)), (WS, dict(ws_bytes=100)), (OK, dict(T=0)), (OK, dict(T=0, q=rows(rows=None), out=rows(rows=None))), (OK, dict(most=0)),
+    (UNS, dict(T=(1 << 22) + 1)), (UNS, dict(T=1 << 22, most=1 << 22, d=desc(Hq=4096, Hkv=4096), ws_bytes=1 << 62)), (OK, dict(d=desc(B=0), T=0)),
     (OK, dict(d=desc(Hq=0, Hkv=0))),
 ])
 def test_attn_refusals(lib, want, kw):
