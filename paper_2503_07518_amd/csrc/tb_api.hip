@@ -504,7 +504,7 @@ tb_status check_paged(const tb_cache_desc* d, const tb_paged_cache* c) {
   TB_TRY(check_strides(d, c->k_stride_p, c->k_stride_h, c->k_stride_n, d->D));
   TB_TRY(check_strides(d, c->v_stride_p, c->v_stride_h, c->v_stride_n, d->D));
   // (a page's rows of a head are addressed with 32-bit offsets)
-  if (c->k_stride_n * c->page >= (int64_t{1} << 29) || c->v_stride_n * c->page >= (int64_t{1} << 29)) return TB_ERR_UNSUPPORTED;
+  if (c->k_stride_n >= (int64_t{1} << 29) / c->page || c->v_stride_n >= (int64_t{1} << 29) / c->page) return TB_ERR_UNSUPPORTED;
   if (!aligned16(c->K) || !aligned16(c->V)) return TB_ERR_UNSUPPORTED;
   return TB_OK;
 }

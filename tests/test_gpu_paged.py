@@ -443,6 +443,31 @@ def test_two_streams_with_workspaces_of_their_own():
         assert torch.equal(o, o2) and torch.equal(l, l2)
 
 
+def test_a_pool_of_more_than_32_bits():
+    """Pages behind the first 4 GiB of a pool whose other pages no table names (all NaN the first of them): the bits of a small pool's."""
+    c = on_gpu(make(BF, 16, 8, 128, 16, [1, 40], [600, 700]))
+    more = (1 << 32) // c.K[0].nbytes + 5
+    K, V = (torch.empty((more + x.shape[0], *x.shape[1:]), dtype=BF, device=DEV) for x in (c.K, c.V))
+    for x, y in ((K, c.K), (V, c.V)):
+        x[0] = math.nan
+        x[more:] = y.to(DEV)
+    far = on_gpu(make(BF, 16, 8, 128, 16, [1, 40], [600, 700]))
+    far.cache = tb.PagedCache(K, V, (c.table + more).to(DEV))
+    idx, count = lists(c, 300)
+    idx[1, 3, 7:] = -1
+    got = []
+    for x in (c, far):
+        k, v = x.k.to(DEV), x.v.to(DEV)
+        tb.tb_append_paged_kv(x.desc, x.cache, None, k, v, x.cu.to(DEV), x.lens.to(DEV), inv_freq(128).to(DEV), None, None)
+        mixed = run_attn(x, 0.09)
+        one = make(BF, 16, 8, 128, 16, [1, 1], [600, 739])
+        one.cache, one.desc = x.cache, x.desc
+        got.append((*mixed, *run_attn(one, 0.09), *run_sparse(x, one.q, idx, count, 300, (590, 601), 0.09)))
+    for a, b in zip(*got):
+        assert torch.equal(a, b) and bool(torch.isfinite(a).all())
+    assert same_bits(c.cache.K, K[more:]) and same_bits(c.cache.V, V[more:])
+
+
 def test_no_tokens():
     c = on_gpu(make(BF, 4, 2, 64, 16, [0, 0], [9, 40]))
     lens = c.lens.to(DEV)

@@ -61,7 +61,7 @@ CACHES = [
     (INV, dict(c=cache(table_len=-1))), (INV, dict(c=cache(table_stride=-64))), (INV, dict(c=cache(k_stride_p=-8))), (INV, dict(c=cache(v_stride_n=64))),
     (UNS, dict(c=cache(page=8, table_len=200))), (UNS, dict(c=cache(page=48))), (UNS, dict(c=cache(page=1 << 17))),
     (UNS, dict(c=cache(k_stride_h=1028))), (UNS, dict(c=cache(v_stride_p=4100))), (UNS, dict(c=cache(K=P + 8))), (UNS, dict(c=cache(V=P + 2))),
-    (UNS, dict(c=cache(k_stride_n=1 << 25))), (UNS, dict(d=desc(N=(1 << 30) + 1), c=cache(page=65536, table_len=1 << 20))),
+    (UNS, dict(c=cache(k_stride_n=1 << 25))), (UNS, dict(c=cache(k_stride_n=1 << 60))), (UNS, dict(c=cache(v_stride_n=1 << 59))), (UNS, dict(d=desc(N=(1 << 30) + 1), c=cache(page=65536, table_len=1 << 20))),
     (INV, dict(d=desc(dtype=5))), (INV, dict(d=desc(Hq=7))), (UNS, dict(d=desc(D=96))), (UNS, dict(d=desc(Hq=32))), (INV, dict(d=desc(N=-1))),
     (UNS, dict(d=desc(B=65536))),
 ]
