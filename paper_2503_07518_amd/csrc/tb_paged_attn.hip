@@ -37,7 +37,7 @@ struct PagedAttnArgs {
   int32_t max_new, window;
   int32_t nsplit;      // at most
   int32_t target;      // chunk_kernel: workgroups that share the keys
-  int32_t* splits_of;  // ... and how many a row has got
+  int32_t* splits_of;  // ... and how many a token's rows have got
   int32_t few;  // chunk_kernel: sequences with up to so many rows are the token_kernel's
   float* partials;
   int64_t pairs_off;
@@ -491,7 +491,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
   l += other_half(l);
   if (!mine) return;
   const int64_t unit = static_cast<int64_t>(my_t) * a.Hq + my_h;
-  if (a.nsplit > 1 && split == 0 && half == 0) a.splits_of[unit] = splits;
+  if (a.nsplit > 1 && split == 0 && half == 0 && my_h == 0) a.splits_of[my_t] = splits;  // (the same for all heads)
   if (splits > 1) {
     float* part = a.partials + (unit * a.nsplit + split) * D;
 #pragma unroll
@@ -521,12 +521,14 @@ __global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
   if (a.lse && half == 0) a.lse[unit] = any ? m * kLn2 + logf(l) : -INFINITY;
 }
 
-// Adds up the splits of the chunk_kernel: a wave for 16 heads of a token, D / 4 lanes a row.
-constexpr int kJoinWaves = 4, kJoinHeads = 16;
+// Adds up the splits of the chunk_kernel: D / 4 lanes a row, a wave for two or four heads of a token.  A row's references are read by its
+// lanes at once, eight of its partial results are on their way together (32 heads, 64 tokens over 30000 rows, 26 splits: with a wave for 16 heads and one
+// partial result at a time 160 us of the call's 213, so 13 of 68).
+constexpr int kJoinWaves = 4;
 template <typename T, int D>
 __global__ __launch_bounds__(kJoinWaves * kWave) void join_kernel(PagedAttnArgs a) {
   constexpr int LANES = D / 4, ROWS = kWave / LANES;
-  const int lane = lane_id(), d = lane % LANES * 4;
+  const int lane = lane_id(), j = lane % LANES, r = lane / LANES;
   const int32_t t = blockIdx.x * kJoinWaves + wave_id();
   if (t >= a.tok.T) return;
   const int32_t b = sequence_of(a.tok, t);
@@ -535,39 +537,52 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void join_kernel(PagedAttnArgs 
   const int32_t i = t - s.first, p = s.row + i;
   const int32_t n = min(s.n, a.max_new);
   if (i < 0 || i >= n || n <= a.few >> a.gs || p < 0 || p >= a.tok.N) return;
-  for (int h0 = 0; h0 < kJoinHeads; h0 += ROWS) {
-    const int h = blockIdx.y * kJoinHeads + h0 + lane / LANES;
-    if (h >= a.Hq) return;
-    const int64_t unit = static_cast<int64_t>(t) * a.Hq + h;
-    const int32_t splits = a.splits_of[unit];
-    if (splits < 2) continue;  // (its output is there)
-    const float* part = a.partials + unit * a.nsplit * D + d;
-    const float* pairs = a.partials + a.pairs_off + unit * a.nsplit * 2;
-    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < splits; ++k) m = fmaxf(m, pairs[2 * k]);
-    const float m_ref = m > -INFINITY ? m : 0.f;
-    for (int k = 0; k < splits; ++k) {
-      const float2 ml = *reinterpret_cast<const float2*>(pairs + 2 * k);
-      const float4 x = *reinterpret_cast<const float4*>(part + static_cast<int64_t>(k) * D);
-      if (ml.x == -INFINITY && ml.y == 0.f) continue;  // (saw nothing)
-      const float w = exp2_safe(ml.x - m_ref);
-      l += ml.y * w;
-      o[0] += x.x * w;
-      o[1] += x.y * w;
-      o[2] += x.z * w;
-      o[3] += x.w * w;
-    }
-    const bool any = has_weight<true>(l);
-    float f[4];
+  const int32_t splits = __builtin_amdgcn_readfirstlane(a.splits_of[t]);
+  if (splits < 2) return;  // (its output is there)
+  const int h0 = blockIdx.y * ROWS, h = min(h0 + r, a.Hq - 1);
+  const int64_t unit = static_cast<int64_t>(t) * a.Hq + h;
+  const float* part = a.partials + unit * a.nsplit * D + j * 4;
+  const float2* pairs = reinterpret_cast<const float2*>(a.partials + a.pairs_off + unit * a.nsplit * 2);
+  float m = -INFINITY;
+  for (int k = j; k < splits; k += LANES) m = fmaxf(m, pairs[k].x);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = any ? o[e] / l : 0.f;
-    char* out = a.out + t * a.out_t + h * a.out_h + d * sizeof(T);
-    if constexpr (std::is_same<T, float>::value)
-      *reinterpret_cast<uint4*>(out) = pack16(f);
-    else
-      *reinterpret_cast<uint2*>(out) = make_uint2(bf16x2(f[0], f[1]), bf16x2(f[2], f[3]));
-    if (a.lse && d == 0) a.lse[unit] = any ? m * kLn2 + logf(l) : -INFINITY;
+  for (int x = 1; x < LANES; x <<= 1) m = fmaxf(m, __shfl_xor(m, x, kWave));
+  const float m_ref = m > -INFINITY ? m : 0.f;
+  float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int k0 = 0; k0 < splits; k0 += LANES) {
+    const float2 ml = k0 + j < splits ? pairs[k0 + j] : make_float2(-INFINITY, 0.f);
+    const float w = exp2_safe(ml.x - m_ref);  // (0 where nothing was seen)
+    l += ml.y * w;
+    const int many = min(splits - k0, LANES);
+    constexpr int AHEAD = 8;
+    for (int k = 0; k < many; k += AHEAD) {
+      float4 x[AHEAD];
+#pragma unroll
+      for (int y = 0; y < AHEAD; ++y) x[y] = *reinterpret_cast<const float4*>(part + static_cast<int64_t>(k0 + min(k + y, many - 1)) * D);
+#pragma unroll
+      for (int y = 0; y < AHEAD; ++y) {
+        if (k + y >= many) break;
+        const float wy = __shfl(w, r * LANES + k + y, kWave);
+        o[0] += x[y].x * wy;
+        o[1] += x[y].y * wy;
+        o[2] += x[y].z * wy;
+        o[3] += x[y].w * wy;
+      }
+    }
   }
+#pragma unroll
+  for (int x = 1; x < LANES; x <<= 1) l += __shfl_xor(l, x, kWave);
+  if (h0 + r >= a.Hq) return;
+  const bool any = has_weight<true>(l);
+  float f[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f[e] = any ? o[e] / l : 0.f;
+  char* out = a.out + t * a.out_t + h * a.out_h + j * 4 * sizeof(T);
+  if constexpr (std::is_same<T, float>::value)
+    *reinterpret_cast<uint4*>(out) = pack16(f);
+  else
+    *reinterpret_cast<uint2*>(out) = make_uint2(bf16x2(f[0], f[1]), bf16x2(f[2], f[3]));
+  if (a.lse && j == 0) a.lse[unit] = any ? m * kLn2 + logf(l) : -INFINITY;
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------
@@ -971,6 +986,7 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
     tb_status rc = waves == 8 ? launch_one(chunk_kernel<T, D, 8>, grid, 8 * kWave, st, a) : launch_one(chunk_kernel<T, D, 4>, grid, 4 * kWave, st, a);
     if (rc != TB_OK) return rc;
     if (a.nsplit > 1) {
+      constexpr int kJoinHeads = 4 * kWave / D;
       const dim3 rows(static_cast<unsigned>((L.T + kJoinWaves - 1) / kJoinWaves), (d.Hq + kJoinHeads - 1) / kJoinHeads);
       rc = launch_one(join_kernel<T, D>, rows, kJoinWaves * kWave, st, a);
       if (rc != TB_OK) return rc;
@@ -993,9 +1009,9 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
 size_t paged_attn_ws_bytes(const tb_cache_desc* d, int64_t T) {
   const int64_t row = (d->D + 2) * static_cast<int64_t>(sizeof(float));
   const int64_t tokens = static_cast<int64_t>(d->B) * d->Hkv * kTokenRows * token_splits(*d);
-  // a call's rows times its splits, where there are several (of fewer tokens: more splits, but no more rows), and the number of each row's
-  const int64_t rows = std::min(kPartialRows, T * d->Hq), chunk = std::min(kPartialRows, T * d->Hq * std::max<int64_t>(1, d->N / (split_tiles(d->dtype == TB_F32) * chunk_keys(*d))));
-  return partials_at(*d) + static_cast<size_t>(std::max(tokens * row, chunk * row + rows * static_cast<int64_t>(sizeof(int32_t))));
+  // a call's rows times its splits, where there are several (of fewer tokens: more splits, but no more rows), and the number of each token's
+  const int64_t chunk = std::min(kPartialRows, T * d->Hq * std::max<int64_t>(1, d->N / (split_tiles(d->dtype == TB_F32) * chunk_keys(*d))));
+  return partials_at(*d) + static_cast<size_t>(std::max(tokens * row, chunk * row + std::min(kPartialRows, T) * static_cast<int64_t>(sizeof(int32_t))));
 }
 
 tb_status launch_paged_attn(const PagedAttnLaunch& L, hipStream_t st) {
