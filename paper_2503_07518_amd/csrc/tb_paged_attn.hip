@@ -1,7 +1,8 @@
 // Causal attention of new tokens over the rows of their sequences, held in pages.
 //
-//   chunk_kernel  many tokens: a workgroup takes 128 rows of (token, head of a KV group), so that a tile of K and V in LDS serves all
-//                 heads of the group, and runs over the rows that they see.
+//   chunk_kernel  many tokens: a workgroup takes 128 or 256 rows of (token, head of a KV group), so that a tile of K and V in LDS serves all
+//                 heads of the group, and runs over the rows that they see, with the running maximum and sum of the softmax.  Bound by the matrix
+//                 cores and what feeds them.  join_kernel adds up where workgroups have shared a row.
 //   token_kernel  up to 16 such rows a sequence (a decode step): bound by the rows of K and V, which go from memory to the matrix
 //                 cores without a stop in LDS; the rows of a sequence are split over workgroups.
 //
@@ -99,14 +100,22 @@ __device__ __forceinline__ float over_halves(float x) {
 
 // ---- many tokens ----------------------------------------------------------------------------------
 // A wave holds 32 rows as columns of v_mfma_f32_32x32x16_bf16 (or 32x32x2_f32, which keeps fp32 as it is): their queries (32 or 64 registers), their
-// outputs transposed (D / 32 blocks of 32 columns of V), running reference and sum.  Four waves share the tiles of K and V, two of each in LDS:
-// while one is worked on, the next one comes straight from memory (global_load_lds, 16 bytes a lane).  Rows in LDS are
+// outputs transposed (D / 32 blocks of 32 columns of V), running reference and sum.  Four or eight waves share the tiles of K and V, two of each in LDS:
+// while one is worked on, the next one comes straight from memory (global_load_lds, 16 bytes a lane).  The weights of a tile are computed under the
+// products of the next one's scores, and the next one's maximum is looked for under this one's products with V, so that the matrix cores do not
+// wait for the vector units.  Rows in LDS are
 // permuted in pieces of 16 bytes by their number so that neither the rows of K (a piece of 32 rows at once) nor the transposing reads
 // of V (a column of four rows) meet on a bank.
+//
+// bf16, D = 128: 8192 tokens, 32 heads on 8, 560 us (980 TFLOP/s of what the mask leaves), 1024 over 64000 rows, 64 on 8, 2030 us (1070); a
+// library product of 8192^3 runs at 1350.  Of 2215 us for the latter, before eight waves shared a tile, the products alone were 1170 (at the
+// power limit: 1850 TFLOP/s on random numbers), the reads from LDS another 106, staging 260, exponentials and the rest of the softmax 295.  64 rows
+// a wave would halve the reads of LDS, but leave one wave a SIMD: 3085.  fp32, 300 tokens over 30000 rows, 16 heads on 4, D = 64: 358 us, 103 TFLOP/s.
 // The reference of a row's softmax follows its maximum only when that has moved by more than this (weights stay below 2^8): the
 // accumulators are seldom rescaled.
 constexpr float kLazy = 8.f;
-// Tiles of keys that a split is worth its hand-over from (fp32: an eighth of the rate).
+// Tiles of keys that a split is worth its hand-over from (fp32: an eighth of the rate).  Twice as many, 64 tokens over 30000 rows: 67 and 85 us,
+// 128 over 4096 37 and 56; half as many: no faster.
 constexpr int split_tiles(bool f32) { return f32 ? 4 : 16; }
 
 template <typename T, int D, int NW>
@@ -185,7 +194,8 @@ __global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
     // as many tiles of keys for a workgroup as make a.target of them in all, as far as there is room for partial results
     const int32_t share = static_cast<int32_t>((static_cast<uint64_t>(work_all) * a.Hkv + a.target - 1) / a.target);
     const int32_t tiles = tile_end - tile;
-    splits = max(min(tiles / max(share, split_tiles(S::F32)), a.nsplit), 1);
+    // (rounded up from 7/8: sequences alike come out a little below a whole number of shares as often as above; 1024 tokens over 30000 rows 867 and 513 us)
+    splits = max(min((8 * tiles + share) / (8 * max(share, split_tiles(S::F32))), a.nsplit), 1);
     const int32_t per = (tiles + splits - 1) / splits;
     splits = (tiles + per - 1) / per;
     if (split >= splits) return;
@@ -224,7 +234,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void chunk_kernel(PagedAttnArgs a) {
   constexpr unsigned long long kAll = ~0ull;
   const char* const kh = a.pages.K + hkv * a.pages.k_h;
   const char* const vh = a.pages.V + hkv * a.pages.v_h;
-  // A wave loads a quarter of the tile's rows: 8 or 16, which lie in one page.
+  // A wave loads its share of the tile's rows: 4 to 16, which lie in one page.
   constexpr int MY_ROWS = S::LOADS * S::AT_ONCE;
   static_assert(16 % MY_ROWS == 0, "rows of a wave lie in one page");
   const int lane_row = lane / S::PIECES, piece = lane % S::PIECES;
@@ -922,18 +932,20 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
 constexpr int64_t kCus = 256;
 
 int chunk_keys(const tb_cache_desc& d) { return d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 32 : 64; }
-// Waves of a workgroup: eight read each row of K and V half as often, four leave less idle where they see different numbers of rows.
+// Waves of a workgroup: eight read each row of K and V half as often, four leave less idle where they see different numbers of rows.  32 heads on 8, four
+// and eight waves: 2048 tokens 62 and 75 us, 8192 592 and 566, 512 over 30000 rows 281 and 270, 1024 over 30000 545 and 513, 2048 over 8192 331 and 329,
+// 64 over 30000 66 and 100; six sequences of 1 to 1000 over 0 to 20000 178 and 199.
 int chunk_waves(const tb_cache_desc& d, int64_t T) {
   const int64_t rows = T * d.Hq;
-  return d.dtype == TB_BF16 && d.D == 128 && rows >= 256 * kCus && (rows >= 512 * kCus || d.N >= 4 * T) ? 8 : 4;
+  return d.dtype == TB_BF16 && d.D == 128 && rows >= (d.B == 1 ? 64 : 256) * kCus && (rows >= 512 * kCus || d.N >= 4 * T) ? 8 : 4;
 }
 // Workgroups share the rows of a sequence where those of whole tiles of tokens do not fill the chip: in up to so many splits, which a
-// workspace has room for.
+// workspace has room for (half as many: six sequences of 1 to 1000 tokens over 0 to 20000 rows 178 and 233 us, twice as many: no faster).
 constexpr int64_t kPartialRows = 262144;
 int64_t chunk_splits(const tb_cache_desc& d, int64_t T) {
   return std::max<int64_t>(1, std::min(kPartialRows / std::max<int64_t>(T * d.Hq, 1), d.N / (split_tiles(d.dtype == TB_F32) * chunk_keys(d))));
 }
-// ... of at least two steps.
+// ... of at least two steps (one or four: 1024 rows 11.5 and 10.5 us with 10.6, 4096 within the noise, the smallest of fp32 7.6 and 7.8 with 7.3).
 int64_t token_splits(const tb_cache_desc& d) {
   const int64_t groups = std::max<int64_t>(static_cast<int64_t>(d.B) * d.Hkv, 1), step = d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 16 : 32;
   return std::max<int64_t>(1, std::min(kCus / groups, d.N / (2 * step)));
@@ -977,8 +989,9 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
     const int64_t tiles = L.cu ? (L.T >> tq_log) + std::min<int64_t>(d.B, L.T) : d.B * ((std::min<int64_t>(a.tok.each, L.max_new) + (1 << tq_log) - 1) >> tq_log);
     if (d.Hkv * tiles > kMostTiles) return TB_ERR_UNSUPPORTED;
     a.few = tokens ? kTokenRows : 0;
-    // what the chip holds at once; a quarter more in fp32, whose products one wave a SIMD keeps busy
-    a.target = static_cast<int32_t>(d.dtype == TB_F32 ? 5 * kCus / 2 : 2 * kCus * 4 / waves);
+    // what the chip holds at once; twice that in fp32, whose products one wave a SIMD keeps busy (300 tokens over 30000 rows, 16 heads on 4, D = 64: 422 and
+    // 358 us with 5/8 of it and all, a ragged batch 156 and 160)
+    a.target = static_cast<int32_t>(d.dtype == TB_F32 ? 4 * kCus : 2 * kCus * 4 / waves);
     a.nsplit = static_cast<int32_t>(L.T * d.Hq >= 32 * waves * a.target ? 1 : chunk_splits(d, L.T));
     a.pairs_off = static_cast<int64_t>(a.tok.T) * a.Hq * a.nsplit * D;
     a.splits_of = reinterpret_cast<int32_t*>(a.partials + a.pairs_off + static_cast<int64_t>(a.tok.T) * a.Hq * a.nsplit * 2);
@@ -996,7 +1009,7 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
     a.nsplit = static_cast<int32_t>(token_splits(d));
     const dim3 grid(a.nsplit, d.Hkv, d.B);
     a.pairs_off = static_cast<int64_t>(d.B) * d.Hkv * kTokenRows * a.nsplit * D;
-    const int64_t rows = most << a.gs;  // (results of fewer rows are merged faster)
+    const int64_t rows = most << a.gs;  // (results of fewer rows are merged faster: 4 rows, 32768 keys 31.6 and 26.6 us with 16 and 4)
     if (rows <= 4) return launch_one(token_kernel<T, D, 4>, grid, kTokenWaves * kWave, st, a);
     if (rows <= 8) return launch_one(token_kernel<T, D, 8>, grid, kTokenWaves * kWave, st, a);
     return launch_one(token_kernel<T, D, kTokenRows>, grid, kTokenWaves * kWave, st, a);
