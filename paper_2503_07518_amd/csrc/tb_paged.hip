@@ -8,9 +8,10 @@ namespace tb {
 namespace {
 
 // ---- arrival of new rows --------------------------------------------------------------------------
-// A workgroup per token: the angles of its position once, into LDS, then all heads of q, k and v.  A unit of work is two
+// A workgroup per token, or a wave: the angles of its position once, into LDS, then all heads of q, k and v.  A unit of work is two
 // 128-bit pieces of a row whose elements are rotated with each other.  Bound by HBM for many tokens, by the trips to memory (offsets, table,
-// row) for few; a unit's elements are on their way while the angles are computed.
+// row) for few; a unit's elements are on their way while the angles are computed.  32 heads on 8, D = 128, bf16: 8192 tokens 45 us, 218 MB at
+// the 4.8 TB/s of a plain copy; 16 tokens 4.4 us.
 //
 // Angles: position times frequency is a product of at most 31 and 24 bits, exact in 64 to 2^-53; in turns, its fraction is taken in
 // 64 bits and is then a number of fp32, so that a far position rotates as exactly as a near one.
@@ -28,13 +29,18 @@ struct AppendArgs {
 constexpr int kAppendThreads = 256;
 constexpr int kAppendUnits = 2;  // of a thread at a time
 
-template <typename T, int D, bool PAIRS>
+// WAVES: of a token, one or all.
+template <typename T, int D, bool PAIRS, int WAVES>
 __global__ __launch_bounds__(kAppendThreads) void append_paged_kernel(AppendArgs a) {
   constexpr int EPL = Pack16<T>::kElts;
   constexpr int UNITS = D / (2 * EPL);  // of a row
-  __shared__ __attribute__((aligned(16))) float s_cos[D / 2], s_sin[D / 2];
-  const int tid = threadIdx.x;
-  const int32_t t = blockIdx.x;
+  constexpr int THREADS = WAVES * kWave, TOKENS = kAppendThreads / THREADS;
+  __shared__ __attribute__((aligned(16))) float s_cos_of[TOKENS][D / 2], s_sin_of[TOKENS][D / 2];
+  const int tid = threadIdx.x % THREADS, mine = TOKENS > 1 ? wave_id() : 0;
+  float* const s_cos = s_cos_of[mine];
+  float* const s_sin = s_sin_of[mine];
+  const int32_t t = blockIdx.x * TOKENS + mine;
+  if (t >= a.tok.T) return;
   const int32_t b = sequence_of(a.tok, t);
   if (b >= a.tok.B) return;
   const Sequence s = sequence(a.tok, b);
@@ -48,12 +54,12 @@ __global__ __launch_bounds__(kAppendThreads) void append_paged_kernel(AppendArgs
   const int turned = a.rot / (2 * EPL);  // units of a row that are rotated
   const int units = (a.Hq + 2 * a.Hkv) * UNITS;
 
-  for (int u0 = 0; u0 < units; u0 += kAppendUnits * kAppendThreads) {
+  for (int u0 = 0; u0 < units; u0 += kAppendUnits * THREADS) {
     typename Pack16<T>::Raw x[kAppendUnits], y[kAppendUnits];
     int which[kAppendUnits], head[kAppendUnits], part[kAppendUnits], at[kAppendUnits], to[kAppendUnits];
 #pragma unroll
     for (int k = 0; k < kAppendUnits; ++k) {
-      const int u = u0 + k * kAppendThreads + tid;
+      const int u = u0 + k * THREADS + tid;
       const int h = u / UNITS;
       part[k] = u % UNITS;
       which[k] = u >= units ? 3 : (h < a.Hq ? 0 : (h < a.Hq + a.Hkv ? 1 : 2));
@@ -78,7 +84,12 @@ __global__ __launch_bounds__(kAppendThreads) void append_paged_kernel(AppendArgs
         s_cos[tid] = cs;
         s_sin[tid] = sn;
       }
-      __syncthreads();
+      if constexpr (TOKENS > 1) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (a token's wave has its angles to itself)
+        __builtin_amdgcn_wave_barrier();
+      } else {
+        __syncthreads();
+      }
     }
 #pragma unroll
     for (int k = 0; k < kAppendUnits; ++k) {
@@ -129,6 +140,18 @@ __global__ __launch_bounds__(kAppendThreads) void append_paged_kernel(AppendArgs
   }
 }
 
+// Tokens of few heads, which a wave holds in its registers at once, have a wave each (bf16, D = 128, 16384 tokens, 8 heads on 2: 36 us with a
+// workgroup, 25 with a wave; 27922 ragged ones, 4 on 1: 46 and 23).
+template <typename T, int D, bool PAIRS>
+tb_status launch_append_waves(AppendArgs& a, hipStream_t st) {
+  constexpr int units_of_row = D * static_cast<int>(sizeof(T)) / 32;
+  const int64_t units = (a.Hq + 2 * static_cast<int64_t>(a.Hkv)) * units_of_row;
+  const unsigned tokens = static_cast<unsigned>(a.tok.T);
+  constexpr unsigned kTokens = kAppendThreads / kWave;
+  if (units <= kAppendUnits * kWave) return launch_one(append_paged_kernel<T, D, PAIRS, 1>, dim3((tokens + kTokens - 1) / kTokens), kAppendThreads, st, a);
+  return launch_one(append_paged_kernel<T, D, PAIRS, 4>, dim3(tokens), kAppendThreads, st, a);
+}
+
 template <typename T, int D>
 tb_status launch_append_td(const AppendPagedLaunch& L, hipStream_t st) {
   constexpr int64_t elt = sizeof(T);
@@ -152,15 +175,14 @@ tb_status launch_append_td(const AppendPagedLaunch& L, hipStream_t st) {
   a.rot = L.rot;
   a.Hq = L.q ? L.desc->Hq : 0;
   a.Hkv = L.desc->Hkv;
-  const dim3 grid(static_cast<unsigned>(L.T));
-  return L.interleaved ? launch_one(append_paged_kernel<T, D, true>, grid, kAppendThreads, st, a)
-                       : launch_one(append_paged_kernel<T, D, false>, grid, kAppendThreads, st, a);
+  return L.interleaved ? launch_append_waves<T, D, true>(a, st) : launch_append_waves<T, D, false>(a, st);
 }
 
 // ---- attention over lists of rows -----------------------------------------------------------------
 // The split attention over rows of a contiguous cache, with a trip through the page table on the way to a row: a lane looks up
 // the page of its slot's row a tile ahead of the gathers, and the slot's entry a tile ahead of that.  A row's place is a 32-bit offset in
-// units of 16 bytes.
+// units of 16 bytes.  Each gathered row is used once, by the lane group that fetched it.  32 heads on 8, D = 128, bf16: 3277 of 32768 rows 12.6 us (the
+// trips: list, table, row, then the hand-over of splits), a batch of 16 with 2048 of 16384 74.5 us, 449 MB of distinct rows at 6.0 TB/s.
 struct SparseArgs {
   const void* q;
   Pages pages;
