@@ -37,7 +37,8 @@ struct PagedAttnArgs {
   int32_t Hq, Hkv, gs;  // 1 << gs query heads a KV head
   int32_t max_new, window;
   int32_t nsplit;      // at most
-  int32_t target;      // chunk_kernel: workgroups that share the keys
+  int32_t target;      // workgroups that share the keys (token_kernel: of a KV head)
+  int32_t each;        // token_kernel: splits of every sequence, at most; 0: by their lengths
   int32_t* splits_of;  // ... and how many a token's rows have got
   int32_t few;  // chunk_kernel: sequences with up to so many rows are the token_kernel's
   float* partials;
@@ -599,8 +600,8 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void join_kernel(PagedAttnArgs 
 // 16 rows (token, head of the group) as columns of v_mfma_f32_16x16x32_bf16 (16x16x4_f32).  Lane (i, kb) = (lane % 16, lane / 16) loads pieces
 // kb, kb + 4, .. of row i of 16 rows of K, and of the rows 4 kb + v of V the elements EV i .. + EV - 1; accumulator v of the scores
 // is then key 4 kb + v of column i, and element e of V's pieces the column EV i + e of the output, whose accumulator v is that of row 4 kb + v.
-// A wave has two steps' rows in flight.  Splits of a sequence fill the chip once (kCus / groups of them).  32 heads on 8, D = 128, bf16: 32768 rows 26.3 us, 134 MB
-// at 5.1 TB/s, of which 19 are the bytes at a read stream's 7.0; 16 sequences of 9002 to 16384 152 us, 947 MB at 6.2.  Workgroups that share a sequence hand over by tb_attn_merge.h's protocol.
+// A wave has two steps' rows in flight.  Splits of all sequences fill the chip once.  32 heads on 8, D = 128, bf16: 32768 rows 26.5 us, 134 MB
+// at 5.1 TB/s, of which 19 are the bytes at a read stream's 7.0; 16 sequences of 9002 to 16384 154 us, 947 MB at 6.1.  Workgroups that share a sequence hand over by tb_attn_merge.h's protocol.
 constexpr int kTokenWaves = 8;
 // Every row is read once: not kept for anybody (32 heads on 8, D = 128, bf16, plain loads and these: 32768 rows 30.0 and 26.6 us, 16 sequences of
 // 9002 to 16384 163 and 152, one of 16384, whose rows the last-level cache still held, 18.5 and 18.4).
@@ -627,16 +628,59 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
   __shared__ float s_out[GH * D], s_lse[GH];
   const int tid = threadIdx.x, lane = lane_id(), wave = wave_id();
   const int i16 = lane & 15, kb = lane >> 4;
-  const int split = blockIdx.x, hkv = blockIdx.y, b = blockIdx.z;
-  const Sequence s = sequence(a.tok, b);
+  const int hkv = blockIdx.y;
+
+  // Steps that a sequence's tokens see (0 of those that are not this kernel's), and of whose this workgroup takes a split: splits are of the same
+  // number of steps, give or take, so that sequences of different lengths are done together.
+  auto steps_of = [&](const Sequence& x) -> int32_t {
+    const int32_t of = min(x.n, a.max_new);
+    if (of <= 0 || of > GH >> a.gs) return 0;
+    const int32_t p0 = max(x.row, 0), p1 = min(x.row + of - 1, a.tok.N - 1);
+    if (p0 > p1) return 0;
+    return p1 / S::STEP + 1 - (a.window ? max(p0 - a.window + 1, 0) / S::STEP : 0);
+  };
+  Sequence s;
+  int32_t b, split, steps, splits;
+  if (a.each > 0) {
+    b = a.tok.B > 1 ? blockIdx.x / a.each : 0;
+    split = blockIdx.x - b * a.each;
+    s = sequence(a.tok, b);
+    steps = steps_of(s);
+    splits = min(a.each, (steps + 1) / 2);
+  } else {
+    const Sequence x = sequence(a.tok, min(lane, a.tok.B - 1));
+    const uint32_t x_steps = lane < a.tok.B ? steps_of(x) : 0;
+    auto sum = [](uint32_t y) -> uint32_t { return __builtin_amdgcn_readlane(wave_incl_scan_u32(y), kWave - 1); };
+    const float all = 65536.f * sum(x_steps >> 16) + sum(x_steps & 0xFFFFu);
+    // the fewest steps a split, from those of a.target equal ones to half as much again, with which there are no more than a.target (or one a sequence); failing that, a
+    // split a sequence more at most.  (x / y rounded up, from the reciprocal of y: less than x / y + 1 also where that is rounded.)
+    const float share = fmaxf(all / a.target, 2.f);
+    const uint32_t goal = max(static_cast<uint32_t>(a.target), static_cast<uint32_t>(popc64(ballot64(x_steps > 0))));
+    uint32_t mine = 0, upto = 0;
+    for (int k = 16; k <= 25; ++k) {
+      const float inv = (1.f - 0x1p-20f) / (share * (k < 25 ? k / 16.f : 1.f));
+      mine = x_steps ? static_cast<uint32_t>(x_steps * inv) + 1 : 0;
+      upto = wave_incl_scan_u32(mine);
+      if (__builtin_amdgcn_readlane(upto, kWave - 1) <= goal) break;
+    }
+    b = static_cast<int32_t>(popc64(ballot64(upto <= blockIdx.x)));
+    if (b >= a.tok.B) return;
+    b = __builtin_amdgcn_readfirstlane(b);
+    split = static_cast<int32_t>(blockIdx.x - __builtin_amdgcn_readlane(upto - mine, b));
+    s.first = __builtin_amdgcn_readlane(x.first, b);
+    s.n = __builtin_amdgcn_readlane(x.n, b);
+    s.row = __builtin_amdgcn_readlane(x.row, b);
+    steps = __builtin_amdgcn_readlane(x_steps, b);
+    splits = __builtin_amdgcn_readlane(mine, b);
+  }
+  if (split >= splits) return;
   const int32_t n = min(s.n, a.max_new);
-  if (n <= 0 || n > GH >> a.gs) return;
   const int32_t p_first = max(s.row, 0), p_last = min(s.row + n - 1, a.tok.N - 1);
-  if (p_first > p_last) return;
   const int32_t see_first = a.window ? max(p_first - a.window + 1, 0) : 0;
+  const int32_t step_0 = see_first / S::STEP;
   // whole steps for a workgroup: the splits that get any
-  const int32_t step_0 = see_first / S::STEP, steps = p_last / S::STEP + 1 - step_0;
-  const int32_t per = (steps + a.nsplit - 1) / a.nsplit, splits = (steps + per - 1) / per;
+  const int32_t per = (steps + splits - 1) / splits;
+  splits = (steps + per - 1) / per;
   if (split >= splits) return;
   const int32_t step_end = step_0 + min((split + 1) * per, steps);
 
@@ -886,8 +930,9 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
     store_elt(reinterpret_cast<T*>(a.out + t * a.out_t + h * a.out_h) + d, any ? v : 0.f);
     if (a.lse && d == 0) a.lse[t * a.Hq + h] = any ? lse : -INFINITY;
   };
-  float* const po = a.partials + group * GH * a.nsplit * D;  // [row][split][D]
-  float* const pp = a.partials + a.pairs_off + group * GH * a.nsplit * 2;
+  const int64_t slot = static_cast<int64_t>(hkv) * gridDim.x + blockIdx.x - split;  // of its first split
+  float* const po = a.partials + slot * GH * D;  // [row][split][D]
+  float* const pp = a.partials + a.pairs_off + slot * GH * 2;
 #pragma unroll
   for (int x = 0; x < OUTS; ++x) {
     const int e = tid + x * kThreads, row = e / D, d = e % D;
@@ -946,11 +991,16 @@ constexpr int64_t kPartialRows = 262144;
 int64_t chunk_splits(const tb_cache_desc& d, int64_t T) {
   return std::max<int64_t>(1, std::min(kPartialRows / std::max<int64_t>(T * d.Hq, 1), d.N / (split_tiles(d.dtype == TB_F32) * chunk_keys(d))));
 }
-// ... of at least two steps (one or four: 1024 rows 11.5 and 10.5 us with 10.6, 4096 within the noise, the smallest of fp32 7.6 and 7.8 with 7.3).
-int64_t token_splits(const tb_cache_desc& d) {
-  const int64_t groups = std::max<int64_t>(static_cast<int64_t>(d.B) * d.Hkv, 1), step = d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 16 : 32;
-  return std::max<int64_t>(1, std::min(kCus / groups, d.N / (2 * step)));
+// Single tokens: workgroups that share a KV head's rows of all sequences, as many as the chip holds, with two steps each or more.
+int64_t token_target(const tb_cache_desc& d) {
+  const int64_t step = d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 16 : 32;
+  return std::max<int64_t>(1, std::min(kCus / std::max(d.Hkv, 1), d.B * std::max<int64_t>(1, d.N / (2 * step))));
 }
+// Of up to 64 sequences, which a wave looks at in one instruction, each gets splits by its length; of more, all the same.  32 heads on 8, as many for all
+// and by length: 8542, 1, 3214 and 76203 rows 145 and 64 us, 39 of 2000 and one of 60000 829 and 120; 16 of 9002 to 16384 153 and 153, one of 24444 and a short
+// one, 64 heads on 8, D = 64, whose hand-over has more to read, 19.4 and 21.8.
+int64_t token_each(const tb_cache_desc& d) { return d.B > 1 && d.B <= kWave ? 0 : std::max<int64_t>(1, token_target(d) / std::max(d.B, 1)); }
+int64_t token_slots(const tb_cache_desc& d) { return token_each(d) > 0 ? token_each(d) * d.B : token_target(d) + d.B; }
 // Partial results lie behind the counters of B * Hq units, as in the workspaces of the other operations, so that one may serve several.
 size_t partials_at(const tb_cache_desc& d) { return ws_layout(static_cast<int64_t>(d.B) * d.Hq, d.D, 1).part_off; }
 // (of a launch's threads, which are numbered with 32 bits)
@@ -1007,9 +1057,10 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
     }
   }
   if (tokens) {
-    a.nsplit = static_cast<int32_t>(token_splits(d));
-    const dim3 grid(a.nsplit, d.Hkv, d.B);
-    a.pairs_off = static_cast<int64_t>(d.B) * d.Hkv * kTokenRows * a.nsplit * D;
+    a.target = static_cast<int32_t>(token_target(d));
+    a.each = static_cast<int32_t>(token_each(d));
+    const dim3 grid(static_cast<unsigned>(token_slots(d)), d.Hkv);
+    a.pairs_off = token_slots(d) * d.Hkv * kTokenRows * D;
     const int64_t rows = most << a.gs;  // (results of fewer rows are merged faster: 4 rows, 32768 keys 31.6 and 26.6 us with 16 and 4)
     if (rows <= 4) return launch_one(token_kernel<T, D, 4>, grid, kTokenWaves * kWave, st, a);
     if (rows <= 8) return launch_one(token_kernel<T, D, 8>, grid, kTokenWaves * kWave, st, a);
@@ -1022,7 +1073,7 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
 
 size_t paged_attn_ws_bytes(const tb_cache_desc* d, int64_t T) {
   const int64_t row = (d->D + 2) * static_cast<int64_t>(sizeof(float));
-  const int64_t tokens = static_cast<int64_t>(d->B) * d->Hkv * kTokenRows * token_splits(*d);
+  const int64_t tokens = token_slots(*d) * d->Hkv * kTokenRows;
   // a call's rows times its splits, where there are several (of fewer tokens: more splits, but no more rows), and the number of each token's
   const int64_t chunk = std::min(kPartialRows, T * d->Hq * std::max<int64_t>(1, d->N / (split_tiles(d->dtype == TB_F32) * chunk_keys(*d))));
   return partials_at(*d) + static_cast<size_t>(std::max(tokens * row, chunk * row + std::min(kPartialRows, T) * static_cast<int64_t>(sizeof(int32_t))));

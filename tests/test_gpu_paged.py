@@ -168,6 +168,15 @@ def test_pages(page):
     check_attn(make(BF, 4, 2, 128, page, [70, 1, 5], [100, 1025, 15]))
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,D", [(BF, 4, 1, 64), (BF, 16, 8, 128), (F32, 8, 2, 128)])
+@pytest.mark.parametrize("kept,window", [([3000, 0, 17, 900], 0), ([500] * 16, 0), ([500, 460, 520, 300, 530, 480] * 2, 0), ([5000] + [0] * 40, 0), ([1500, 2500, 3, 0, 700], 1100),
+                                         ([380, 5, 0, 77, 200] * 14, 0), ([0, 1200] + [3] * 62, 0)])
+def test_decode_steps_of_ragged_batches(dtype, Hq, Hkv, D, kept, window):
+    """Splits by the sequences' lengths (up to 64 of them; as many for all where there are more), sequences without new tokens among them."""
+    new = [0 if i % 11 == 5 else 1 + (i % 7 == 3) for i in range(len(kept))]
+    check_attn(make(dtype, Hq, Hkv, D, 16, new, kept, seed=len(kept)), window=window)
+
+
 @pytest.mark.parametrize("n", [1, 2, 4, 5, 16, 17, 31])
 def test_numbers_of_tokens(n):
     check_attn(make(BF, 4, 1, 64, 16, [n, n], [40, 0]))
