@@ -36,7 +36,7 @@ struct PagedAttnArgs {
   uint32_t q_and, q_xor;
   int32_t Hq, Hkv, gs;  // 1 << gs query heads a KV head
   int32_t max_new, window;
-  int32_t nsplit;      // at most
+  int32_t nsplit;      // of a row, at most
   int32_t target;      // workgroups that share the keys (token_kernel: of a KV head)
   int32_t each;        // token_kernel: splits of every sequence, at most; 0: by their lengths
   int32_t* splits_of;  // ... and how many a token's rows have got
@@ -659,7 +659,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
     uint32_t mine = 0, upto = 0;
     for (int k = 16; k <= 25; ++k) {
       const float inv = (1.f - 0x1p-20f) / (share * (k < 25 ? k / 16.f : 1.f));
-      mine = x_steps ? static_cast<uint32_t>(x_steps * inv) + 1 : 0;
+      mine = x_steps ? min(static_cast<uint32_t>(x_steps * inv) + 1, static_cast<uint32_t>(a.nsplit)) : 0;
       upto = wave_incl_scan_u32(mine);
       if (__builtin_amdgcn_readlane(upto, kWave - 1) <= goal) break;
     }
@@ -991,15 +991,19 @@ constexpr int64_t kPartialRows = 262144;
 int64_t chunk_splits(const tb_cache_desc& d, int64_t T) {
   return std::max<int64_t>(1, std::min(kPartialRows / std::max<int64_t>(T * d.Hq, 1), d.N / (split_tiles(d.dtype == TB_F32) * chunk_keys(d))));
 }
-// Single tokens: workgroups that share a KV head's rows of all sequences, as many as the chip holds, with two steps each or more.
+// Single tokens: workgroups that share a KV head's rows of all sequences, as many as the chip holds (two a compute unit where registers allow it: bf16,
+// D = 64, 8 sequences of 32000 rows 140 and 90 us with one and two), with two steps each or more.
 int64_t token_target(const tb_cache_desc& d) {
-  const int64_t step = d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 16 : 32;
-  return std::max<int64_t>(1, std::min(kCus / std::max(d.Hkv, 1), d.B * std::max<int64_t>(1, d.N / (2 * step))));
+  const int64_t step = d.D * (d.dtype == TB_F32 ? 4 : 2) >= 512 ? 16 : 32, chip = d.dtype == TB_BF16 && d.D == 64 ? 2 * kCus : kCus;
+  return std::max<int64_t>(1, std::min(chip / std::max(d.Hkv, 1), d.B * std::max<int64_t>(1, d.N / (2 * step))));
 }
+// One sequence's splits: more cost more in the hand-over than they save.  (bf16: 90000 rows of one KV head for 8 heads 31.6 and 25.9 us with 256 and 128, fp32
+// for 4 heads 32 and 40; 32000 rows of eight, D = 64, 20.0 and 17.4 with 64 and 32.)
+int64_t token_most(const tb_cache_desc& d) { return std::max<int64_t>(1, std::min<int64_t>(kCus / std::max(d.Hkv, 1), d.dtype == TB_F32 ? 256 : 128)); }
 // Of up to 64 sequences, which a wave looks at in one instruction, each gets splits by its length; of more, all the same.  32 heads on 8, as many for all
 // and by length: 8542, 1, 3214 and 76203 rows 145 and 64 us, 39 of 2000 and one of 60000 829 and 120; 16 of 9002 to 16384 153 and 153, one of 24444 and a short
-// one, 64 heads on 8, D = 64, whose hand-over has more to read, 19.4 and 21.8.
-int64_t token_each(const tb_cache_desc& d) { return d.B > 1 && d.B <= kWave ? 0 : std::max<int64_t>(1, token_target(d) / std::max(d.B, 1)); }
+// one, 64 heads on 8, D = 64, whose hand-over has more to read, 19.4 and 21.5.
+int64_t token_each(const tb_cache_desc& d) { return d.B > 1 && d.B <= kWave ? 0 : std::max<int64_t>(1, std::min(token_target(d) / std::max(d.B, 1), token_most(d))); }
 int64_t token_slots(const tb_cache_desc& d) { return token_each(d) > 0 ? token_each(d) * d.B : token_target(d) + d.B; }
 // Partial results lie behind the counters of B * Hq units, as in the workspaces of the other operations, so that one may serve several.
 size_t partials_at(const tb_cache_desc& d) { return ws_layout(static_cast<int64_t>(d.B) * d.Hq, d.D, 1).part_off; }
@@ -1047,7 +1051,8 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
     a.pairs_off = static_cast<int64_t>(a.tok.T) * a.Hq * a.nsplit * D;
     a.splits_of = reinterpret_cast<int32_t*>(a.partials + a.pairs_off + static_cast<int64_t>(a.tok.T) * a.Hq * a.nsplit * 2);
     const dim3 grid(static_cast<unsigned>(d.Hkv * tiles), a.nsplit);
-    tb_status rc = waves == 8 ? launch_one(chunk_kernel<T, D, 8>, grid, 8 * kWave, st, a) : launch_one(chunk_kernel<T, D, 4>, grid, 4 * kWave, st, a);
+    constexpr int kMostWaves = std::is_same<T, float>::value || D != 128 ? 4 : 8;  // (as chunk_waves says)
+    tb_status rc = waves == kMostWaves ? launch_one(chunk_kernel<T, D, kMostWaves>, grid, kMostWaves * kWave, st, a) : launch_one(chunk_kernel<T, D, 4>, grid, 4 * kWave, st, a);
     if (rc != TB_OK) return rc;
     if (a.nsplit > 1) {
       constexpr int kJoinHeads = 4 * kWave / D;
@@ -1059,6 +1064,7 @@ tb_status launch_td(const PagedAttnLaunch& L, hipStream_t st) {
   if (tokens) {
     a.target = static_cast<int32_t>(token_target(d));
     a.each = static_cast<int32_t>(token_each(d));
+    a.nsplit = static_cast<int32_t>(token_most(d));
     const dim3 grid(static_cast<unsigned>(token_slots(d)), d.Hkv);
     a.pairs_off = token_slots(d) * d.Hkv * kTokenRows * D;
     const int64_t rows = most << a.gs;  // (results of fewer rows are merged faster: 4 rows, 32768 keys 31.6 and 26.6 us with 16 and 4)
