@@ -321,7 +321,8 @@ typedef struct tb_token_rows {
 /* New tokens of the sequences reach the cache, their queries and keys rotated by their positions on the way.
  * The T tokens of a call are those of sequence 0, then of sequence 1, ...: sequence b has the tokens cu[b] .. cu[b+1]-1 (cu: int32 [B+1],
  * cu[0] = 0; NULL: T / B tokens each), which are the last of its lens[b] rows (int32 [B], on the device as cu is): token number i of n
- * is row lens[b] - n + i.  T <= 2^22 (else TB_ERR_UNSUPPORTED).  Tokens whose row is not in [0, N), and those from cu[B] on, take no part: nothing of theirs is read or written.
+ * is row lens[b] - n + i.  T <= 2^22 (else TB_ERR_UNSUPPORTED).  Tokens whose row is not in [0, N), and those from cu[B] on, take no part:
+ * nothing of theirs is read or written.
  *   angle(t, i) = positions[t] * inv_freq[i]   0 <= i < rot / 2; positions: int32 [T], NULL: the token's row; inv_freq: fp32 [rot / 2]
  *   (x[j], x[k]) -> (x[j] cos - x[k] sin, x[k] cos + x[j] sin)   of q and k, (j, k) = (i, i + rot / 2), or (2i, 2i + 1) if interleaved
  * with one rounding at the end, angles in 64 bits; elements from rot on stay as they are.  rot: 0 (no rotation) to D, a multiple of 16.
