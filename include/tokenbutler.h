@@ -338,8 +338,9 @@ tb_status tb_append_paged_kv(const tb_cache_desc* desc, const tb_paged_cache* ca
  * where p is the token's row; T, cu and lens as above.  One token of every sequence is a dense decode step, many are a prompt or a chunk of
  * one; a call may hold both.  max_new: host-side bound on a sequence's new tokens (tokens past it are left out, as are those past cu[B]:
  * their outputs are not written).
- * out has the element type of q (one rounding; weights are rounded to that type, too, before they meet V); lse: fp32 [T][Hq] or NULL.  A
- * token that attends to nothing, or with scores of minus infinity alone, has out = 0 and lse = -inf.  Rows that a token does not attend to
+ * out has the element type of q (one rounding).  Weights are rounded to that type, too, before they meet V, except in calls of few tokens
+ * (max_new, or T / B without cu, times Hq / Hkv up to 8), which lose at most 2^-16 of each.  lse: fp32 [T][Hq] or NULL.
+ * A token that attends to nothing, or with scores of minus infinity alone, has out = 0 and lse = -inf.  Rows that a token does not attend to
  * add nothing to its result, whatever they hold.
  * ws: tb_workspace_bytes(TB_OP_PAGED_ATTN, desc, T); calls that share it have the same Hkv, too. */
 tb_status tb_paged_attn(const tb_cache_desc* desc, const tb_paged_cache* cache, int64_t T, const int32_t* cu, const int32_t* lens,

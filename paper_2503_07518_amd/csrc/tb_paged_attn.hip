@@ -111,7 +111,9 @@ __device__ __forceinline__ float over_halves(float x) {
 // bf16, D = 128: 8192 tokens, 32 heads on 8, 560 us (980 TFLOP/s of what the mask leaves), 1024 over 64000 rows, 64 on 8, 2030 us (1070); a
 // library product of 8192^3 runs at 1350.  Of 2215 us for the latter, before eight waves shared a tile, the products alone were 1170 (at the
 // power limit: 1850 TFLOP/s on random numbers), the reads from LDS another 106, staging 260, exponentials and the rest of the softmax 295.  64 rows
-// a wave would halve the reads of LDS, but leave one wave a SIMD: 3085.  fp32, 300 tokens over 30000 rows, 16 heads on 4, D = 64: 358 us, 103 TFLOP/s.
+// a wave would halve the reads of LDS, but leave one wave a SIMD: 3085.  Weights are rounded to bf16, the type of the products (outputs are off 64 bits
+// by 0.0022 of their norm, 0.0016 of it by the rounding of the output): what that loses, as a second part of the weights, would be half as many
+// products again, of a kernel that is bound by them.  fp32, 300 tokens over 30000 rows, 16 heads on 4, D = 64: 358 us, 103 TFLOP/s.
 // The reference of a row's softmax follows its maximum only when that has moved by more than this (weights stay below 2^8): the
 // accumulators are seldom rescaled.
 constexpr float kLazy = 8.f;
@@ -602,6 +604,11 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void join_kernel(PagedAttnArgs 
 // is then key 4 kb + v of column i, and element e of V's pieces the column EV i + e of the output, whose accumulator v is that of row 4 kb + v.
 // A wave has two steps' rows in flight.  Splits of all sequences fill the chip once.  32 heads on 8, D = 128, bf16: 32768 rows 26.5 us, 134 MB
 // at 5.1 TB/s, of which 19 are the bytes at a read stream's 7.0; 16 sequences of 9002 to 16384 154 us, 947 MB at 6.1.  Workgroups that share a sequence hand over by tb_attn_merge.h's protocol.
+//
+// Weights of bf16 calls: up to eight rows leave half of the columns free, which hold the same rows once more and take what the weights of the first half
+// lose when they are rounded to bf16, rounded itself: a weight is then off by 2^-16 of it at most, without a product more (32768 rows: outputs off
+// 64 bits by 0.0017 of their norm, which is what bf16 holds, instead of 0.0022; 27.0 us instead of 26.8, the batch of 16 154.4 instead of 154.0).  Nine to
+// sixteen rows fill the columns: rounded to bf16, as the chunk_kernel's are.
 constexpr int kTokenWaves = 8;
 // Every row is read once: not kept for anybody (32 heads on 8, D = 128, bf16, plain loads and these: 32768 rows 30.0 and 26.6 us, 16 sequences of
 // 9002 to 16384 163 and 152, one of 16384, whose rows the last-level cache still held, 18.5 and 18.4).
@@ -619,12 +626,16 @@ struct TokenShape {
   static constexpr int VB = EV * sizeof(T);          // ... bytes: 8, 16 or 32
   static constexpr int VP = (VB + 15) / 16;          // ... in pieces of up to 16
   static_assert(F32 || GROUPS == 2, "32 keys fill a product");
+  // columns 8 to 15 hold rows 0 to 7 once more, for the rest of their weights
+  static constexpr bool rests(int rows) { return !F32 && rows <= 8; }
 };
 
 template <typename T, int D, int GH>
 __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttnArgs a) {
   using S = TokenShape<T, D>;
+  constexpr bool RESTS = S::rests(GH);
   __shared__ GroupLds<D, GH, kTokenWaves> gl;
+  __shared__ __attribute__((aligned(16))) float s_rest[RESTS ? kTokenWaves : 1][RESTS ? GH : 1][D];  // as gl.acc
   __shared__ float s_out[GH * D], s_lse[GH];
   const int tid = threadIdx.x, lane = lane_id(), wave = wave_id();
   const int i16 = lane & 15, kb = lane >> 4;
@@ -661,7 +672,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
       const float inv = (1.f - 0x1p-20f) / (share * (k < 25 ? k / 16.f : 1.f));
       mine = x_steps ? min(static_cast<uint32_t>(x_steps * inv) + 1, static_cast<uint32_t>(a.nsplit)) : 0;
       upto = wave_incl_scan_u32(mine);
-      if (__builtin_amdgcn_readlane(upto, kWave - 1) <= goal) break;
+      if (static_cast<uint32_t>(__builtin_amdgcn_readlane(upto, kWave - 1)) <= goal) break;
     }
     b = static_cast<int32_t>(popc64(ballot64(upto <= blockIdx.x)));
     if (b >= a.tok.B) return;
@@ -684,11 +695,13 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
   if (split >= splits) return;
   const int32_t step_end = step_0 + min((split + 1) * per, steps);
 
-  const int32_t my_i = i16 >> a.gs, my_p = s.row + my_i;
+  constexpr int COLS = RESTS ? 8 : 16;  // that hold different rows
+  const int my_row = i16 & (COLS - 1);
+  const int32_t my_i = my_row >> a.gs, my_p = s.row + my_i;
   const int32_t my_low = a.window ? my_p - a.window : -1;  // it sees the rows behind this one, up to its own
   const bool mine = my_i < n && my_p >= 0 && my_p < a.tok.N;
   u32x4 q[S::KP];
-  const char* qp = a.q + (s.first + (mine ? my_i : 0)) * a.q_t + ((hkv << a.gs) + (i16 & ((1 << a.gs) - 1))) * a.q_h + kb * 16;
+  const char* qp = a.q + (s.first + (mine ? my_i : 0)) * a.q_t + ((hkv << a.gs) + (my_row & ((1 << a.gs) - 1))) * a.q_h + kb * 16;
 #pragma unroll
   for (int c = 0; c < S::KP; ++c) {
     q[c] = u32x4{0u, 0u, 0u, 0u};
@@ -804,7 +817,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
                   const float v = not_finite_or_zero(__uint_as_float(S::F32 ? word : (y ? word & 0xFFFF0000u : word << 16)));
 #pragma unroll
                   for (int j = 0; j < 4; ++j) {
-                    const int32_t p_j = s.row + ((4 * kb + j) >> a.gs);
+                    const int32_t p_j = s.row + (((4 * kb + j) & (COLS - 1)) >> a.gs);
                     o[w * (S::EV * 4 / S::VB) + y][j] += ((key <= p_j) & (key > (a.window ? p_j - a.window : -1))) ? v : 0.f;
                   }
                 }
@@ -855,7 +868,14 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
     } else {
       u32x4 w;
 #pragma unroll
-      for (int y = 0; y < 4; ++y) w[y] = bf16x2(p[y / 2][2 * (y & 1)], p[y / 2][2 * (y & 1) + 1]);
+      for (int y = 0; y < 4; ++y) {
+        const float w0 = p[y / 2][2 * (y & 1)], w1 = p[y / 2][2 * (y & 1) + 1];
+        w[y] = bf16x2(w0, w1);
+        if constexpr (RESTS) {
+          const uint32_t rest = bf16x2(w0 - __uint_as_float(w[y] << 16), w1 - __uint_as_float(w[y] & 0xFFFF0000u));
+          w[y] = i16 < COLS ? w[y] : rest;
+        }
+      }
 #pragma unroll
       for (int e = 0; e < S::EV; ++e) {
         const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;  // element e of two rows side by side
@@ -916,6 +936,9 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
     if (4 * kb + r < GH) {
 #pragma unroll
       for (int e = 0; e < S::EV; ++e) gl.acc[wave][4 * kb + r][S::EV * i16 + e] = o[e][r];
+    } else if (RESTS && 4 * kb + r >= COLS && 4 * kb + r < COLS + GH) {
+#pragma unroll
+      for (int e = 0; e < S::EV; ++e) s_rest[wave][4 * kb + r - COLS][S::EV * i16 + e] = o[e][r];
     }
   __syncthreads();
 
@@ -937,7 +960,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
   for (int x = 0; x < OUTS; ++x) {
     const int e = tid + x * kThreads, row = e / D, d = e % D;
     if (e >= GH * D) continue;
-    float M = -INFINITY, L = 0.f, v = 0.f;
+    float M = -INFINITY, L = 0.f, v = 0.f, rest = 0.f;
 #pragma unroll
     for (int w = 0; w < kTokenWaves; ++w) M = fmaxf(M, gl.m[w][row]);
     const float m_ref = M > -INFINITY ? M : 0.f;
@@ -946,7 +969,10 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
       const float wgt = exp2_safe(gl.m[w][row] - m_ref);
       L += gl.l[w][row] * wgt;
       v += gl.acc[w][row][d] * wgt;
+      if constexpr (RESTS) rest += s_rest[w][row][d] * wgt;
     }
+    // (where an infinite or NaN element came up both are infinite or NaN, and the first one is what it should be)
+    if constexpr (RESTS) v += not_finite_or_zero(v + rest) == 0.f ? rest : 0.f;
     if (splits == 1) {
       store(row, d, has_weight<true>(L), v / L, M * kLn2 + logf(L));
     } else {
