@@ -17,6 +17,8 @@ element is selected, widened and attended by every head.
 """
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import binding as tb
@@ -223,6 +225,8 @@ class PagedIntervalDecoder:
     since.  Projected keys (of rotated ones) are kept in a cache of their own, contiguous, a tenth of the pages' size; those of single steps are
     projected together on the next prediction step.  All sequences have the same number of rows; pages are the caller's to
     hand out, by writing into the table, before their first row arrives.
+
+    A ``prompt`` or ``step`` that raises counts none of its tokens: it can be made again.
     """
 
     def __init__(self, cache: tb.PagedCache, W, Hq: int, k: int, P: int, radius: int, sink: int = 0, window: int = 0, sm_scale: float = 1.0,
@@ -253,18 +257,27 @@ class PagedIntervalDecoder:
         self.n_waiting = 0  # the last ones of them, whose keys wait
         self.N_pred = None
 
-    def _append(self, q, k, v):
+    @contextlib.contextmanager
+    def _arriving(self, n: int):
+        """The number of rows with n more of every sequence, which count when all calls that take them have been accepted."""
+        N = self.N + n
+        if N > self.Ncap:
+            raise ValueError(f"{self.N} + {n} rows in a cache for {self.Ncap}")
+        self.lens.fill_(N)
+        try:
+            yield N
+        except BaseException:
+            self.lens.fill_(self.N)
+            raise
+        self.N = N
+
+    def _append(self, desc, q, k, v):
         """Rows of n more tokens; returns rotated queries and keys [B n, heads, D]."""
         B, n = q.shape[:2]
         assert q.shape == (self.B, n, self.Hq, self.D) and k.shape == v.shape == (B, n, self.Hkv, self.D)
-        if self.N + n > self.Ncap:
-            raise ValueError(f"{self.N} + {n} rows in a cache for {self.Ncap}")
         q, k, v = (x.reshape(B * n, x.shape[2], self.D) for x in (q, k, v))
-        self.N += n
-        self.lens.fill_(self.N)
         q_rot, k_rot = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        tb.tb_append_paged_kv(tb.make_paged_desc(self.N, self.Hq, self.cache), self.cache, q, k, v, None, self.lens, self.inv_freq, q_rot, k_rot,
-                              interleaved=self.interleaved)
+        tb.tb_append_paged_kv(desc, self.cache, q, k, v, None, self.lens, self.inv_freq, q_rot, k_rot, interleaved=self.interleaved)
         return q_rot, k_rot
 
     def _project(self, keys, first: int) -> None:
@@ -273,9 +286,9 @@ class PagedIntervalDecoder:
         n = keys.shape[2]
         tb.tb_project_keys(tb.make_desc(n, self.Hq, K=keys, Kimp=rows), keys, self.W, rows, 0, n)
 
-    def _project_waiting(self, upto: int) -> None:
+    def _project_waiting(self) -> None:
         if self.n_waiting:
-            self._project(self.waiting[:, :self.n_waiting], upto - self.n_waiting)
+            self._project(self.waiting[:, :self.n_waiting], self.N - self.n_waiting)
             self.n_waiting = 0
 
     def prompt(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> torch.Tensor:
@@ -283,36 +296,40 @@ class PagedIntervalDecoder:
         B, n = q.shape[:2]
         if n == 0:
             return torch.empty_like(q)
-        self._project_waiting(self.N)
-        q_rot, k_rot = self._append(q, k, v)
-        desc = tb.make_paged_desc(self.N, self.Hq, self.cache)
-        out = torch.empty_like(q_rot)
-        tb.tb_paged_attn(desc, self.cache, q_rot, None, self.lens, n, self.sm_scale, out, None, tb.new_workspace(tb.TB_OP_PAGED_ATTN, desc, B * n))
-        self._project(k_rot.view(B, n, self.Hkv, self.D), self.N - n)
+        with self._arriving(n) as N:
+            desc = tb.make_paged_desc(N, self.Hq, self.cache)
+            q_rot, k_rot = self._append(desc, q, k, v)
+            out = torch.empty_like(q_rot)
+            tb.tb_paged_attn(desc, self.cache, q_rot, None, self.lens, n, self.sm_scale, out, None, tb.new_workspace(tb.TB_OP_PAGED_ATTN, desc, B * n))
+            self._project_waiting()
+            self._project(k_rot.view(B, n, self.Hkv, self.D), N - n)
         return out.view(B, n, self.Hq, self.D)
 
     def step(self, t: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_imp: torch.Tensor):
         """Step t: one token of every sequence, q [B, Hq, D], k, v [B, Hkv, D], importance queries [B, Hq, d'].  Returns (out, lse) views
         valid until the next call."""
-        q_rot, k_rot = self._append(q.unsqueeze(1), k.unsqueeze(1), v.unsqueeze(1))
-        N, B = self.N, self.B
+        predict = t % self.P == 0
+        if self.N_pred is None and not predict:
+            raise ValueError(f"step {t} of {self.P} comes before any prediction")
         if self.n_waiting == self.P:
-            self._project_waiting(N - 1)
-        self.waiting[:, self.n_waiting].copy_(k_rot)
-        self.n_waiting += 1
-        desc = tb.make_paged_desc(N, self.Hq, self.cache)
-        if t % self.P == 0:
-            self._project_waiting(N)
-            lists = tb.make_desc(N, self.Hq, Kimp=self.Kimp, D=self.D)
-            tb.tb_score(lists, q_imp, self.Kimp, self.score_scale, self.scores)
-            tb.tb_select_topk(lists, self.scores, self.k, self.sink, self.window, self.idx, self.cnt, self.sel_ws)
-            tb.tb_expand_neighbors(B, self.Hq, N, self.radius, self.mode, self.idx, self.cnt, self.exp_idx, self.exp_cnt)
-            self.N_pred = N
-        if t % self.P == 0 and not self.expand_on_predict:
-            tb.tb_sparse_decode_attn_paged(desc, self.cache, q_rot, self.idx, self.cnt, self.sel_cap, self.sm_scale, self.out, self.lse, self.ws)
-        else:
-            tb.tb_sparse_decode_attn_paged(desc, self.cache, q_rot, self.exp_idx, self.exp_cnt, self.exp_cap, self.sm_scale, self.out, self.lse,
-                                           self.ws, tail_begin=self.N_pred, tail_end=N)
+            self._project_waiting()
+        with self._arriving(1) as N:
+            desc = tb.make_paged_desc(N, self.Hq, self.cache)
+            q_rot, k_rot = self._append(desc, q.unsqueeze(1), k.unsqueeze(1), v.unsqueeze(1))
+            waiting = self.n_waiting + 1
+            self.waiting[:, waiting - 1].copy_(k_rot)
+            if predict:
+                self._project(self.waiting[:, :waiting], N - waiting)
+                lists = tb.make_desc(N, self.Hq, Kimp=self.Kimp, D=self.D)
+                tb.tb_score(lists, q_imp, self.Kimp, self.score_scale, self.scores)
+                tb.tb_select_topk(lists, self.scores, self.k, self.sink, self.window, self.idx, self.cnt, self.sel_ws)
+                tb.tb_expand_neighbors(self.B, self.Hq, N, self.radius, self.mode, self.idx, self.cnt, self.exp_idx, self.exp_cnt)
+            if predict and not self.expand_on_predict:
+                tb.tb_sparse_decode_attn_paged(desc, self.cache, q_rot, self.idx, self.cnt, self.sel_cap, self.sm_scale, self.out, self.lse, self.ws)
+            else:
+                tb.tb_sparse_decode_attn_paged(desc, self.cache, q_rot, self.exp_idx, self.exp_cnt, self.exp_cap, self.sm_scale, self.out, self.lse,
+                                               self.ws, tail_begin=N if predict else self.N_pred, tail_end=N)
+        self.n_waiting, self.N_pred = (0, N) if predict else (waiting, self.N_pred)
         return self.out, self.lse
 
 
