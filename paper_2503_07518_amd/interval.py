@@ -237,7 +237,8 @@ class PagedIntervalDecoder:
         _, self.Hkv, page, self.D = cache.K.shape
         self.B, self.Ncap, dev = cache.table.shape[0], cache.table.shape[1] * page, cache.K.device
         B = self.B
-        assert W.dtype == cache.dtype and W.dim() == 3 and W.shape[1] == self.D
+        assert W.dtype == cache.dtype and W.dim() == 3 and W.is_contiguous() and W.shape[0] in (1, self.Hkv) and W.shape[1] == self.D
+        assert W.shape[2] in (16, 32, 64)  # (of a projected key)
         self.sel_cap = sink + k + window
         self.exp_cap = min(self.Ncap, ((2 * radius + 1) if mode == 0 else 2) * self.sel_cap)
         self.Kimp = torch.zeros((B, self.Hkv, self.Ncap, W.shape[2]), dtype=cache.dtype, device=dev)
@@ -306,9 +307,10 @@ class PagedIntervalDecoder:
         return out.view(B, n, self.Hq, self.D)
 
     def step(self, t: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_imp: torch.Tensor):
-        """Step t: one token of every sequence, q [B, Hq, D], k, v [B, Hkv, D], importance queries [B, Hq, d'].  Returns (out, lse) views
-        valid until the next call."""
+        """Step t: one token of every sequence, q [B, Hq, D], k, v [B, Hkv, D], importance queries [B, Hq, d'] (looked at on prediction
+        steps alone).  Returns (out, lse) views valid until the next call."""
         predict = t % self.P == 0
+        assert not predict or (q_imp.dtype == self.cache.dtype and q_imp.shape == (self.B, self.Hq, self.W.shape[2]) and q_imp.is_contiguous())
         if self.N_pred is None and not predict:
             raise ValueError(f"step {t} of {self.P} comes before any prediction")
         if self.n_waiting == self.P:

@@ -111,3 +111,31 @@ def test_a_step_before_any_prediction(calls):
     with pytest.raises(ValueError, match="prediction"):
         x.step(1, *token())
     assert state(x) == (5, 0, None, [5, 5])
+
+
+@pytest.mark.parametrize("W", [torch.zeros((1, D, d)), torch.zeros((1, 2 * D, d), dtype=BF16), torch.zeros((1, D, 48), dtype=BF16), torch.zeros((1, D, 128), dtype=BF16),
+                               torch.zeros((3, D, d), dtype=BF16), torch.zeros((D, d), dtype=BF16), torch.zeros((1, d, D), dtype=BF16).transpose(1, 2)])
+def test_projections_of_another_type_or_shape(calls, W):
+    with pytest.raises(AssertionError):
+        loop(W=W)
+
+
+@pytest.mark.parametrize("Hw", [1, Hkv])
+def test_importance_queries_of_another_type_or_shape(calls, Hw):
+    """The scores' kernel would read past their end, or as other numbers."""
+    x = loop(W=torch.zeros((Hw, D, 32), dtype=BF16))
+    x.prompt(*tokens(5))
+    was = state(x)
+    *qkv, _ = token()
+    q_imp = torch.zeros((B, Hq, 32), dtype=BF16)
+    for t in (0, 3):
+        calls.clear()
+        for bad in (q_imp.float(), q_imp[..., :16], q_imp[:1], q_imp[:, :4], torch.zeros((B, Hq, 64), dtype=BF16), torch.zeros((B, 1, 32), dtype=BF16),
+                    torch.zeros((B, 32, Hq), dtype=BF16).transpose(1, 2)):
+            with pytest.raises(AssertionError):
+                x.step(t, *qkv, bad)
+        assert not calls and state(x) == was
+        x.step(t, *qkv, q_imp)
+        assert calls
+        x.step(t + 1, *qkv, None)
+        was = state(x)
