@@ -594,11 +594,18 @@ def tb_paged_attn(desc, cache: PagedCache, q, cu, lens, max_new: int, sm_scale: 
 
 def tb_sparse_decode_attn_paged(desc, cache: PagedCache, q, idx, count, max_count: int, sm_scale: float, out, lse, ws, tail_begin: int = 0,
                                 tail_end: int = 0, stream=None) -> None:
-    """tb_sparse_decode_attn over a cache in pages."""
+    """tb_sparse_decode_attn over a cache in pages.  idx: int32 [B, Hq, entries], one list after the other; count: int32 [B, Hq]; out, lse:
+    fp32."""
+    heads = (cache.B, desc.Hq)
     assert q.is_contiguous() and out.is_contiguous() and q.dtype is cache.dtype and out.dtype is torch.float32
-    assert q.shape == out.shape == (desc.B, desc.Hq, desc.D) and desc.B == cache.table.shape[0]
+    assert q.shape == out.shape == (*heads, desc.D) and desc.B == cache.B
+    *lists, entries = idx.shape
+    assert idx.dtype is count.dtype is torch.int32 and tuple(lists) == count.shape == heads and count.is_contiguous()
+    idx_b, idx_h, idx_n = idx.stride()
+    assert max_count <= entries and (entries < 2 or idx_n == 1) and (heads[0] < 2 or idx_b == heads[1] * idx_h)
+    assert lse is None or (lse.dtype is torch.float32 and lse.shape == heads and lse.is_contiguous())
     rc = (_lib or load_library()).tb_sparse_decode_attn_paged(
-        ctypes.byref(desc), cache.ref, q.data_ptr(), idx.data_ptr(), count.data_ptr(), idx.stride(-2), max_count, tail_begin, tail_end, sm_scale,
+        ctypes.byref(desc), cache.ref, q.data_ptr(), idx.data_ptr(), count.data_ptr(), idx_h, max_count, tail_begin, tail_end, sm_scale,
         out.data_ptr(), None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes,
         _stream_on(cache.device, stream, (q, idx, count, out, lse, ws) if _several_devices else ()))
     if rc:
