@@ -926,10 +926,10 @@ tb_status tb_sparse_decode_attn_paged(const tb_cache_desc* d, const tb_paged_cac
   if (tail_begin < 0 || tail_begin > tail_end || tail_end > d->N) return TB_ERR_INVALID_ARG;
   if (d->N == 0 && max_count > 0) return TB_ERR_INVALID_ARG;
   if (!aligned16(q) || max_count + (tail_end - tail_begin) > (int64_t{1} << 30)) return TB_ERR_UNSUPPORTED;
-  // (rows are addressed with 32-bit offsets in units of 16 bytes)
-  const int64_t elt = d->dtype == TB_F32 ? 4 : 2, most = (int64_t{1} << 36) / elt;
-  if (cache->k_stride_p > most / std::max(cache->pages, 1) - cache->page * cache->k_stride_n ||
-      cache->v_stride_p > most / std::max(cache->pages, 1) - cache->page * cache->v_stride_n)
+  // (rows of a head are addressed with 32-bit offsets in units of 16 bytes: the last one ends within 64 GiB of the first one's beginning)
+  const int64_t elt = d->dtype == TB_F32 ? 4 : 2, most = (int64_t{1} << 36) / elt - d->D, further = std::max(cache->pages - 1, 1);
+  if (cache->pages > 1 && (cache->k_stride_p > (most - (cache->page - 1) * cache->k_stride_n) / further ||
+                           cache->v_stride_p > (most - (cache->page - 1) * cache->v_stride_n) / further))
     return TB_ERR_UNSUPPORTED;
   const int64_t units = static_cast<int64_t>(d->B) * d->Hq;
   if (units == 0) return TB_OK;
