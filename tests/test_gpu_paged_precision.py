@@ -1,12 +1,13 @@
-"""How exact the calls on a cache in pages are, against 64 bits: weights of single tokens."""
+"""How exact the calls on a cache in pages are, against 64 bits: weights of single tokens, rotated rows."""
 import math
 
 import pytest
 import torch
 
 from oracle import paged as ref
+from paper_2503_07518_amd import binding as tb
 from paged_util import attn_bounds, close, half_step, make
-from test_gpu_paged import BF, on_gpu, run_attn
+from test_gpu_paged import BF, DEV, F32, inv_freq, on_gpu, run_attn
 
 pytestmark = pytest.mark.gpu
 
@@ -42,3 +43,28 @@ def test_infinite_rows_that_all_see(D):
     out, _ = run_attn(c, D ** -0.5)
     tol, _ = attn_bounds(c, c.q, c.K, c.V, c.N, D ** -0.5, mag.nan_to_num(), want.nan_to_num(posinf=0, neginf=0), exact_weights=True)
     close(out, want, tol.nan_to_num(posinf=1e30) + mag.nan_to_num(posinf=0) * half_step(BF) ** 2 * 1.01 + want.nan_to_num(posinf=0, neginf=0).abs() * half_step(BF) * 1.01)
+
+
+# ---- rotation -----------------------------------------------------------------------------------------
+def rotated(c, f, interleaved, positions=None):
+    """Rotated queries and keys, and the keys in the cache, as the call leaves them."""
+    on_gpu(c)
+    qo, ko = torch.zeros(c.q.shape, dtype=c.dtype, device=DEV), torch.zeros(c.k.shape, dtype=c.dtype, device=DEV)
+    tb.tb_append_paged_kv(c.desc, c.cache, c.q.to(DEV), c.k.to(DEV), c.v.to(DEV), c.cu.to(DEV), c.lens.to(DEV), f.to(DEV), qo, ko,
+                          positions=None if positions is None else positions.to(DEV), interleaved=interleaved)
+    torch.cuda.synchronize()
+    return qo, ko
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,D,rot", [(4, 2, 64, 64), (4, 1, 128, 128), (32, 8, 128, 128), (16, 4, 64, 32), (2, 1, 128, 48)])
+def test_fp32_rows_are_rounded_once(Hq, Hkv, D, rot, interleaved):
+    """Positions below 2^17, where 64 bits leave 2^17 2^-53 of an angle uncertain, in the call's as in the reference's; what is computed in 64 bits
+    from there adds less than 2^-40.  The rest is one rounding: half a step of the result."""
+    c = make(F32, Hq, Hkv, D, 16, [40, 1, 3], [0, 333, 0], seed=rot)
+    positions = torch.randint(0, 1 << 17, (c.T,), generator=c.gen, dtype=torch.int32)
+    f = inv_freq(rot)
+    for at in (None, positions):
+        q, k, _, _ = ref.append(c.q, c.k, c.v, c.K, c.V, c.table, c.cu, c.lens, c.N, f, interleaved, at)
+        for got, x, want in zip(rotated(c, f, interleaved, at), (c.q, c.k), (q, k)):
+            close(got, want, want.abs() * half_step(F32) + x.double().abs().amax(-1, keepdim=True) * 2 * 2.0 ** -35)
