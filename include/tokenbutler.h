@@ -325,7 +325,8 @@ typedef struct tb_token_rows {
  * nothing of theirs is read or written.
  *   angle(t, i) = positions[t] * inv_freq[i]   0 <= i < rot / 2; positions: int32 [T], NULL: the token's row; inv_freq: fp32 [rot / 2]
  *   (x[j], x[k]) -> (x[j] cos - x[k] sin, x[k] cos + x[j] sin)   of q and k, (j, k) = (i, i + rot / 2), or (2i, 2i + 1) if interleaved
- * angles in 64 bits, the rest in 64 (fp32 rows) or in 32 (bf16 rows), rounded at the end; elements from rot on stay as they are.  rot: 0 (no rotation) to D, a multiple of 16.
+ * angles (up to 2^50) to 2^-50 of a turn, the rest in 64 (fp32 rows) or in 32 (bf16 rows), rounded at the end; elements from rot on stay as they are.
+ * rot: 0 (no rotation) to D, a multiple of 16.
  * k goes to K and, unless NULL, to k_out (what tb_project_keys takes); v to V; q, unless NULL, to q_out.  q_out may be q, and k_out k
  * (the same rows with the same strides); otherwise outputs overlap nothing.  No two tokens of a call may have the same row of the same page. */
 tb_status tb_append_paged_kv(const tb_cache_desc* desc, const tb_paged_cache* cache, int64_t T, const int32_t* cu, const int32_t* lens,

@@ -2,8 +2,11 @@
 
 Everything is a torch tensor on the CPU; K, V [pages, Hkv, page, D], table [B, entries], cu [B + 1], lens [B] as in include/tokenbutler.h."""
 import math
+from fractions import Fraction
 
 import torch
+
+PI = Fraction("3.141592653589793238462643383279502884197169399375105820974944592307812")
 
 
 def place(table, b, n, page, pages):
@@ -22,6 +25,13 @@ def tokens(cu, lens, N, max_new=None):
                 yield first + i, b, row
 
 
+def cos_sin(position, inv_freq):
+    """Of position * inv_freq: the product and what is left of its last turn are exact, whatever the position."""
+    angle = Fraction(position) * Fraction(inv_freq)
+    left = float(angle - round(angle / (2 * PI)) * 2 * PI)
+    return math.cos(left), math.sin(left)
+
+
 def append(q, k, v, K, V, table, cu, lens, N, inv_freq, interleaved, positions=None):
     """Returns rotated q and k, and K and V with their new rows, all in 64 bits; tokens that take no part keep what they had as NaN."""
     page, pages = K.shape[2], K.shape[0]
@@ -33,9 +43,8 @@ def append(q, k, v, K, V, table, cu, lens, N, inv_freq, interleaved, positions=N
         for x, out in ((q, q_out), (k, k_out)):
             y = x[t].double().clone()
             for i in range(rot // 2):
-                angle = at * float(inv_freq[i])
                 lo, hi = (2 * i, 2 * i + 1) if interleaved else (i, i + rot // 2)
-                c, s = math.cos(angle), math.sin(angle)
+                c, s = cos_sin(at, float(inv_freq[i]))
                 y[:, lo], y[:, hi] = x[t, :, lo].double() * c - x[t, :, hi].double() * s, x[t, :, hi].double() * c + x[t, :, lo].double() * s
             out[t] = y
         where = place(table, b, row, page, pages)

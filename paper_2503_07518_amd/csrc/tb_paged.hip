@@ -13,8 +13,9 @@ namespace {
 // row) for few; a unit's elements are on their way while the angles are computed.  32 heads on 8, D = 128, bf16: 8192 tokens 45 us, 218 MB at
 // the 4.8 TB/s of a plain copy; 16 tokens 4.4 us.
 //
-// Angles: position times frequency is a product of at most 31 and 24 bits, exact in 64 to 2^-53; in turns, its fraction is taken in
-// 64 bits and is then a number of fp32, so that a far position rotates as exactly as a near one.
+// Angles: position times frequency is a product of at most 31 and 24 bits, two more than a double has, and a far position has 2^31 of its
+// turns in front of the part that counts: the product, and its product with 1 / (2 pi), are sums of two doubles each, so that a far position rotates as
+// exactly as a near one (with one double each, position 2^31 was off by 4e-7).
 // Rows of fp32 are rotated in 64 bits and rounded once (off 64 bits by 1.8e-8 of their norm, 3.5e-8 in 32 bits; 2501 ragged tokens and others, 16 heads
 // on 4, D = 64: 10.9 and 10.8 us); rows of bf16 in 32, whose roundings are 2^-15 of the one that follows.
 template <typename T>
@@ -27,6 +28,15 @@ struct TurnOf<float> {
 };
 __device__ __forceinline__ void sincos_pi(float x, float* sn, float* cs) { sincospif(x, sn, cs); }
 __device__ __forceinline__ void sincos_pi(double x, double* sn, double* cs) { sincospi(x, sn, cs); }
+
+// The part of the last turn of the angle p * f, from -1/2 to 1/2.
+__device__ __forceinline__ double part_of_turn(double p, double f) {
+#pragma clang fp contract(off)
+  constexpr double kHigh = 0x1.45f306dc9c883p-3, kLow = -0x1.6b01ec5417056p-57;  // 1 / (2 pi)
+  const double angle = p * f, angle_low = fma(p, f, -angle);
+  const double turns = angle * kHigh, turns_low = fma(angle, kHigh, -turns) + (angle * kLow + angle_low * kHigh);
+  return (turns - rint(turns)) + turns_low;
+}
 
 struct AppendArgs {
   Pages pages;
@@ -91,10 +101,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_paged_kernel(AppendArgs
     if (u0 == 0 && a.rot > 0) {
       if (tid < a.rot / 2) {
         const double p = a.positions ? a.positions[t] : row;
-        constexpr double kTurns = 0.15915494309189533577;  // 1 / (2 pi)
-        const double turns = p * static_cast<double>(a.inv_freq[tid]) * kTurns;
         Turn sn, cs;
-        sincos_pi(static_cast<Turn>(2.0 * (turns - rint(turns))), &sn, &cs);
+        sincos_pi(static_cast<Turn>(2.0 * part_of_turn(p, a.inv_freq[tid])), &sn, &cs);
         s_cos[tid] = cs;
         s_sin[tid] = sn;
       }

@@ -68,3 +68,16 @@ def test_fp32_rows_are_rounded_once(Hq, Hkv, D, rot, interleaved):
         q, k, _, _ = ref.append(c.q, c.k, c.v, c.K, c.V, c.table, c.cu, c.lens, c.N, f, interleaved, at)
         for got, x, want in zip(rotated(c, f, interleaved, at), (c.q, c.k), (q, k)):
             close(got, want, want.abs() * half_step(F32) + x.double().abs().amax(-1, keepdim=True) * 2 * 2.0 ** -35)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("most", [1.0, 1000.0])
+def test_far_positions(most, interleaved):
+    """Angles of up to 2^41: a turn's part is as exact as at position 1."""
+    c = make(F32, 4, 1, 128, 16, [8, 3], [1, 2], seed=11)
+    positions = torch.tensor([2 ** 31 - 1, -2 ** 31, 999999937, -5, 1 << 30, 131071, 1 << 24, 1234567891, 1, 0, 2 ** 31 - 2], dtype=torch.int32)
+    f = inv_freq(128) * most
+    f[1::7] *= -1
+    q, k, _, _ = ref.append(c.q, c.k, c.v, c.K, c.V, c.table, c.cu, c.lens, c.N, f, interleaved, positions)
+    for got, x, want in zip(rotated(c, f, interleaved, positions), (c.q, c.k), (q, k)):
+        close(got, want, want.abs() * half_step(F32) + x.double().abs().amax(-1, keepdim=True) * 2 * 2.0 ** -40)
