@@ -602,12 +602,12 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void join_kernel(PagedAttnArgs 
 // 16 rows (token, head of the group) as columns of v_mfma_f32_16x16x32_bf16 (16x16x4_f32).  Lane (i, kb) = (lane % 16, lane / 16) loads pieces
 // kb, kb + 4, .. of row i of 16 rows of K, and of the rows 4 kb + v of V the elements EV i .. + EV - 1; accumulator v of the scores
 // is then key 4 kb + v of column i, and element e of V's pieces the column EV i + e of the output, whose accumulator v is that of row 4 kb + v.
-// A wave has two steps' rows in flight.  Splits of all sequences fill the chip once.  32 heads on 8, D = 128, bf16: 32768 rows 26.5 us, 134 MB
-// at 5.1 TB/s, of which 19 are the bytes at a read stream's 7.0; 16 sequences of 9002 to 16384 154 us, 947 MB at 6.1.  Workgroups that share a sequence hand over by tb_attn_merge.h's protocol.
+// A wave has two steps' rows in flight.  Splits of all sequences fill the chip once.  32 heads on 8, D = 128, bf16: 32768 rows 26.8 us, 134 MB
+// at 5.0 TB/s, of which 19 are the bytes at a read stream's 7.0; 16 sequences of 9002 to 16384 154 us, 947 MB at 6.1.  Workgroups that share a sequence hand over by tb_attn_merge.h's protocol.
 //
-// Weights of bf16 calls: up to eight rows leave half of the columns free, which hold the same rows once more and take what the weights of the first half
+// Weights of bf16 calls: up to eight rows leave half of the columns free, which hold the same rows once more and take what the weights of the others
 // lose when they are rounded to bf16, rounded itself: a weight is then off by 2^-16 of it at most, without a product more (32768 rows: outputs off
-// 64 bits by 0.0017 of their norm, which is what bf16 holds, instead of 0.0022; 27.0 us instead of 26.8, the batch of 16 154.4 instead of 154.0).  Nine to
+// 64 bits by 0.0017 of their norm, which is what bf16 holds, instead of 0.0022; 27.5 us instead of 27.3, the batch of 16 155.1 instead of 154.9).  Nine to
 // sixteen rows fill the columns: rounded to bf16, as the chunk_kernel's are.
 constexpr int kTokenWaves = 8;
 // Every row is read once: not kept for anybody (32 heads on 8, D = 128, bf16, plain loads and these: 32768 rows 30.0 and 26.6 us, 16 sequences of
@@ -625,17 +625,19 @@ struct TokenShape {
   static constexpr int EV = D / 16;                  // elements of a row of V for a lane
   static constexpr int VB = EV * sizeof(T);          // ... bytes: 8, 16 or 32
   static constexpr int VP = (VB + 15) / 16;          // ... in pieces of up to 16
+  static constexpr int WAVES_A_SIMD = !F32 && D == 64 ? 4 : 2;  // (two workgroups a compute unit, as token_target counts on, or one)
   static_assert(F32 || GROUPS == 2, "32 keys fill a product");
-  // columns 8 to 15 hold rows 0 to 7 once more, for the rest of their weights
+  // With up to eight rows in bf16, columns 4 j + 2 and 4 j + 3 take the rests of the weights of 4 j and 4 j + 1, so that a lane's accumulators have both.
   static constexpr bool rests(int rows) { return !F32 && rows <= 8; }
+  template <int GH>
+  __device__ static __forceinline__ int row_of(int column) { return rests(GH) ? (column >> 2) * 2 + (column & 1) : column; }
 };
 
 template <typename T, int D, int GH>
-__global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(kTokenWaves * kWave, (TokenShape<T, D>::WAVES_A_SIMD)) void token_kernel(PagedAttnArgs a) {
   using S = TokenShape<T, D>;
   constexpr bool RESTS = S::rests(GH);
   __shared__ GroupLds<D, GH, kTokenWaves> gl;
-  __shared__ __attribute__((aligned(16))) float s_rest[RESTS ? kTokenWaves : 1][RESTS ? GH : 1][D];  // as gl.acc
   __shared__ float s_out[GH * D], s_lse[GH];
   const int tid = threadIdx.x, lane = lane_id(), wave = wave_id();
   const int i16 = lane & 15, kb = lane >> 4;
@@ -695,8 +697,8 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
   if (split >= splits) return;
   const int32_t step_end = step_0 + min((split + 1) * per, steps);
 
-  constexpr int COLS = RESTS ? 8 : 16;  // that hold different rows
-  const int my_row = i16 & (COLS - 1);
+  const int my_row = S::template row_of<GH>(i16);
+  const bool my_rest = RESTS && (i16 & 2) != 0;
   const int32_t my_i = my_row >> a.gs, my_p = s.row + my_i;
   const int32_t my_low = a.window ? my_p - a.window : -1;  // it sees the rows behind this one, up to its own
   const bool mine = my_i < n && my_p >= 0 && my_p < a.tok.N;
@@ -817,7 +819,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
                   const float v = not_finite_or_zero(__uint_as_float(S::F32 ? word : (y ? word & 0xFFFF0000u : word << 16)));
 #pragma unroll
                   for (int j = 0; j < 4; ++j) {
-                    const int32_t p_j = s.row + (((4 * kb + j) & (COLS - 1)) >> a.gs);
+                    const int32_t p_j = s.row + (S::template row_of<GH>(4 * kb + j) >> a.gs);
                     o[w * (S::EV * 4 / S::VB) + y][j] += ((key <= p_j) & (key > (a.window ? p_j - a.window : -1))) ? v : 0.f;
                   }
                 }
@@ -873,7 +875,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
         w[y] = bf16x2(w0, w1);
         if constexpr (RESTS) {
           const uint32_t rest = bf16x2(w0 - __uint_as_float(w[y] << 16), w1 - __uint_as_float(w[y] & 0xFFFF0000u));
-          w[y] = i16 < COLS ? w[y] : rest;
+          w[y] = my_rest ? rest : w[y];
         }
       }
 #pragma unroll
@@ -927,19 +929,23 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
   l += __shfl_xor(l, 16, kWave);
   l += __shfl_xor(l, 32, kWave);
   if (l != l && m == -INFINITY) m = 0.f;  // (scores that are all NaN: the merges leave out what has a reference of -inf)
-  if (lane < GH) {
-    gl.m[wave][lane] = m;
-    gl.l[wave][lane] = l;
+  if (kb == 0 && !my_rest && my_row < GH) {
+    gl.m[wave][my_row] = m;
+    gl.l[wave][my_row] = l;
   }
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
-    if (4 * kb + r < GH) {
+  for (int r = 0; r < (RESTS ? 2 : 4); ++r) {
+    const int row = S::template row_of<GH>(4 * kb + r);
+    if (row < GH) {
 #pragma unroll
-      for (int e = 0; e < S::EV; ++e) gl.acc[wave][4 * kb + r][S::EV * i16 + e] = o[e][r];
-    } else if (RESTS && 4 * kb + r >= COLS && 4 * kb + r < COLS + GH) {
-#pragma unroll
-      for (int e = 0; e < S::EV; ++e) s_rest[wave][4 * kb + r - COLS][S::EV * i16 + e] = o[e][r];
+      for (int e = 0; e < S::EV; ++e) {
+        float v = o[e][r];
+        // (where an infinite or NaN element came up both are infinite or NaN, and the first one is what it should be)
+        if constexpr (RESTS) v = not_finite_or_zero(v + o[e][r + 2]) == 0.f ? v + o[e][r + 2] : v;
+        gl.acc[wave][row][S::EV * i16 + e] = v;
+      }
     }
+  }
   __syncthreads();
 
   // merge the waves; a thread has outputs tid, tid + 512, ... of the GH x D
@@ -960,7 +966,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
   for (int x = 0; x < OUTS; ++x) {
     const int e = tid + x * kThreads, row = e / D, d = e % D;
     if (e >= GH * D) continue;
-    float M = -INFINITY, L = 0.f, v = 0.f, rest = 0.f;
+    float M = -INFINITY, L = 0.f, v = 0.f;
 #pragma unroll
     for (int w = 0; w < kTokenWaves; ++w) M = fmaxf(M, gl.m[w][row]);
     const float m_ref = M > -INFINITY ? M : 0.f;
@@ -969,10 +975,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 2) void token_kernel(PagedAttn
       const float wgt = exp2_safe(gl.m[w][row] - m_ref);
       L += gl.l[w][row] * wgt;
       v += gl.acc[w][row][d] * wgt;
-      if constexpr (RESTS) rest += s_rest[w][row][d] * wgt;
     }
-    // (where an infinite or NaN element came up both are infinite or NaN, and the first one is what it should be)
-    if constexpr (RESTS) v += not_finite_or_zero(v + rest) == 0.f ? rest : 0.f;
     if (splits == 1) {
       store(row, d, has_weight<true>(L), v / L, M * kLn2 + logf(L));
     } else {
