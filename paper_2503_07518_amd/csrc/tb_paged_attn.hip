@@ -104,16 +104,18 @@ __device__ __forceinline__ float over_halves(float x) {
 // outputs transposed (D / 32 blocks of 32 columns of V), running reference and sum.  Four or eight waves share the tiles of K and V, two of each in LDS:
 // while one is worked on, the next one comes straight from memory (global_load_lds, 16 bytes a lane).  The weights of a tile are computed under the
 // products of the next one's scores, and the next one's maximum is looked for under this one's products with V, so that the matrix cores do not
-// wait for the vector units.  Rows in LDS are
-// permuted in pieces of 16 bytes by their number so that neither the rows of K (a piece of 32 rows at once) nor the transposing reads
+// wait for the vector units.  Rows in LDS are permuted in pieces of 16 bytes by their number so that neither the rows of K (a piece of 32 rows at once) nor the transposing reads
 // of V (a column of four rows) meet on a bank.
 //
 // bf16, D = 128: 8192 tokens, 32 heads on 8, 560 us (980 TFLOP/s of what the mask leaves), 1024 over 64000 rows, 64 on 8, 2030 us (1070); a
-// library product of 8192^3 runs at 1350.  Of 2215 us for the latter, before eight waves shared a tile, the products alone were 1170 (at the
-// power limit: 1850 TFLOP/s on random numbers), the reads from LDS another 106, staging 260, exponentials and the rest of the softmax 295.  64 rows
-// a wave would halve the reads of LDS, but leave one wave a SIMD: 3085.  Weights are rounded to bf16, the type of the products (outputs are off 64 bits
-// by 0.0022 of their norm, 0.0016 of it by the rounding of the output): what that loses, as a second part of the weights, would be half as many
-// products again, of a kernel that is bound by them.  fp32, 300 tokens over 30000 rows, 16 heads on 4, D = 64: 358 us, 103 TFLOP/s.
+// library product of 8192^3 runs at 1350.  Of 2215 us for the latter, before eight waves shared a tile, exponentials and the rest of the softmax were
+// 295, staging 258, reads from LDS 106, barriers 19; of the 1537 left the products on their own take 1170 (at the power limit: 1850 TFLOP/s on random
+// numbers), and what the others are is not known.  64 rows a wave would halve the reads of LDS, but leave one wave a SIMD: 3085.  fp32, 300 tokens over
+// 30000 rows, 16 heads on 4: D = 64 354 us, 105 TFLOP/s, D = 128 655, 113.
+//
+// Weights are rounded to bf16, the type of the products (outputs are off 64 bits by 0.0021 to 0.0023 of their norm, bf16 itself by 0.0016): what that
+// loses, as a second part of the weights, would be half as many products again, of a kernel that is bound by them.
+
 // The reference of a row's softmax follows its maximum only when that has moved by more than this (weights stay below 2^8): the
 // accumulators are seldom rescaled.
 constexpr float kLazy = 8.f;
