@@ -298,7 +298,7 @@ tb_status tb_sparse_decode_attn_shared_mx(const tb_cache_desc* desc, const void*
  * K, V : [pages][Hkv][page][D]   element (p,h,r,d) at  p*stride_p + h*stride_h + r*stride_n + d, strides in elements (alignment as above)
  * table: int32, on the device, table_len entries a sequence.  An entry outside [0, pages) is a hole: nothing is written there, and its
  *        rows are attended to by nobody.  Sequences may share pages that are only read.
- * page is a power of two from 16 to 65536.
+ * page is a power of two from 16 to 65536; page * stride_n stays below 2^29 elements (else TB_ERR_UNSUPPORTED, as for a page of another size).
  * Calls take the element type, B, Hq, Hkv and D from the descriptor, and N, the most rows that a sequence has (at most table_len * page);
  * the descriptor's strides are not looked at. */
 typedef struct tb_paged_cache {

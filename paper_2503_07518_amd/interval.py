@@ -293,7 +293,7 @@ class PagedIntervalDecoder:
             self.n_waiting = 0
 
     def prompt(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> torch.Tensor:
-        """The next n tokens of every sequence; their attention over all rows so far, [B, n, Hq, D]."""
+        """The next n tokens of every sequence, B n <= 2^22; their attention over all rows so far, [B, n, Hq, D]."""
         B, n = q.shape[:2]
         if n == 0:
             return torch.empty_like(q)
